@@ -379,6 +379,108 @@ int icq_fast_set(const icq_index *index, const uint8_t *xi, uint8_t *fast_out, v
 int icq_margin(const double *lambda, const uint8_t *xi, int d, double *sigma_out, void *stream);
 
 /*
+ * Training-side operators.  A scoring head W [V][F] over V items (or codewords)
+ * learns to reproduce the lists that icq_search returns: its logits X W^T and
+ * the products of the backward pass run on operands in 8-bit floating point
+ * with one scale per block of 128, and the loss compares the logits with the
+ * lists.  None of these calls needs an index; each works on the current device.
+ * Matrices are row-major, `ld*` is the distance between rows in elements (at
+ * least their length).  Element types of values:
+ */
+#define ICQ_F32 0
+#define ICQ_F16 1
+#define ICQ_BF16 2
+/* 8-bit formats: four bits of exponent and three of mantissa (largest value 448, NaN, no infinities), or five and two (57344) */
+#define ICQ_E4M3 0
+#define ICQ_E5M2 1
+/* scales: any positive 32-bit value, or powers of two only */
+#define ICQ_SCALES_F32 0
+#define ICQ_SCALES_POW2 1
+#define ICQ_BLOCK 128
+#define ICQ_MAX_EXTENT 0x7FFFFF00ll /* rows or columns of a matrix in these calls */
+
+/*
+ * Values x [rows][cols] in 8-bit floating point with a scale per block.  With a
+ * the largest finite magnitude in the block (at least 2^-100) and F the
+ * format's largest value, in 32-bit arithmetic, every operation rounded once:
+ *     s = a / F   or, with ICQ_SCALES_POW2,   s = 2^ceil(log2(a / F)),
+ *     code = the format's value nearest to x * (1 / s), ties to even.
+ * Infinities and NaN do not count for a; they become the format's own (an
+ * infinity in e4m3: NaN).
+ * Either output or both (the other's pointers NULL), from one reading of x:
+ *   codes [rows][cols], scales [..][ceil(cols/128)]: block_rows = 1: a block is
+ *     128 values of a row, scales [rows][..]; block_rows = 128: a 128 x 128 tile,
+ *     scales [ceil(rows/128)][..];
+ *   codes_t [cols][rows], scales_t [..][ceil(rows/128)]: the same of x's
+ *     transpose (block_rows = 1: blocks of 128 down a column of x).
+ * Code rows start on 16 bytes (pointers and ld a multiple of 16, ICQ_ERR_ARG
+ * otherwise); the bytes from a row's end to the next multiple of 16 are zeroed.
+ */
+int icq_block_quantize(const void *x, int x_type, int64_t rows, int64_t cols, int64_t ldx, int format, int scaling,
+                       int block_rows, uint8_t *codes, int64_t ld_codes, float *scales, uint8_t *codes_t,
+                       int64_t ld_codes_t, float *scales_t, void *stream);
+
+/*
+ * Product of two such matrices along their rows:
+ *   out[m][n] = sum_kb sa[m][kb] sb[n][kb] sum_{k in block kb} a[m][k] b[n][k],
+ * a [M][K] in blocks of 1 x 128, b [N][K] in blocks of b_block_rows x 128 (1 or
+ * 128; with 128 the scale is sb[n / 128][kb]), scales and code rows laid out as
+ * icq_block_quantize writes them (what the padding bytes hold does not matter).
+ * Sums are held in 32 bits; out [M][N] of out_type is rounded once.  scaling =
+ * ICQ_SCALES_POW2 promises that every scale is a power of two (as
+ * icq_block_quantize makes them): the matrix instructions then apply them; of
+ * other scales only the exponent would count.  N at most 65535 * 128.
+ * workspace: icq_block_matmul_workspace_bytes(M, N, K) bytes (may be 0: NULL),
+ * 256-byte aligned.
+ * With W held in 128 x 128 blocks as codes and codes_t, and G the gradient of
+ * the logits: X W^T = (X, W), G W = (G, W's codes_t), G^T X = (G's codes_t, X's
+ * codes_t).
+ */
+int icq_block_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K, size_t *out /*host*/);
+int icq_block_matmul(const uint8_t *a, int a_format, int64_t lda, const float *a_scales, const uint8_t *b, int b_format,
+                     int64_t ldb, const float *b_scales, int b_block_rows, int scaling, int64_t M, int64_t N, int64_t K,
+                     void *out, int out_type, int64_t ldo, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Distillation from a teacher's lists.  Row r of logits [R][V] (element type
+ * `type`) gives q = softmax(scale * logits), scale > 0; its list ids / values
+ * [R][topk] gives teacher scores z_j = teacher_scale * value_j.  The lists of
+ * icq_search are such lists: ids, distances, teacher_scale = -1 / temperature.
+ * An entry is a place whose id is below V and whose score is not -inf (padding
+ * is not one, whatever its value); an id listed twice is one entry with the sum
+ * of its probabilities.
+ *   teacher_lse NULL: p_j = exp(z_j - logsumexp of the row's entries),
+ *     loss[r] = sum_j p_j (log p_j - log q_j);
+ *   teacher_lse [R]:  p_j = exp(z_j - teacher_lse[r]), the logsumexp of
+ *     everything the teacher scored; what is left, p_r = max(0, 1 - sum_j p_j),
+ *     is compared with the student's mass off the list, q_r:
+ *     loss[r] gains p_r (log p_r - log q_r)   (not if the list names all V items).
+ *   grad[r][v] = grad_loss[r] * d loss[r] / d logits[r][v]
+ *              = grad_loss[r] * scale * (q_v - p_v)      for listed items,
+ *                grad_loss[r] * scale * c * q_v          for the others,
+ *     c = 1, or 1 - p_r / q_r with teacher_lse; grad_loss NULL: 1.
+ * A row without entries, or whose logits are all -inf, has loss 0 and gradient
+ * 0.  A listed item of positive probability whose logit is -inf: loss +inf.
+ * NaN, and logits of +inf, make the row's loss and gradient NaN.
+ * icq_distill writes loss [R]; stats [R][4] fp32, 16-byte aligned, if not NULL
+ * (what icq_distill_backward reads); and the gradient if grad is not NULL (in
+ * logits' type; grad_loss is then used).  grad may be the logits' own memory
+ * (same pointer, ld_grad = ld), else the two must not overlap.
+ * icq_distill_backward writes the gradient from the logits, the same lists and
+ * the stats of an earlier icq_distill.
+ * R <= ICQ_MAX_Q, 1 <= topk <= ICQ_MAX_TOPK; workspace (icq_distill):
+ * icq_distill_workspace_bytes(R, V) bytes, 256-byte aligned.
+ */
+int icq_distill_workspace_bytes(int64_t R, int64_t V, size_t *out /*host*/);
+int icq_distill(const void *logits, int type, int64_t R, int64_t V, int64_t ld, float scale, const uint32_t *ids,
+                const float *values, int topk, float teacher_scale, const float *teacher_lse, float *loss, float *stats,
+                const float *grad_loss, void *grad, int64_t ld_grad, void *workspace, size_t workspace_bytes,
+                void *stream);
+int icq_distill_backward(const void *logits, int type, int64_t R, int64_t V, int64_t ld, float scale, const uint32_t *ids,
+                         const float *values, int topk, float teacher_scale, const float *teacher_lse,
+                         const float *stats, const float *grad_loss, void *grad, int64_t ld_grad, void *stream);
+
+/*
  * Machine-limit probe, a measurement aid (nothing on the search path uses it): runs one of a few
  * plain kernels `reps` times on `stream`, WAITS for them, and reports the mean launch time in
  * milliseconds (*ms_out, host) and the work one launch did (*units_out, host): bytes read

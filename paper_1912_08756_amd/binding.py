@@ -19,7 +19,7 @@ ICQ_PAD_ID = 0xFFFFFFFF
 ICQ_LUT_W = 256
 
 # name -> (restype, argtypes); mirrors include/icq.h one to one
-_vp, _i, _i64, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_size_t
+_vp, _i, _i64, _sz, _f = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float
 SIGNATURES = {
     "icq_strerror": (ctypes.c_char_p, [_i]),
     "icq_index_create": (_i, [ctypes.POINTER(_vp), _vp, _vp, _i, _i, _i, _i, _i64, _vp]),
@@ -49,6 +49,12 @@ SIGNATURES = {
     "icq_subspace_mask": (_i, [_vp, _i] + [ctypes.c_double] * 6 + [_vp, _vp]),
     "icq_fast_set": (_i, [_vp, _vp, _vp, _vp]),
     "icq_margin": (_i, [_vp, _vp, _i, _vp, _vp]),
+    "icq_block_quantize": (_i, [_vp, _i, _i64, _i64, _i64, _i, _i, _i, _vp, _i64, _vp, _vp, _i64, _vp, _vp]),
+    "icq_block_matmul_workspace_bytes": (_i, [_i64, _i64, _i64, ctypes.POINTER(_sz)]),
+    "icq_block_matmul": (_i, [_vp, _i, _i64, _vp, _vp, _i, _i64, _vp, _i, _i, _i64, _i64, _i64, _vp, _i, _i64, _vp, _sz, _vp]),
+    "icq_distill_workspace_bytes": (_i, [_i64, _i64, ctypes.POINTER(_sz)]),
+    "icq_distill": (_i, [_vp, _i, _i64, _i64, _i64, _f, _vp, _vp, _i, _f, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _sz, _vp]),
+    "icq_distill_backward": (_i, [_vp, _i, _i64, _i64, _i64, _f, _vp, _vp, _i, _f, _vp, _vp, _vp, _vp, _i64, _vp]),
     "icq_machine_probe": (_i, [_i, _vp, _sz, _i, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double), _vp]),
 }
 _lib = None
@@ -324,6 +330,120 @@ def icq_margin(lam, xi, sigma_out):
     d = lam.shape[0]
     _check(load().icq_margin(_dev(lam, torch.float64, (d,)), _dev(xi, torch.uint8, (d,)), d,
                              _dev(sigma_out, torch.float64, (1,)), _stream()), "icq_margin")
+
+
+ICQ_F32, ICQ_F16, ICQ_BF16 = 0, 1, 2
+ICQ_E4M3, ICQ_E5M2 = 0, 1
+ICQ_SCALES_F32, ICQ_SCALES_POW2 = 0, 1
+ICQ_BLOCK = 128
+_TYPES = {torch.float32: ICQ_F32, torch.float16: ICQ_F16, torch.bfloat16: ICQ_BF16}
+_FORMATS = {torch.float8_e4m3fn: ICQ_E4M3, torch.float8_e5m2: ICQ_E5M2}
+
+
+def _rows(t, dtypes, shape, name):
+    """(pointer, code of the dtype, distance between rows) of a matrix whose rows are contiguous."""
+    if not (t.is_cuda and t.dim() == 2 and t.dtype in dtypes):
+        raise TypeError("%s must be a CUDA matrix of %s" % (name, ", ".join(str(d) for d in dtypes)))
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
+    rows, cols = t.shape
+    if (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols):
+        raise ValueError("%s must have contiguous rows that do not overlap (strides %s)" % (name, tuple(t.stride())))
+    # (a single row's stride is of no consequence: any multiple of 16 that covers it will do)
+    return ctypes.c_void_p(t.data_ptr()), dtypes[t.dtype], t.stride(0) if rows > 1 else -(-cols // 16) * 16
+
+
+def _code_rows(t, shape, name, written):
+    """_rows of a code matrix; one that is written has its rows' bytes up to the next multiple of 16 in its own storage."""
+    ptr, fmt, _ = _rows(t, _FORMATS, shape, name)
+    rows, cols = t.shape
+    if written and rows and cols and t.stride(0) % 16 == 0 and t.storage_offset() + (rows - 1) * t.stride(0) + -(-cols // 16) * 16 > t.untyped_storage().nbytes():
+        raise ValueError("%s ends before its last row's next multiple of 16 bytes (see icq_block_codes)" % name)
+    return ptr, fmt, t.stride(0)
+
+
+def icq_block_codes(rows, cols, dtype=torch.float8_e4m3fn, device="cuda"):
+    """An uninitialised [rows][cols] code matrix whose rows start on 16 bytes, as the block calls want them."""
+    return torch.empty((rows, -(-cols // 16) * 16), dtype=torch.uint8, device=device).view(dtype)[:, :cols]
+
+
+def icq_block_quantize(x, codes, scales, codes_t=None, scales_t=None, block_rows=1, pow2=False):
+    """x [rows][cols] f32 / f16 / bf16 -> codes [rows][cols] and / or codes_t [cols][rows] (float8_e4m3fn or float8_e5m2, see
+    icq_block_codes; either may be None) with their scales."""
+    rows, cols = x.shape
+    blocks = lambda n: -(-n // ICQ_BLOCK)
+    xp, x_type, ldx = _rows(x, _TYPES, None, "x")
+    if codes is None and codes_t is None:
+        raise ValueError("codes or codes_t must be given")
+    if codes is not None and codes_t is not None and codes.dtype != codes_t.dtype:
+        raise TypeError("codes and codes_t must have the same dtype")
+    of = lambda n: blocks(n) if block_rows == ICQ_BLOCK else n
+    cp, fmt, ld = _code_rows(codes, (rows, cols), "codes", True) if codes is not None else (None, None, 0)
+    tp, fmt_t, ld_t = _code_rows(codes_t, (cols, rows), "codes_t", True) if codes_t is not None else (None, None, 0)
+    _check(load().icq_block_quantize(
+        xp, x_type, rows, cols, ldx, fmt if codes is not None else fmt_t, ICQ_SCALES_POW2 if pow2 else ICQ_SCALES_F32, int(block_rows),
+        cp, ld, _dev(scales, torch.float32, (of(rows), blocks(cols)), "scales") if codes is not None else None,
+        tp, ld_t, _dev(scales_t, torch.float32, (of(cols), blocks(rows)), "scales_t") if codes_t is not None else None, _stream()),
+        "icq_block_quantize")
+
+
+def icq_block_matmul_workspace_bytes(M, N, K):
+    out = ctypes.c_size_t(0)
+    _check(load().icq_block_matmul_workspace_bytes(M, N, K, ctypes.byref(out)), "icq_block_matmul_workspace_bytes")
+    return int(out.value)
+
+
+def icq_block_matmul(a, a_scales, b, b_scales, out, workspace=None, pow2=False):
+    """out [M][N] f32 / f16 / bf16 = a [M][K] times b [N][K] transposed, both 8-bit codes with their scales; b's scales are
+    [N][ceil(K/128)] or [ceil(N/128)][ceil(K/128)]."""
+    (M, K), N = a.shape, b.shape[0]
+    blocks = lambda n: -(-n // ICQ_BLOCK)
+    ap, fa, lda = _code_rows(a, None, "a", False)
+    bp, fb, ldb = _code_rows(b, (N, K), "b", False)
+    op, out_type, ldo = _rows(out, _TYPES, (M, N), "out")
+    block_rows = 1 if b_scales.shape[0] == N else ICQ_BLOCK
+    _check(load().icq_block_matmul(
+        ap, fa, lda, _dev(a_scales, torch.float32, (M, blocks(K)), "a_scales"), bp, fb, ldb,
+        _dev(b_scales, torch.float32, (N if block_rows == 1 else blocks(N), blocks(K)), "b_scales"), block_rows,
+        ICQ_SCALES_POW2 if pow2 else ICQ_SCALES_F32, M, N, K, op, out_type, ldo,
+        _dev(workspace, torch.uint8, name="workspace"), workspace.numel() if workspace is not None else 0, _stream()), "icq_block_matmul")
+    return out
+
+
+def icq_distill_workspace_bytes(R, V):
+    out = ctypes.c_size_t(0)
+    _check(load().icq_distill_workspace_bytes(R, V, ctypes.byref(out)), "icq_distill_workspace_bytes")
+    return int(out.value)
+
+
+def _distill_lists(logits, ids, values, scale, teacher_scale, teacher_lse):
+    R, V = logits.shape
+    xp, xt, ld = _rows(logits, _TYPES, None, "logits")
+    return (xp, xt, R, V, ld, float(scale), _dev(ids, torch.int32, (R, ids.shape[1]), "ids"),
+            _dev(values, torch.float32, tuple(ids.shape), "values"), ids.shape[1], float(teacher_scale),
+            _dev(teacher_lse, torch.float32, (R,), "teacher_lse"))
+
+
+def icq_distill(logits, ids, values, scale, teacher_scale, teacher_lse, loss, stats=None, grad_loss=None, grad=None, workspace=None):
+    """logits [R][V] f32 / f16 / bf16; ids [R][topk] int32 (item ids as unsigned bits) and values [R][topk] f32, e.g. what icq_search
+    wrote; teacher_lse [R] f32 or None; loss [R] f32; stats [R][4] f32 or None; grad [R][V] in logits' type (may be logits) or None."""
+    R, V = logits.shape
+    gp, _, ldg = _rows(grad, {logits.dtype: 0}, (R, V), "grad") if grad is not None else (None, 0, 0)
+    _check(load().icq_distill(
+        *_distill_lists(logits, ids, values, scale, teacher_scale, teacher_lse), _dev(loss, torch.float32, (R,), "loss"),
+        _dev(stats, torch.float32, (R, 4), "stats"), _dev(grad_loss, torch.float32, (R,), "grad_loss"), gp, ldg,
+        _dev(workspace, torch.uint8, name="workspace"), workspace.numel() if workspace is not None else 0, _stream()), "icq_distill")
+    return loss
+
+
+def icq_distill_backward(logits, ids, values, scale, teacher_scale, teacher_lse, stats, grad_loss, grad):
+    """The gradient from the stats that icq_distill left; grad_loss [R] f32 or None (ones)."""
+    R, V = logits.shape
+    gp, _, ldg = _rows(grad, {logits.dtype: 0}, (R, V), "grad")
+    _check(load().icq_distill_backward(
+        *_distill_lists(logits, ids, values, scale, teacher_scale, teacher_lse), _dev(stats, torch.float32, (R, 4), "stats"),
+        _dev(grad_loss, torch.float32, (R,), "grad_loss"), gp, ldg, _stream()), "icq_distill_backward")
+    return grad
 
 
 ICQ_PROBE_READ, ICQ_PROBE_READ_NT, ICQ_PROBE_LDS_B32, ICQ_PROBE_LDS_B64, ICQ_PROBE_LDS_B128, ICQ_PROBE_VALU, \

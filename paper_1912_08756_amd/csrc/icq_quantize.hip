@@ -1,0 +1,233 @@
+// Values in 8-bit floating point with one scale per block of 128.
+//
+// A block is 128 consecutive values of a row (of a column, for the transposed output), or a 128 x 128 tile.  With a the
+// largest finite magnitude of the block (at least 2^-100) and F the format's largest value,
+//     s = a / F,  or  s = 2^ceil(log2(a / F)) for scales that are powers of two,
+//     code = the format's value nearest to x * (1 / s), ties to even;
+// the quotients and the product are single-precision operations rounded once each.  Infinities and NaN do not count for a and
+// become what the format has for them (e4m3 has no infinity: NaN).
+//
+// Both kernels read every value once and are bound by memory: rows alone need no more than the 16 lanes that hold a block
+// agreeing on its largest value; columns need a 128 x 128 tile in registers, whose codes turn round in the LDS so that
+// either output is written in whole 128-byte pieces.
+#include "icq_types.h"
+
+namespace {
+
+struct Quantize {
+    const void *x;
+    int64_t rows, cols, ldx;
+    uint8_t *codes, *codes_t;
+    int64_t ld, ld_t;
+    float *scales, *scales_t;
+    int across, down;          // blocks of 128 along a row, along a column
+    int pow2;
+    int vec;                   // rows of x start on 16 bytes
+};
+
+// Magnitude's bits for the largest-value search: 0 for infinities and NaN.
+__device__ __forceinline__ uint32_t size_bits(float x) {
+    const uint32_t b = __float_as_uint(x) & 0x7fffffffu;
+    return b < 0x7f800000u ? b : 0u;
+}
+
+// Scale and its reciprocal from the bits of the largest magnitude.
+template <int FORMAT>
+__device__ __forceinline__ void block_scale(uint32_t amax, int pow2, float &s, float &inv) {
+    constexpr uint32_t least = 27u << 23;              // 2^-100
+    amax = amax > least ? amax : least;
+    if (pow2) {                                        // F = 1.75 * 2^8 or 1.75 * 2^15
+        const uint32_t e = (amax >> 23) - (FORMAT == ICQ_E4M3 ? 8u : 15u) + ((amax & 0x7fffffu) > 0x600000u ? 1u : 0u);
+        s = __uint_as_float(e << 23);
+        inv = __uint_as_float((254u - e) << 23);
+    } else {
+        s = __uint_as_float(amax) / (FORMAT == ICQ_E4M3 ? 448.0f : 57344.0f);
+        inv = 1.0f / s;
+    }
+}
+
+// Eight values of row r from column c on, zero where there are none.
+template <int TYPE>
+__device__ __forceinline__ void load8(const Quantize &a, int64_t r, int64_t c, float *x) {
+    typedef IcqElem<TYPE> E;
+    const typename E::raw *p = static_cast<const typename E::raw *>(a.x) + r * a.ldx + c;
+    if (a.vec && c + 8 <= a.cols) {
+#pragma unroll
+        for (int h = 0; h < 8 / E::PER; ++h) E::unpack(reinterpret_cast<const uint4 *>(p)[h], x + h * E::PER);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = c + i < a.cols ? E::get(p[i]) : 0.0f;
+    }
+}
+
+template <int FORMAT>
+__device__ __forceinline__ uint2 codes8(const float *x, float inv) {
+    uint2 w;
+    w.x = icq_codes2<FORMAT, false>(x[0] * inv, x[1] * inv, 0);
+    w.x = icq_codes2<FORMAT, true>(x[2] * inv, x[3] * inv, w.x);
+    w.y = icq_codes2<FORMAT, false>(x[4] * inv, x[5] * inv, 0);
+    w.y = icq_codes2<FORMAT, true>(x[6] * inv, x[7] * inv, w.y);
+    return w;
+}
+
+// Rows: 16 lanes per block of 128, eight values each.
+template <int TYPE, int FORMAT>
+__global__ __launch_bounds__(256) void quantize_rows_kernel(Quantize a, int64_t first_row, uint32_t tasks) {
+    const uint32_t t = blockIdx.x * 16u + threadIdx.x / 16u;
+    if (t >= tasks) return;
+    const uint32_t row = t / (uint32_t)a.across, block = t % (uint32_t)a.across;
+    const int64_t r = first_row + row, c = (int64_t)block * 128 + (threadIdx.x & 15u) * 8;
+    float x[8];
+    load8<TYPE>(a, r, c, x);
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, size_bits(x[i]));
+#pragma unroll
+    for (int d = 1; d < 16; d <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d, 16));
+    float s, inv;
+    block_scale<FORMAT>(m, a.pow2, s, inv);
+    if (c < ((a.cols + 15) & ~(int64_t)15)) *reinterpret_cast<uint2 *>(a.codes + r * a.ld + c) = codes8<FORMAT>(x, inv);
+    if ((threadIdx.x & 15u) == 0) a.scales[r * a.across + block] = s;
+}
+
+// A 128 x 128 tile per block; thread (g, h) holds rows 8 h .. 8 h + 7 of columns 8 g .. 8 g + 7.
+// TILE: one scale for the whole tile, else one per row and column of it.
+template <int TYPE, int FORMAT, bool TILE>
+__global__ __launch_bounds__(256) void quantize_tile_kernel(Quantize a) {
+    __shared__ uint32_t s_max[4][128];
+    __shared__ __attribute__((aligned(16))) uint8_t s_turn[128][144];
+    const int g = threadIdx.x & 15, h = threadIdx.x >> 4, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int bc = blockIdx.x % a.across, br = blockIdx.x / a.across;
+    const int64_t r0 = (int64_t)br * 128 + 8 * h, c0 = (int64_t)bc * 128 + 8 * g;
+    float x[8][8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (r0 + i < a.rows) load8<TYPE>(a, r0 + i, c0, x[i]);
+        else
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[i][j] = 0.0f;
+    }
+    const int64_t wide = (a.cols + 15) & ~(int64_t)15, tall = (a.rows + 15) & ~(int64_t)15;
+    float tile_s = 0.0f, tile_inv = 0.0f;
+    if constexpr (TILE) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) m = max(m, size_bits(x[i][j]));
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d, 64));
+        if (lane == 0) s_max[wave][0] = m;
+        __syncthreads();
+        m = max(max(s_max[0][0], s_max[1][0]), max(s_max[2][0], s_max[3][0]));
+        block_scale<FORMAT>(m, a.pow2, tile_s, tile_inv);
+        if (threadIdx.x == 0) {
+            if (a.codes) a.scales[(int64_t)br * a.across + bc] = tile_s;
+            if (a.codes_t) a.scales_t[(int64_t)bc * a.down + br] = tile_s;
+        }
+    }
+    if (a.codes) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float s = tile_s, inv = tile_inv;
+            if constexpr (!TILE) {
+                uint32_t m = 0;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) m = max(m, size_bits(x[i][j]));
+#pragma unroll
+                for (int d = 1; d < 16; d <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d, 16));
+                block_scale<FORMAT>(m, a.pow2, s, inv);
+            }
+            if (r0 + i < a.rows) {
+                if (c0 < wide) *reinterpret_cast<uint2 *>(a.codes + (r0 + i) * a.ld + c0) = codes8<FORMAT>(x[i], inv);
+                if (!TILE && g == 0) a.scales[(r0 + i) * a.across + bc] = s;
+            }
+        }
+    }
+    if (!a.codes_t) return;
+    float inv_t[8];
+    if constexpr (!TILE) {
+        uint32_t m[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            m[j] = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m[j] = max(m[j], size_bits(x[i][j]));
+            m[j] = max(m[j], (uint32_t)__shfl_xor((int)m[j], 16, 64));
+            m[j] = max(m[j], (uint32_t)__shfl_xor((int)m[j], 32, 64));
+            if (lane < 16) s_max[wave][8 * g + j] = m[j];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int c = 8 * g + j;
+            const uint32_t all = max(max(s_max[0][c], s_max[1][c]), max(s_max[2][c], s_max[3][c]));
+            float s;
+            block_scale<FORMAT>(all, a.pow2, s, inv_t[j]);
+            if (h == 0 && c0 + j < a.cols) a.scales_t[(c0 + j) * a.down + br] = s;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) inv_t[j] = tile_inv;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = x[i][j];
+        *reinterpret_cast<uint2 *>(&s_turn[8 * g + j][8 * h]) = codes8<FORMAT>(y, inv_t[j]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        const int at = u * 256 + threadIdx.x, c = at >> 3, piece = (at & 7) * 16;
+        const int64_t col = (int64_t)bc * 128 + c, row = (int64_t)br * 128 + piece;
+        if (col < a.cols && row < tall)
+            *reinterpret_cast<uint4 *>(a.codes_t + col * a.ld_t + row) = *reinterpret_cast<const uint4 *>(&s_turn[c][piece]);
+    }
+}
+
+template <int TYPE, int FORMAT>
+int launch(const Quantize &a, int block_rows, hipStream_t s) {
+    if (block_rows == 1 && !a.codes_t) {
+        const int64_t step = (int64_t)0x7fffffff / a.across;          // rows whose blocks 32 bits count
+        for (int64_t r = 0; r < a.rows; r += step) {
+            const uint32_t tasks = (uint32_t)((a.rows - r < step ? a.rows - r : step) * a.across);
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(quantize_rows_kernel<TYPE, FORMAT>), dim3((tasks + 15u) / 16u), dim3(256), 0, s, a, r, tasks);
+        }
+    } else if (block_rows == 1) {
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(quantize_tile_kernel<TYPE, FORMAT, false>), dim3((uint32_t)((int64_t)a.across * a.down)), dim3(256), 0, s, a);
+    } else {
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(quantize_tile_kernel<TYPE, FORMAT, true>), dim3((uint32_t)((int64_t)a.across * a.down)), dim3(256), 0, s, a);
+    }
+    return icq_check_launch();
+}
+
+}  // namespace
+
+ICQ_EXPORT int icq_block_quantize(const void *x, int x_type, int64_t rows, int64_t cols, int64_t ldx, int format, int scaling,
+                                  int block_rows, uint8_t *codes, int64_t ld_codes, float *scales, uint8_t *codes_t,
+                                  int64_t ld_codes_t, float *scales_t, void *stream) {
+    const int size = icq_type_bytes(x_type);
+    if (size == 0 || (format != ICQ_E4M3 && format != ICQ_E5M2) || (scaling != ICQ_SCALES_F32 && scaling != ICQ_SCALES_POW2) ||
+        (block_rows != 1 && block_rows != ICQ_BLOCK) || rows < 0 || cols < 0 || rows > ICQ_MAX_EXTENT || cols > ICQ_MAX_EXTENT ||
+        (!codes && !codes_t))
+        return ICQ_ERR_ARG;
+    if (codes && (!scales || ld_codes < cols || ld_codes % 16 != 0 || (uintptr_t)codes % 16 != 0)) return ICQ_ERR_ARG;
+    if (codes_t && (!scales_t || ld_codes_t < rows || ld_codes_t % 16 != 0 || (uintptr_t)codes_t % 16 != 0)) return ICQ_ERR_ARG;
+    if (rows == 0 || cols == 0) return ICQ_OK;
+    if (!x || ldx < cols || (uintptr_t)x % size != 0) return ICQ_ERR_ARG;
+    Quantize a;
+    a.x = x; a.rows = rows; a.cols = cols; a.ldx = ldx;
+    a.codes = codes; a.ld = ld_codes; a.scales = scales;
+    a.codes_t = codes_t; a.ld_t = ld_codes_t; a.scales_t = scales_t;
+    a.across = (int)((cols + 127) / 128);
+    a.down = (int)((rows + 127) / 128);
+    a.pow2 = scaling == ICQ_SCALES_POW2;
+    a.vec = (uintptr_t)x % 16 == 0 && ldx * size % 16 == 0;
+    if ((block_rows != 1 || codes_t) && (int64_t)a.across * a.down > 0x7fffffff) return ICQ_ERR_ARG;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    int rc = ICQ_OK;
+    ICQ_FOR_TYPE(x_type, rc = format == ICQ_E4M3 ? launch<TYPE, ICQ_E4M3>(a, block_rows, s) : launch<TYPE, ICQ_E5M2>(a, block_rows, s))
+    return rc;
+}
