@@ -398,6 +398,7 @@ int icq_margin(const double *lambda, const uint8_t *xi, int d, double *sigma_out
 #define ICQ_SCALES_POW2 1
 #define ICQ_BLOCK 128
 #define ICQ_MAX_EXTENT 0x7FFFFF00ll /* rows or columns of a matrix in these calls */
+#define ICQ_MAX_CODE_LD 0xFFFFF0    /* bytes between rows of a product's operands  */
 
 /*
  * Values x [rows][cols] in 8-bit floating point with a scale per block.  With a
@@ -426,10 +427,13 @@ int icq_block_quantize(const void *x, int x_type, int64_t rows, int64_t cols, in
  * a [M][K] in blocks of 1 x 128, b [N][K] in blocks of b_block_rows x 128 (1 or
  * 128; with 128 the scale is sb[n / 128][kb]), scales and code rows laid out as
  * icq_block_quantize writes them (what the padding bytes hold does not matter).
- * Sums are held in 32 bits; out [M][N] of out_type is rounded once.  scaling =
+ * out [M][N] of out_type is rounded once from sums held in 32 bits; within
+ * each eight neighbouring products of a 16-bit out, terms smaller than about
+ * 2^-13 of the largest are lost (1.4e-5 of the result in the 2-norm for normal
+ * values, below the result's rounding), a 32-bit out takes them all.  scaling =
  * ICQ_SCALES_POW2 promises that every scale is a power of two (as
  * icq_block_quantize makes them): the matrix instructions then apply them; of
- * other scales only the exponent would count.  N at most 65535 * 128.
+ * other scales only the exponent would count.
  * workspace: icq_block_matmul_workspace_bytes(M, N, K) bytes (may be 0: NULL),
  * 256-byte aligned.
  * With W held in 128 x 128 blocks as codes and codes_t, and G the gradient of

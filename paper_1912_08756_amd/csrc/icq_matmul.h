@@ -48,6 +48,15 @@ __device__ __forceinline__ void store4(const Product &p, int64_t m, int64_t n, c
     }
 }
 
+__device__ __forceinline__ void store_part(const Product &p, int split, int64_t m, int64_t n, const icq_f32x4 &v) {
+    float *o = p.part + ((int64_t)split * p.M + m) * p.N + n;
+    if (p.N % 4 == 0 && n < p.N) *reinterpret_cast<icq_f32x4 *>(o) = v;
+    else
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (n + e < p.N) o[e] = v[e];
+}
+
 // The first n < 16 of 16 bytes, zeros after them.
 __device__ __forceinline__ uint4 first_bytes(const uint4 &v, int n) {
     uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -59,13 +68,9 @@ __device__ __forceinline__ uint4 first_bytes(const uint4 &v, int n) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// Bytes of row `r` of a code matrix from position k on, zero beyond the row's K codes and beyond the last row.
-__device__ __forceinline__ uint4 load16(const uint8_t *x, int64_t ld, int64_t rows, int64_t K, int64_t r, int64_t k) {
-    if (r >= rows || k >= K) return make_uint4(0, 0, 0, 0);
-    const uint4 v = *reinterpret_cast<const uint4 *>(x + r * ld + k);
-    return K - k < 16 ? first_bytes(v, (int)(K - k)) : v;
-}
-
-// The 256 x 256 tile kernel (icq_matmul_wide.hip); which products it takes, and its launch.
-bool icq_product_wide_usable(int64_t M, int64_t N, int64_t K, int64_t lda, int64_t ldb, int num_cu);
-int icq_launch_product_wide(const Product &p, int a_format, int b_format, bool rows, bool pow2, int out_type, hipStream_t s);
+// The product in tiles of 256 x 256 (wide) or 128 x 128, p.splits parts of the contraction (icq_matmul_tiles.hip).
+int icq_launch_product_tiles(const Product &p, bool wide, int a_format, int b_format, bool rows, bool pow2, int out_type, hipStream_t s);
+// The product of at most ICQ_FEW_ROWS rows of a (icq_matmul_few.hip).
+#define ICQ_FEW_ROWS 64
+int icq_product_few_splits(int64_t N, int64_t K, int num_cu);
+int icq_launch_product_few(const Product &p, int num_cu, int a_format, int b_format, bool rows, int out_type, hipStream_t s);
