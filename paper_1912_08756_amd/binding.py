@@ -340,26 +340,44 @@ _TYPES = {torch.float32: ICQ_F32, torch.float16: ICQ_F16, torch.bfloat16: ICQ_BF
 _FORMATS = {torch.float8_e4m3fn: ICQ_E4M3, torch.float8_e5m2: ICQ_E5M2}
 
 
-def _rows(t, dtypes, shape, name):
-    """(pointer, code of the dtype, distance between rows) of a matrix whose rows are contiguous."""
-    if not (t.is_cuda and t.dim() == 2 and t.dtype in dtypes):
-        raise TypeError("%s must be a CUDA matrix of %s" % (name, ", ".join(str(d) for d in dtypes)))
-    if shape is not None and tuple(t.shape) != tuple(shape):
+def _raw_stream():
+    """torch's current stream on the current device, without the objects around it (these calls can take a few microseconds)."""
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+
+
+def _ptr(t, dtype, shape, name):
+    """Address of a contiguous device tensor, None for None."""
+    if t is None:
+        return None
+    if t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
+        raise TypeError("%s must be a contiguous CUDA tensor of %s" % (name, dtype))
+    if shape is not None and t.shape != shape:
         raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
+    return t.data_ptr()
+
+
+def _rows(t, dtypes, shape, name):
+    """(address, code of the dtype, distance between rows) of a matrix whose rows are contiguous."""
+    code = dtypes.get(t.dtype)
+    if code is None or not t.is_cuda or t.dim() != 2:
+        raise TypeError("%s must be a CUDA matrix of %s" % (name, ", ".join(str(d) for d in dtypes)))
     rows, cols = t.shape
-    if (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols):
-        raise ValueError("%s must have contiguous rows that do not overlap (strides %s)" % (name, tuple(t.stride())))
-    # (a single row's stride is of no consequence: any multiple of 16 that covers it will do)
-    return ctypes.c_void_p(t.data_ptr()), dtypes[t.dtype], t.stride(0) if rows > 1 else -(-cols // 16) * 16
+    if shape is not None and (rows, cols) != shape:
+        raise ValueError("%s has shape %s, expected %s" % (name, (rows, cols), tuple(shape)))
+    ld, step = t.stride()
+    if (step != 1 and cols > 1) or (ld < cols and rows > 1):
+        raise ValueError("%s must have contiguous rows that do not overlap (strides %s)" % (name, (ld, step)))
+    return t.data_ptr(), code, ld if rows > 1 else max(ld, cols)
 
 
 def _code_rows(t, shape, name, written):
     """_rows of a code matrix; one that is written has its rows' bytes up to the next multiple of 16 in its own storage."""
-    ptr, fmt, _ = _rows(t, _FORMATS, shape, name)
-    rows, cols = t.shape
-    if written and rows and cols and t.stride(0) % 16 == 0 and t.storage_offset() + (rows - 1) * t.stride(0) + -(-cols // 16) * 16 > t.untyped_storage().nbytes():
-        raise ValueError("%s ends before its last row's next multiple of 16 bytes (see icq_block_codes)" % name)
-    return ptr, fmt, t.stride(0)
+    ptr, fmt, ld = _rows(t, _FORMATS, shape, name)
+    if written and ld % 16 == 0:
+        rows, cols = t.shape
+        if rows and cols and t.storage_offset() + (rows - 1) * ld + -(-cols // 16) * 16 > t.untyped_storage().nbytes():
+            raise ValueError("%s ends before its last row's next multiple of 16 bytes (see icq_block_codes)" % name)
+    return ptr, fmt, ld
 
 
 def icq_block_codes(rows, cols, dtype=torch.float8_e4m3fn, device="cuda"):
@@ -370,21 +388,26 @@ def icq_block_codes(rows, cols, dtype=torch.float8_e4m3fn, device="cuda"):
 def icq_block_quantize(x, codes, scales, codes_t=None, scales_t=None, block_rows=1, pow2=False):
     """x [rows][cols] f32 / f16 / bf16 -> codes [rows][cols] and / or codes_t [cols][rows] (float8_e4m3fn or float8_e5m2, see
     icq_block_codes; either may be None) with their scales."""
-    rows, cols = x.shape
-    blocks = lambda n: -(-n // ICQ_BLOCK)
     xp, x_type, ldx = _rows(x, _TYPES, None, "x")
-    if codes is None and codes_t is None:
+    rows, cols = x.shape
+    across, down = -(-cols // ICQ_BLOCK), -(-rows // ICQ_BLOCK)
+    tiles = block_rows == ICQ_BLOCK
+    cp = sp = tp = stp = fmt = None
+    ld = ld_t = 0
+    if codes is not None:
+        cp, fmt, ld = _code_rows(codes, (rows, cols), "codes", True)
+        sp = _ptr(scales, torch.float32, (down if tiles else rows, across), "scales")
+    if codes_t is not None:
+        if codes is not None and codes.dtype != codes_t.dtype:
+            raise TypeError("codes and codes_t must have the same dtype")
+        tp, fmt, ld_t = _code_rows(codes_t, (cols, rows), "codes_t", True)
+        stp = _ptr(scales_t, torch.float32, (across if tiles else cols, down), "scales_t")
+    if fmt is None:
         raise ValueError("codes or codes_t must be given")
-    if codes is not None and codes_t is not None and codes.dtype != codes_t.dtype:
-        raise TypeError("codes and codes_t must have the same dtype")
-    of = lambda n: blocks(n) if block_rows == ICQ_BLOCK else n
-    cp, fmt, ld = _code_rows(codes, (rows, cols), "codes", True) if codes is not None else (None, None, 0)
-    tp, fmt_t, ld_t = _code_rows(codes_t, (cols, rows), "codes_t", True) if codes_t is not None else (None, None, 0)
-    _check(load().icq_block_quantize(
-        xp, x_type, rows, cols, ldx, fmt if codes is not None else fmt_t, ICQ_SCALES_POW2 if pow2 else ICQ_SCALES_F32, int(block_rows),
-        cp, ld, _dev(scales, torch.float32, (of(rows), blocks(cols)), "scales") if codes is not None else None,
-        tp, ld_t, _dev(scales_t, torch.float32, (of(cols), blocks(rows)), "scales_t") if codes_t is not None else None, _stream()),
-        "icq_block_quantize")
+    rc = (_lib or load()).icq_block_quantize(xp, x_type, rows, cols, ldx, fmt, ICQ_SCALES_POW2 if pow2 else ICQ_SCALES_F32, block_rows,
+                                             cp, ld, sp, tp, ld_t, stp, _raw_stream())
+    if rc:
+        _check(rc, "icq_block_quantize")
 
 
 def icq_block_matmul_workspace_bytes(M, N, K):
@@ -396,17 +419,19 @@ def icq_block_matmul_workspace_bytes(M, N, K):
 def icq_block_matmul(a, a_scales, b, b_scales, out, workspace=None, pow2=False):
     """out [M][N] f32 / f16 / bf16 = a [M][K] times b [N][K] transposed, both 8-bit codes with their scales; b's scales are
     [N][ceil(K/128)] or [ceil(N/128)][ceil(K/128)]."""
-    (M, K), N = a.shape, b.shape[0]
-    blocks = lambda n: -(-n // ICQ_BLOCK)
     ap, fa, lda = _code_rows(a, None, "a", False)
+    M, K = a.shape
+    N, blocks = b.shape[0], -(-K // ICQ_BLOCK)
     bp, fb, ldb = _code_rows(b, (N, K), "b", False)
     op, out_type, ldo = _rows(out, _TYPES, (M, N), "out")
     block_rows = 1 if b_scales.shape[0] == N else ICQ_BLOCK
-    _check(load().icq_block_matmul(
-        ap, fa, lda, _dev(a_scales, torch.float32, (M, blocks(K)), "a_scales"), bp, fb, ldb,
-        _dev(b_scales, torch.float32, (N if block_rows == 1 else blocks(N), blocks(K)), "b_scales"), block_rows,
+    rc = (_lib or load()).icq_block_matmul(
+        ap, fa, lda, _ptr(a_scales, torch.float32, (M, blocks), "a_scales"), bp, fb, ldb,
+        _ptr(b_scales, torch.float32, (N if block_rows == 1 else -(-N // ICQ_BLOCK), blocks), "b_scales"), block_rows,
         ICQ_SCALES_POW2 if pow2 else ICQ_SCALES_F32, M, N, K, op, out_type, ldo,
-        _dev(workspace, torch.uint8, name="workspace"), workspace.numel() if workspace is not None else 0, _stream()), "icq_block_matmul")
+        _ptr(workspace, torch.uint8, None, "workspace"), workspace.numel() if workspace is not None else 0, _raw_stream())
+    if rc:
+        _check(rc, "icq_block_matmul")
     return out
 
 
@@ -417,32 +442,36 @@ def icq_distill_workspace_bytes(R, V):
 
 
 def _distill_lists(logits, ids, values, scale, teacher_scale, teacher_lse):
-    R, V = logits.shape
     xp, xt, ld = _rows(logits, _TYPES, None, "logits")
-    return (xp, xt, R, V, ld, float(scale), _dev(ids, torch.int32, (R, ids.shape[1]), "ids"),
-            _dev(values, torch.float32, tuple(ids.shape), "values"), ids.shape[1], float(teacher_scale),
-            _dev(teacher_lse, torch.float32, (R,), "teacher_lse"))
+    (R, V), topk = logits.shape, ids.shape[-1]
+    return (xp, xt, R, V, ld, scale, _ptr(ids, torch.int32, (R, topk), "ids"), _ptr(values, torch.float32, (R, topk), "values"), topk,
+            teacher_scale, _ptr(teacher_lse, torch.float32, (R,), "teacher_lse"))
 
 
 def icq_distill(logits, ids, values, scale, teacher_scale, teacher_lse, loss, stats=None, grad_loss=None, grad=None, workspace=None):
     """logits [R][V] f32 / f16 / bf16; ids [R][topk] int32 (item ids as unsigned bits) and values [R][topk] f32, e.g. what icq_search
     wrote; teacher_lse [R] f32 or None; loss [R] f32; stats [R][4] f32 or None; grad [R][V] in logits' type (may be logits) or None."""
-    R, V = logits.shape
-    gp, _, ldg = _rows(grad, {logits.dtype: 0}, (R, V), "grad") if grad is not None else (None, 0, 0)
-    _check(load().icq_distill(
-        *_distill_lists(logits, ids, values, scale, teacher_scale, teacher_lse), _dev(loss, torch.float32, (R,), "loss"),
-        _dev(stats, torch.float32, (R, 4), "stats"), _dev(grad_loss, torch.float32, (R,), "grad_loss"), gp, ldg,
-        _dev(workspace, torch.uint8, name="workspace"), workspace.numel() if workspace is not None else 0, _stream()), "icq_distill")
+    lists = _distill_lists(logits, ids, values, scale, teacher_scale, teacher_lse)
+    R = lists[2]
+    gp, _, ldg = _rows(grad, {logits.dtype: 0}, (R, lists[3]), "grad") if grad is not None else (None, 0, 0)
+    rc = (_lib or load()).icq_distill(
+        *lists, _ptr(loss, torch.float32, (R,), "loss"), _ptr(stats, torch.float32, (R, 4), "stats"),
+        _ptr(grad_loss, torch.float32, (R,), "grad_loss"), gp, ldg, _ptr(workspace, torch.uint8, None, "workspace"),
+        workspace.numel() if workspace is not None else 0, _raw_stream())
+    if rc:
+        _check(rc, "icq_distill")
     return loss
 
 
 def icq_distill_backward(logits, ids, values, scale, teacher_scale, teacher_lse, stats, grad_loss, grad):
     """The gradient from the stats that icq_distill left; grad_loss [R] f32 or None (ones)."""
-    R, V = logits.shape
-    gp, _, ldg = _rows(grad, {logits.dtype: 0}, (R, V), "grad")
-    _check(load().icq_distill_backward(
-        *_distill_lists(logits, ids, values, scale, teacher_scale, teacher_lse), _dev(stats, torch.float32, (R, 4), "stats"),
-        _dev(grad_loss, torch.float32, (R,), "grad_loss"), gp, ldg, _stream()), "icq_distill_backward")
+    lists = _distill_lists(logits, ids, values, scale, teacher_scale, teacher_lse)
+    R = lists[2]
+    gp, _, ldg = _rows(grad, {logits.dtype: 0}, (R, lists[3]), "grad")
+    rc = (_lib or load()).icq_distill_backward(*lists, _ptr(stats, torch.float32, (R, 4), "stats"),
+                                               _ptr(grad_loss, torch.float32, (R,), "grad_loss"), gp, ldg, _raw_stream())
+    if rc:
+        _check(rc, "icq_distill_backward")
     return grad
 
 

@@ -71,6 +71,6 @@ __device__ __forceinline__ uint4 first_bytes(const uint4 &v, int n) {
 // The product in tiles of 256 x 256 (wide) or 128 x 128, p.splits parts of the contraction (icq_matmul_tiles.hip).
 int icq_launch_product_tiles(const Product &p, bool wide, int a_format, int b_format, bool rows, bool pow2, int out_type, hipStream_t s);
 // The product of at most ICQ_FEW_ROWS rows of a (icq_matmul_few.hip).
-#define ICQ_FEW_ROWS 64
+#define ICQ_FEW_ROWS 32
 int icq_product_few_splits(int64_t N, int64_t K, int num_cu);
 int icq_launch_product_few(const Product &p, int num_cu, int a_format, int b_format, bool rows, int out_type, hipStream_t s);

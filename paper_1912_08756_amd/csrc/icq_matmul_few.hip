@@ -1,4 +1,4 @@
-// Products of 8-bit matrices with block scales for up to 64 rows of a: reading b is all that counts.
+// Products of 8-bit matrices with block scales for up to 32 rows of a: reading b is all that counts.
 //
 // A block of eight wavefronts has 16 NT rows of b; each wavefront takes every eighth scale block of them, straight from memory into
 // the registers in the matrix instruction's layout, the next one requested before the present one is multiplied; a's rows come
@@ -129,8 +129,7 @@ int launch(const Product &p, int num_cu, int out_type, hipStream_t s) {
     };
     const int64_t fill = 16 * (int64_t)num_cu;
     if (p.M <= 16) p.N >= 4 * fill ? go(product_few_kernel<FA, FB, ROWS, EXACT, 1, 4>, 4) : go(product_few_kernel<FA, FB, ROWS, EXACT, 1, 1>, 1);
-    else if (p.M <= 32) p.N >= 2 * fill ? go(product_few_kernel<FA, FB, ROWS, EXACT, 2, 2>, 2) : go(product_few_kernel<FA, FB, ROWS, EXACT, 2, 1>, 1);
-    else go(product_few_kernel<FA, FB, ROWS, EXACT, 4, 1>, 1);
+    else p.N >= 2 * fill ? go(product_few_kernel<FA, FB, ROWS, EXACT, 2, 2>, 2) : go(product_few_kernel<FA, FB, ROWS, EXACT, 2, 1>, 1);
     return icq_check_launch();
 }
 

@@ -86,10 +86,10 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product p, int t
         off_b[u] = (uint32_t)(rb * p.ldb) + piece * 16;
     }
     const i32x4 rsrc_a = bytes_from(p.a + m0 * p.lda), rsrc_b = bytes_from(p.b + n0 * p.ldb);
-    auto load_part = [&](int kb, int buf, int u, int beyond) {                // a quarter of a stage
+    auto load_part = [&](int kb, int buf, int u, uint32_t back) {                // a quarter of a stage
         const uint32_t to = buf * S::STAGE + wave * 1024 + u * WAVES * 1024;
-        load_to_lds(rsrc_a, off_a[u] - beyond, kb * 128, to);
-        load_to_lds(rsrc_b, off_b[u] - beyond, kb * 128, to + T * 128);
+        load_to_lds(rsrc_a, off_a[u] - back, kb * 128, to);
+        load_to_lds(rsrc_b, off_b[u] - back, kb * 128, to + T * 128);
     };
     // the last block's bytes from K on become zero: thread t has row t of the stage (a's rows, then b's)
     auto clear_beyond = [&](int buf) {
@@ -175,23 +175,27 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product p, int t
         for (int h = 0; h < 2; ++h) fb[j][h] = two_pieces(smem + buf * S::STAGE + (T + wn + j * 32 + at) * 128, place[h][0], place[h][1]);
     };
 
-    const int kw = min(k1, whole);                                            // whole blocks: [k0, kw)
-    if (k0 < kw) {
-        const int last = kw - 1;
+    const int kw = min(k1, whole), last = k1 - 1;                             // whole blocks: [k0, kw); a ragged one may follow
+    const uint32_t beyond = piece * 16 >= ragged ? piece * 16 : 0;            // there, pieces beyond the row: any of its bytes will do
+    int block = 0;
+    if (k0 < k1) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) load_part(k0, 0, u, 0);
+        for (int u = 0; u < 4; ++u) load_part(k0, 0, u, k0 == whole ? beyond : 0);
         write_scales(0, read_scales(k0));
-        Four next = read_scales(min(k0 + 4, last));
         __builtin_amdgcn_s_waitcnt(ALL_LOADS);
         __syncthreads();
-        load_part(min(k0 + 1, last), 1, 0, 0);
-        load_part(min(k0 + 1, last), 1, 1, 0);
+    }
+    if (k0 < kw) {
+        Four next = read_scales(min(k0 + 4, last));
+        uint32_t back = min(k0 + 1, last) == whole ? beyond : 0;
+        load_part(min(k0 + 1, last), 1, 0, back);
+        load_part(min(k0 + 1, last), 1, 1, back);
         read_a(0, 0, s_scales);
 #pragma unroll
         for (int j = 0; j < NJ; ++j) read_b(j, 0, s_scales);
         int kb = k0, third = 0;
         do {                                                                  // four blocks: their scales are in the LDS
-            int block = third * 4;
+            block = third * 4;
             third = third == 2 ? 0 : third + 1;
             write_scales(third, next);                                        // (nobody reads that third any more: two barriers since)
             next = read_scales(min(kb + 8, last));
@@ -214,8 +218,11 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product p, int t
 #pragma unroll
                     for (int j = 0; j < NJ; ++j) {
                         // a stage's requests are spread over four parts of the multiplication: all at once they hold up the wavefront
-                        if (i == 0) load_part(min(kb + 1, last), buf ^ 1, 2 + j, 0);
-                        if (i == NI - 1) load_part(min(kb + 2, last), buf, j, 0);
+                        if (i == 0) load_part(min(kb + 1, last), buf ^ 1, 2 + j, back);
+                        if (i == NI - 1) {
+                            back = min(kb + 2, last) == whole ? beyond : 0;
+                            load_part(min(kb + 2, last), buf, j, back);
+                        }
                         multiply(i, j, sc);
                         if (i == NI - 1) {                                    // the next step's first fragments (after the last step: not used)
                             if (j == 0) read_a(0, buf ^ 1, sc_next);
@@ -229,20 +236,17 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product p, int t
         __builtin_amdgcn_s_waitcnt(ALL_LOADS);
         __syncthreads();
     }
-    if (whole >= k0 && whole < k1) {                                          // the ragged end
+    if (k0 < k1 && kw < k1) {                                                // the ragged end: its stage has arrived
+        const int buf = (kw - k0) & 1;
+        const float *sc = s_scales + block * 2 * T;
+        clear_beyond(buf);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) load_part(whole, 0, u, piece * 16 >= ragged ? piece * 16 : 0);     // (pieces beyond the row: any of its bytes will do)
-        s_scales[tid] = scale_row[whole];
-        __builtin_amdgcn_s_waitcnt(ALL_LOADS);
-        __syncthreads();
-        clear_beyond(0);
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) read_b(j, 0, s_scales);
+        for (int j = 0; j < NJ; ++j) read_b(j, buf, sc);
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-            read_a(i, 0, s_scales);
+            read_a(i, buf, sc);
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) multiply(i, j, s_scales);
+            for (int j = 0; j < NJ; ++j) multiply(i, j, sc);
             __builtin_amdgcn_sched_barrier(0);
         }
     }
