@@ -9,16 +9,18 @@
 // Statistics and sums are held in 32 bits.  The mass off the list is summed directly (the listed items are marked bit by bit), not as
 // one minus the listed mass: a student that has learnt its list leaves little there.
 //
-// A row is a one-pass reduction (running maximum, sum rescaled when it moves) and one more pass for the gradient.  Few rows are cut
-// into slices whose partial results a second launch joins; the order of every sum is fixed, so a call gives the same bits each time.
+// A row is a one-pass reduction (running maximum, sum rescaled when it moves) and one more pass for the gradient.  Loss and gradient of
+// many rows: a block per row, what the registers hold of it read once, the rest a second time.  Few rows are cut into slices whose
+// partial results the gradient's launch joins.  The order of every sum is fixed, so a call gives the same bits each time.
 #include "icq_types.h"
 
 #include <float.h>
 
 namespace {
 
-constexpr int T = 256;
+constexpr int T = 256;             // threads where a row is cut into slices
 constexpr int CHUNK = 65536;       // elements marked at a time
+constexpr int SHORT = 128;         // lists of up to so many places take less LDS
 constexpr float LOG2E = 1.44269504088896340736f;
 
 struct Distill {
@@ -36,11 +38,18 @@ struct Distill {
     void *grad;
     int64_t ld_grad;
     int splits;
-    float4 *part;                  // [R][splits] maximum, sum, sum off the list
+    struct Part *part;             // [R][splits]
+};
+
+struct __attribute__((aligned(32))) Part {
+    float m, s, r;                 // maximum, sum, sum off the list
+    float t, p;                    // over the listed items of the slice: sum of p (x - m), sum of p
+    float unused[3];
 };
 
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
 
+template <int N>
 __device__ __forceinline__ float block_sum(float v, float *red) {
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
@@ -48,10 +57,11 @@ __device__ __forceinline__ float block_sum(float v, float *red) {
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
     __syncthreads();
     v = red[0];
-    for (int w = 1; w < (int)blockDim.x / 64; ++w) v += red[w];
+    for (int w = 1; w < N / 64; ++w) v += red[w];
     return v;
 }
 
+template <int N>
 __device__ __forceinline__ float block_max(float v, float *red) {      // NaN does not count
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d, 64));
@@ -59,22 +69,25 @@ __device__ __forceinline__ float block_max(float v, float *red) {      // NaN do
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
     __syncthreads();
     v = red[0];
-    for (int w = 1; w < (int)blockDim.x / 64; ++w) v = fmaxf(v, red[w]);
+    for (int w = 1; w < N / 64; ++w) v = fmaxf(v, red[w]);
     return v;
 }
 
 // The row's list in LDS.  id[j] = ICQ_PAD_ID where position j holds no entry of its own.
+template <int CAP>
 struct List {
-    uint32_t id[ICQ_MAX_TOPK];
-    float p[ICQ_MAX_TOPK], log_p[ICQ_MAX_TOPK];
-    uint32_t slot_id[2 * ICQ_MAX_TOPK];                 // the ids, by hash
+    uint32_t id[CAP];
+    float p[CAP], log_p[CAP];
+    uint32_t slot_id[2 * CAP];     // the ids, by hash
     float red[16];
     uint32_t twice;
 };
 
 // Fills the list; returns the number of entries (distinct ids) and the sum of their probabilities.  All threads of the block.
-__device__ int load_list(const Distill &a, int64_t row, List &l, float &sum_p) {
-    const int tid = threadIdx.x, n = blockDim.x;
+template <int CAP, int N>
+__device__ int load_list(const Distill &a, int64_t row, List<CAP> &l, float &sum_p) {
+    constexpr int n = N, PLACES = (CAP + N - 1) / N;
+    const int tid = threadIdx.x;
     for (int i = tid; i < a.slots; i += n) l.slot_id[i] = ICQ_PAD_ID;
     if (tid == 0) l.twice = 0;
     float top = -INFINITY;
@@ -86,7 +99,7 @@ __device__ int load_list(const Distill &a, int64_t row, List &l, float &sum_p) {
         l.p[j] = entry ? z : -INFINITY;
         if (entry) top = fmaxf(top, z);
     }
-    top = block_max(top, l.red);                       // (its barriers also cover the tables)
+    top = block_max<N>(top, l.red);                       // (its barriers also cover the tables)
     float lse = 0.0f, ref = 0.0f;
     if (a.teacher_lse) {
         ref = a.teacher_lse[row];
@@ -95,7 +108,7 @@ __device__ int load_list(const Distill &a, int64_t row, List &l, float &sum_p) {
         float s = 0.0f;
         for (int j = tid; j < a.topk; j += n)
             if (l.id[j] != ICQ_PAD_ID) s += expf(l.p[j] - top);
-        lse = logf(block_sum(s, l.red));
+        lse = logf(block_sum<N>(s, l.red));
     }
     for (int j = tid; j < a.topk; j += n) {
         const uint32_t id = l.id[j];
@@ -113,11 +126,10 @@ __device__ int load_list(const Distill &a, int64_t row, List &l, float &sum_p) {
     }
     __syncthreads();
     if (l.twice) {                                     // every id's probability to its first place
-        float p[4];
-        bool first[4];
-        static_assert(ICQ_MAX_TOPK <= 4 * T, "places per thread");
+        float p[PLACES];
+        bool first[PLACES];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < PLACES; ++u) {
             const int j = u * n + tid;
             p[u] = 0.0f;
             first[u] = true;
@@ -128,7 +140,7 @@ __device__ int load_list(const Distill &a, int64_t row, List &l, float &sum_p) {
         }
         __syncthreads();
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < PLACES; ++u) {
             const int j = u * n + tid;
             if (j < a.topk && l.id[j] != ICQ_PAD_ID) {
                 if (first[u]) { l.p[j] = p[u]; l.log_p[j] = logf(p[u]); }
@@ -140,8 +152,8 @@ __device__ int load_list(const Distill &a, int64_t row, List &l, float &sum_p) {
     float s = 0.0f, count = 0.0f;
     for (int j = tid; j < a.topk; j += n)
         if (l.id[j] != ICQ_PAD_ID) { s += l.p[j]; count += 1.0f; }
-    sum_p = block_sum(s, l.red);
-    return (int)block_sum(count, l.red);
+    sum_p = block_sum<N>(s, l.red);
+    return (int)block_sum<N>(count, l.red);
 }
 
 // Where a row's elements lie: `head` single elements, `body` groups of PER that start on 16 bytes, then `tail` single ones.
@@ -196,29 +208,40 @@ __device__ __forceinline__ void run_add(Run &a, const float *x, uint32_t listed,
 }
 
 // Block-wide: the join of all threads' runs, in a fixed order.
+template <int N>
 __device__ __forceinline__ Run block_run(Run a, float a2, float *red) {
-    const float m = block_max(a.m, red);
+    const float m = block_max<N>(a.m, red);
     const float f = ex2((a.m - m) * a2);
     Run b;
     b.m = m;
-    b.s = block_sum(a.s * f, red);
-    b.r = block_sum(a.r * f, red);
+    b.s = block_sum<N>(a.s * f, red);
+    b.r = block_sum<N>(a.r * f, red);
     return b;
 }
 
-// Loss and statistics of a row from its sums; all threads of the block.
-template <int TYPE>
-__device__ void finish_row(const Distill &a, int64_t row, List &l, int entries, float sum_p, const Run &run) {
-    typedef IcqElem<TYPE> E;
-    const typename E::raw *x = static_cast<const typename E::raw *>(a.x) + row * a.ld;
+// What the loss needs of the listed items in [from, to) of the row, relative to the maximum m: sum of p (x - m).
+template <int TYPE, int CAP, int N, typename In>
+__device__ __forceinline__ float listed_sum(const Distill &a, const typename IcqElem<TYPE>::raw *x, List<CAP> &l, float m, float *p_sum, In in) {
+    float sum = 0.0f, ps = 0.0f;
+    for (int j = threadIdx.x; j < a.topk; j += N) {
+        const float p = l.p[j];
+        if (l.id[j] != ICQ_PAD_ID && !(p == 0.0f) && in(l.id[j])) {
+            sum += p * (IcqElem<TYPE>::get(x[l.id[j]]) - m);
+            ps += p;
+        }
+    }
+    if (p_sum) *p_sum = block_sum<N>(ps, l.red);
+    return block_sum<N>(sum, l.red);
+}
+
+// Loss and statistics of a row from its sums; listed = sum of p (x - m).  All threads of the block get the statistics.
+template <int CAP, int N>
+__device__ float4 finish_row(const Distill &a, int64_t row, List<CAP> &l, int entries, float sum_p, const Run &run, float listed, bool write) {
     const float log_s = logf(run.s);
     float sum = 0.0f;
-    for (int j = threadIdx.x; j < a.topk; j += blockDim.x) {
-        const float p = l.p[j];
-        if (l.id[j] != ICQ_PAD_ID && !(p == 0.0f)) sum += p * (l.log_p[j] - (a.scale * (E::get(x[l.id[j]]) - run.m) - log_s));
-    }
-    sum = block_sum(sum, l.red);
-    if (threadIdx.x != 0) return;
+    for (int j = threadIdx.x; j < a.topk; j += N)
+        if (l.id[j] != ICQ_PAD_ID && !(l.p[j] == 0.0f)) sum += l.p[j] * (l.log_p[j] + log_s);
+    sum = block_sum<N>(sum, l.red) - a.scale * listed;
     const bool counts = entries > 0 && !(run.s == 0.0f);
     float c = 1.0f;
     if (a.teacher_lse && (int64_t)entries < a.V) {
@@ -226,8 +249,12 @@ __device__ void finish_row(const Distill &a, int64_t row, List &l, int entries, 
         if (p_r > 0.0f) sum += p_r * (logf(p_r) - (logf(run.r) - log_s));
         if (run.r > 0.0f) c = 1.0f - p_r * run.s / run.r;          // (nothing off the list: no item takes c)
     }
-    a.loss[row] = counts ? sum : 0.0f;
-    if (a.stats) a.stats[row] = make_float4(run.m, run.s, c, counts ? 1.0f : 0.0f);
+    const float4 st = make_float4(run.m, run.s, c, counts ? 1.0f : 0.0f);
+    if (write && threadIdx.x == 0) {
+        a.loss[row] = counts ? sum : 0.0f;
+        if (a.stats) a.stats[row] = st;
+    }
+    return st;
 }
 
 // A slice of a row: groups [b0, b1) and single elements [e0, e1) of it (the single ones numbered head first).
@@ -243,8 +270,16 @@ __device__ __forceinline__ Slice slice_of(const Span &s, int k, int splits) {
     return c;
 }
 
+__device__ __forceinline__ bool in_slice(const Span &s, const Slice &c, uint32_t id, int per) {
+    const int64_t v = id, e = v - s.head;
+    if (e >= 0 && e < s.body * per) return e / per >= c.b0 && e / per < c.b1;
+    const int64_t single = e < 0 ? v : v - s.body * per;
+    return single >= c.e0 && single < c.e1;
+}
+
 // Whether the list names item v.
-__device__ __forceinline__ bool on_list(const List &l, int slots, uint32_t v) {
+template <int CAP>
+__device__ __forceinline__ bool on_list(const List<CAP> &l, int slots, uint32_t v) {
     uint32_t at = (v * 0x9E3779B1u) >> 16 & (uint32_t)(slots - 1);
     for (;;) {
         const uint32_t id = l.slot_id[at];
@@ -254,84 +289,127 @@ __device__ __forceinline__ bool on_list(const List &l, int slots, uint32_t v) {
     }
 }
 
-// Sums of a row (splits == 1: and its loss) or of a slice of it.  REST: also those off the list.
-template <int TYPE, bool REST>
-__global__ __launch_bounds__(T) void distill_forward_kernel(Distill a) {
+// Marks the listed items among `count` elements from element `first` on; all threads, two barriers.
+template <int CAP, int N>
+__device__ __forceinline__ void mark(const Distill &a, const List<CAP> &l, uint32_t *bits, int64_t first, int64_t count) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < CHUNK / 32; i += N) bits[i] = 0;
+    __syncthreads();
+    for (int j = threadIdx.x; j < a.topk; j += N) {
+        const int64_t e = (int64_t)l.id[j] - first;
+        if (l.id[j] != ICQ_PAD_ID && e >= 0 && e < count) atomicOr(&bits[e >> 5], 1u << (e & 31));
+    }
+    __syncthreads();
+}
+
+// Sums over groups [b0, b1) of a row, in chunks that can be marked.
+template <int TYPE, bool REST, int CAP, int N>
+__device__ __forceinline__ void run_over(Run &run, const Distill &a, const List<CAP> &l, uint32_t *bits, const uint4 *body, int head, int64_t from,
+                                         int64_t to) {
     typedef IcqElem<TYPE> E;
     constexpr int PER = E::PER, U = 4;
-    __shared__ List l;
+    for (int64_t b0 = from; b0 < to; b0 += CHUNK / PER) {
+        const int n = (int)(to - b0 < CHUNK / PER ? to - b0 : CHUNK / PER);
+        if (REST) mark<CAP, N>(a, l, bits, head + b0 * PER, (int64_t)n * PER);
+        const uint4 *at = body + b0;
+        for (int i = threadIdx.x; i < n; i += U * N) {
+            uint4 w[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (i + u * N < n) w[u] = at[i + u * N];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (i + u * N < n) {
+                    float y[PER];
+                    E::unpack(w[u], y);
+                    const int e = (i + u * N) * PER;
+                    run_add<PER, REST>(run, y, REST ? bits[e >> 5] >> (e & 31) : 0u, a.a2);
+                }
+        }
+    }
+}
+
+// Off-list gradients of one group.
+template <int TYPE>
+__device__ __forceinline__ uint4 gradient_of(const uint4 &w, float m, float a2, float f) {
+    typedef IcqElem<TYPE> E;
+    float y[E::PER];
+    E::unpack(w, y);
+#pragma unroll
+    for (int i = 0; i < E::PER; ++i) y[i] = ex2((y[i] - m) * a2) * f;
+    return E::pack(y);
+}
+
+// Sums of a row (splits == 1: and its loss) or of a slice of it.  REST: also those off the list.
+template <int TYPE, bool REST, int CAP>
+__global__ __launch_bounds__(T) void distill_forward_kernel(Distill a) {
+    typedef IcqElem<TYPE> E;
+    __shared__ List<CAP> l;
     __shared__ uint32_t s_bits[REST ? CHUNK / 32 : 1];
     const int tid = threadIdx.x, k = (int)(blockIdx.x % (uint32_t)a.splits);
     const int64_t row = blockIdx.x / (uint32_t)a.splits;
     const typename E::raw *x = static_cast<const typename E::raw *>(a.x) + row * a.ld;
-    int entries = 0;
     float sum_p = 0.0f;
-    if (REST || a.splits == 1) entries = load_list(a, row, l, sum_p);
+    const int entries = load_list<CAP, T>(a, row, l, sum_p);
     const Span s = span_of<TYPE>(x, a.V);
     const Slice c = slice_of(s, k, a.splits);
-    const uint4 *body = reinterpret_cast<const uint4 *>(x + s.head);
     Run run = {-FLT_MAX, 0.0f, 0.0f};
     for (int64_t i = c.e0 + tid; i < c.e1; i += T) {
-        const int64_t v = i < s.head ? i : i + s.body * PER;
+        const int64_t v = i < s.head ? i : i + s.body * E::PER;
         const float y = E::get(x[v]);
         run_add<1, REST>(run, &y, REST && on_list(l, a.slots, (uint32_t)v) ? 1u : 0u, a.a2);
     }
-    for (int64_t b0 = c.b0; b0 < c.b1; b0 += CHUNK / PER) {
-        const int n = (int)(c.b1 - b0 < CHUNK / PER ? c.b1 - b0 : CHUNK / PER);
-        if (REST) {
-            __syncthreads();
-            for (int i = tid; i < CHUNK / 32; i += T) s_bits[i] = 0;
-            __syncthreads();
-            for (int j = tid; j < a.topk; j += T) {
-                const int64_t e = (int64_t)l.id[j] - s.head - b0 * PER;
-                if (l.id[j] != ICQ_PAD_ID && e >= 0 && e < (int64_t)n * PER) atomicOr(&s_bits[e >> 5], 1u << (e & 31));
-            }
-            __syncthreads();
-        }
-        const uint4 *from = body + b0;
-        for (int i = tid; i < n; i += U * T) {
-            uint4 w[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (i + u * T < n) w[u] = from[i + u * T];
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (i + u * T < n) {
-                    float y[PER];
-                    E::unpack(w[u], y);
-                    const int e = (i + u * T) * PER;
-                    run_add<PER, REST>(run, y, REST ? s_bits[e >> 5] >> (e & 31) : 0u, a.a2);
-                }
+    run_over<TYPE, REST, CAP, T>(run, a, l, s_bits, reinterpret_cast<const uint4 *>(x + s.head), s.head, c.b0, c.b1);
+    run = block_run<T>(run, a.a2, l.red);
+    if (a.splits == 1) {
+        const float listed = listed_sum<TYPE, CAP, T>(a, x, l, run.m, nullptr, [](uint32_t) { return true; });
+        finish_row<CAP, T>(a, row, l, entries, sum_p, run, listed, true);
+    } else {
+        float p;
+        const float listed = listed_sum<TYPE, CAP, T>(a, x, l, run.m, &p, [&](uint32_t id) { return in_slice(s, c, id, E::PER); });
+        if (tid == 0) {
+            const Part part = {run.m, run.s, run.r, listed, p, {0.0f, 0.0f, 0.0f}};
+            a.part[row * a.splits + k] = part;
         }
     }
-    run = block_run(run, a.a2, l.red);
-    if (a.splits == 1) finish_row<TYPE>(a, row, l, entries, sum_p, run);
-    else if (tid == 0) a.part[row * a.splits + k] = make_float4(run.m, run.s, run.r, 0.0f);
 }
 
-// A row's sums from its slices', and its loss.
-template <int TYPE>
-__global__ __launch_bounds__(T) void distill_join_kernel(Distill a) {
-    __shared__ List l;
-    const int64_t row = blockIdx.x;
-    float sum_p;
-    const int entries = load_list(a, row, l, sum_p);
+// A row's sums from its slices'; listed: sum of p (x - m).
+template <int CAP, int N>
+__device__ Run join_row(const Distill &a, int64_t row, List<CAP> &l, float &listed) {
     Run run = {-FLT_MAX, 0.0f, 0.0f};
-    for (int k = threadIdx.x; k < a.splits; k += T) {
-        const float4 p = a.part[row * a.splits + k];
-        const Run b = {p.x, p.y, p.z};
+    for (int k = threadIdx.x; k < a.splits; k += N) {
+        const Part p = a.part[row * a.splits + k];
+        const Run b = {p.m, p.s, p.r};
         run_join(run, b, a.a2);
     }
-    run = block_run(run, a.a2, l.red);
-    finish_row<TYPE>(a, row, l, entries, sum_p, run);
+    run = block_run<N>(run, a.a2, l.red);
+    float t = 0.0f;
+    for (int k = threadIdx.x; k < a.splits; k += N) {
+        const Part p = a.part[row * a.splits + k];
+        if (!(p.p == 0.0f)) t += p.t + p.p * (p.m - run.m);
+    }
+    listed = block_sum<N>(t, l.red);
+    return run;
+}
+
+template <int CAP>
+__global__ __launch_bounds__(T) void distill_join_kernel(Distill a) {
+    __shared__ List<CAP> l;
+    const int64_t row = blockIdx.x;
+    float sum_p, listed;
+    const int entries = load_list<CAP, T>(a, row, l, sum_p);
+    const Run run = join_row<CAP, T>(a, row, l, listed);
+    finish_row<CAP, T>(a, row, l, entries, sum_p, run, listed, true);
 }
 
 // The gradient of a slice of a row.  VEC: logits and gradient rows start at the same place within 16 bytes.
-template <int TYPE, bool VEC>
+// JOIN: the row's sums are still in its slices' (the first block of a row writes the loss), else in the statistics.
+template <int TYPE, bool VEC, bool JOIN, int CAP>
 __global__ __launch_bounds__(T) void distill_backward_kernel(Distill a) {
     typedef IcqElem<TYPE> E;
-    constexpr int PER = E::PER, U = 4;
-    __shared__ List l;
+    constexpr int PER = E::PER, U = 4, PLACES = (CAP + T - 1) / T;
+    __shared__ List<CAP> l;
     const int tid = threadIdx.x, k = (int)(blockIdx.x % (uint32_t)a.splits);
     const int64_t row = blockIdx.x / (uint32_t)a.splits;
     const typename E::raw *x = static_cast<const typename E::raw *>(a.x) + row * a.ld;
@@ -340,7 +418,15 @@ __global__ __launch_bounds__(T) void distill_backward_kernel(Distill a) {
     if (VEC) s = span_of<TYPE>(x, a.V);
     else { s.head = (int)a.V; s.body = 0; s.tail = 0; }
     const Slice c = slice_of(s, k, a.splits);
-    const float4 st = a.stats[row];
+    float sum_p, listed;
+    const int entries = load_list<CAP, T>(a, row, l, sum_p);
+    float4 st;
+    if (JOIN) {
+        const Run run = join_row<CAP, T>(a, row, l, listed);
+        st = finish_row<CAP, T>(a, row, l, entries, sum_p, run, listed, k == 0);
+    } else {
+        st = a.stats[row];
+    }
     const uint4 *body = reinterpret_cast<const uint4 *>(x + s.head);
     uint4 *body_out = reinterpret_cast<uint4 *>(out + s.head);
     if (st.w == 0.0f) {                                // a row that does not count
@@ -348,22 +434,15 @@ __global__ __launch_bounds__(T) void distill_backward_kernel(Distill a) {
         for (int64_t b = c.b0 + tid; b < c.b1; b += T) body_out[b] = make_uint4(0, 0, 0, 0);
         return;
     }
-    float sum_p;
-    load_list(a, row, l, sum_p);
     const float g = (a.grad_loss ? a.grad_loss[row] : 1.0f) * a.scale, q0 = 1.0f / st.y, f = q0 * st.z * g;
     // the listed items of this slice, before anything is written (the gradient may take the logits' place)
-    float mine[ICQ_MAX_TOPK / T];
+    float mine[PLACES];
+    uint32_t here[PLACES];
 #pragma unroll
-    for (int u = 0; u < ICQ_MAX_TOPK / T; ++u) {
+    for (int u = 0; u < PLACES; ++u) {
         const int j = u * T + tid;
-        bool here = false;
-        if (j < a.topk && l.id[j] != ICQ_PAD_ID) {
-            const int64_t v = l.id[j], e = v - s.head;
-            if (e >= 0 && e < s.body * PER) here = e / PER >= c.b0 && e / PER < c.b1;
-            else here = (e < 0 ? v : v - s.body * PER) >= c.e0 && (e < 0 ? v : v - s.body * PER) < c.e1;
-            if (here) mine[u] = (ex2((E::get(x[v]) - st.x) * a.a2) * q0 - l.p[j]) * g;
-        }
-        if (j < a.topk && !here) l.id[j] = ICQ_PAD_ID;
+        here[u] = j < a.topk && l.id[j] != ICQ_PAD_ID && in_slice(s, c, l.id[j], PER) ? l.id[j] : ICQ_PAD_ID;
+        if (here[u] != ICQ_PAD_ID) mine[u] = (ex2((E::get(x[here[u]]) - st.x) * a.a2) * q0 - l.p[j]) * g;
     }
     __syncthreads();
     for (int64_t i = c.e0 + tid; i < c.e1; i += T) {
@@ -377,20 +456,83 @@ __global__ __launch_bounds__(T) void distill_backward_kernel(Distill a) {
             if (b + u * T < c.b1) w[u] = body[b + u * T];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (b + u * T < c.b1) {
-                float y[PER];
-                E::unpack(w[u], y);
-#pragma unroll
-                for (int i = 0; i < PER; ++i) y[i] = ex2((y[i] - st.x) * a.a2) * f;
-                body_out[b + u * T] = E::pack(y);
-            }
+            if (b + u * T < c.b1) body_out[b + u * T] = gradient_of<TYPE>(w[u], st.x, a.a2, f);
     }
     __syncthreads();                                   // the listed items' values replace the ones just written
 #pragma unroll
-    for (int u = 0; u < ICQ_MAX_TOPK / T; ++u) {
-        const int j = u * T + tid;
-        if (j < a.topk && l.id[j] != ICQ_PAD_ID) out[l.id[j]] = E::put(mine[u]);
+    for (int u = 0; u < PLACES; ++u)
+        if (here[u] != ICQ_PAD_ID) out[here[u]] = E::put(mine[u]);
+}
+
+// Loss and gradient of a whole row: N threads, the first N * NV groups of 16 bytes stay in registers.
+template <int TYPE, bool REST, int CAP, int N, int NV>
+__global__ __launch_bounds__(N, NV <= 4 ? 5 : 4) void distill_row_kernel(Distill a) {
+    typedef IcqElem<TYPE> E;
+    constexpr int PER = E::PER, U = 4, PLACES = (CAP + N - 1) / N;
+    static_assert(N * NV * PER <= CHUNK, "one marking covers the registers");
+    __shared__ List<CAP> l;
+    __shared__ uint32_t s_bits[REST ? CHUNK / 32 : 1];
+    const int tid = threadIdx.x;
+    const int64_t row = blockIdx.x;
+    const typename E::raw *x = static_cast<const typename E::raw *>(a.x) + row * a.ld;
+    typename E::raw *out = static_cast<typename E::raw *>(a.grad) + row * a.ld_grad;
+    const Span s = span_of<TYPE>(x, a.V);
+    const uint4 *body = reinterpret_cast<const uint4 *>(x + s.head);
+    uint4 *body_out = reinterpret_cast<uint4 *>(out + s.head);
+    const int held = (int)(s.body < N * NV ? s.body : N * NV);
+    uint4 w[NV];
+#pragma unroll
+    for (int u = 0; u < NV; ++u)
+        if (u * N + tid < held) w[u] = body[u * N + tid];
+    const bool single = tid < s.head + s.tail;         // (fewer than 16 of them)
+    const int64_t v1 = tid < s.head ? tid : tid + s.body * PER;
+    const float y1 = single ? E::get(x[v1]) : 0.0f;
+    float sum_p;
+    const int entries = load_list<CAP, N>(a, row, l, sum_p);
+    Run run = {-FLT_MAX, 0.0f, 0.0f};
+    if (single) run_add<1, REST>(run, &y1, REST && on_list(l, a.slots, (uint32_t)v1) ? 1u : 0u, a.a2);
+    if (REST) mark<CAP, N>(a, l, s_bits, s.head, (int64_t)held * PER);
+#pragma unroll
+    for (int u = 0; u < NV; ++u)
+        if (u * N + tid < held) {
+            float y[PER];
+            E::unpack(w[u], y);
+            const int e = (u * N + tid) * PER;
+            run_add<PER, REST>(run, y, REST ? s_bits[e >> 5] >> (e & 31) : 0u, a.a2);
+        }
+    run_over<TYPE, REST, CAP, N>(run, a, l, s_bits, body, s.head, held, s.body);
+    run = block_run<N>(run, a.a2, l.red);
+    const float listed = listed_sum<TYPE, CAP, N>(a, x, l, run.m, nullptr, [](uint32_t) { return true; });
+    const float4 st = finish_row<CAP, N>(a, row, l, entries, sum_p, run, listed, true);
+    const bool counts = st.w != 0.0f;
+    const float g = (a.grad_loss ? a.grad_loss[row] : 1.0f) * a.scale, q0 = 1.0f / st.y, f = q0 * st.z * g;
+    float mine[PLACES];
+    uint32_t here[PLACES];
+#pragma unroll
+    for (int u = 0; u < PLACES; ++u) {
+        const int j = u * N + tid;
+        here[u] = counts && j < a.topk ? l.id[j] : ICQ_PAD_ID;
+        if (here[u] != ICQ_PAD_ID) mine[u] = (ex2((E::get(x[here[u]]) - st.x) * a.a2) * q0 - l.p[j]) * g;
     }
+    __syncthreads();
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    if (single) out[v1] = E::put(counts ? ex2((y1 - st.x) * a.a2) * f : 0.0f);
+#pragma unroll
+    for (int u = 0; u < NV; ++u)
+        if (u * N + tid < held) body_out[u * N + tid] = counts ? gradient_of<TYPE>(w[u], st.x, a.a2, f) : zero;
+    for (int64_t b = s.body - 1 - tid; b >= held; b -= U * N) {        // from the end: what was read last is nearest
+        uint4 r[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (b - u * N >= held) r[u] = body[b - u * N];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (b - u * N >= held) body_out[b - u * N] = counts ? gradient_of<TYPE>(r[u], st.x, a.a2, f) : zero;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < PLACES; ++u)
+        if (here[u] != ICQ_PAD_ID) out[here[u]] = E::put(mine[u]);
 }
 
 // Slices per row: enough blocks for the chip, none shorter than 8192 elements.
@@ -400,7 +542,7 @@ int splits_of(int64_t R, int64_t V, int num_cu) {
     return (int)(n < 1 ? 1 : n > 1024 ? 1024 : n);
 }
 
-size_t part_bytes(int64_t R, int splits) { return icq_align_up((size_t)R * splits * sizeof(float4), ICQ_ALIGN); }
+size_t part_bytes(int64_t R, int splits) { return icq_align_up((size_t)R * splits * sizeof(Part), ICQ_ALIGN); }
 
 bool shape_ok(const void *logits, int type, int64_t R, int64_t V, int64_t ld, float scale, const uint32_t *ids, const float *values,
               int topk, float teacher_scale) {
@@ -424,14 +566,34 @@ Distill params(const void *logits, int64_t R, int64_t V, int64_t ld, float scale
     return a;
 }
 
-int launch_backward(const Distill &a, int type, hipStream_t s) {
-    const int size = icq_type_bytes(type);
-    const bool vec = ((uintptr_t)a.grad - (uintptr_t)a.x) % 16 == 0 && ((a.ld_grad - a.ld) * size) % 16 == 0;
+// Logits and gradient rows start at the same place within 16 bytes.
+bool same_phase(const Distill &a, int size) {
+    return ((uintptr_t)a.grad - (uintptr_t)a.x) % 16 == 0 && ((a.ld_grad - a.ld) * size) % 16 == 0;
+}
+
+template <int TYPE, int CAP>
+void launch_backward(const Distill &a, bool join, hipStream_t s) {
     const dim3 grid((uint32_t)(a.R * a.splits));
-    ICQ_FOR_TYPE(type,
-        if (vec) hipLaunchKernelGGL(HIP_KERNEL_NAME(distill_backward_kernel<TYPE, true>), grid, dim3(T), 0, s, a);
-        else hipLaunchKernelGGL(HIP_KERNEL_NAME(distill_backward_kernel<TYPE, false>), grid, dim3(T), 0, s, a))
-    return icq_check_launch();
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(T), 0, s, a); };
+    if (same_phase(a, sizeof(typename IcqElem<TYPE>::raw))) join ? go(distill_backward_kernel<TYPE, true, true, CAP>) : go(distill_backward_kernel<TYPE, true, false, CAP>);
+    else join ? go(distill_backward_kernel<TYPE, false, true, CAP>) : go(distill_backward_kernel<TYPE, false, false, CAP>);
+}
+
+template <int TYPE, bool REST, int CAP>
+void launch_distill(const Distill &a, hipStream_t s) {
+    constexpr int SIZE = sizeof(typename IcqElem<TYPE>::raw);
+    if (a.grad && a.splits == 1 && same_phase(a, SIZE)) {
+        // threads and held groups by the row's length: 16 KB, 64 KB, 128 KB and the rest twice
+        auto go = [&](auto kernel, int n) { hipLaunchKernelGGL(kernel, dim3((uint32_t)a.R), dim3(n), 0, s, a); };
+        const int64_t bytes = a.V * SIZE;
+        if (bytes <= 256 * 4 * 16) go(distill_row_kernel<TYPE, REST, CAP, 256, 4>, 256);
+        else if (bytes <= 512 * 8 * 16) go(distill_row_kernel<TYPE, REST, CAP, 512, 8>, 512);
+        else go(distill_row_kernel<TYPE, REST, CAP, 512, 16>, 512);
+        return;
+    }
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(distill_forward_kernel<TYPE, REST, CAP>), dim3((uint32_t)(a.R * a.splits)), dim3(T), 0, s, a);
+    if (a.grad) launch_backward<TYPE, CAP>(a, a.splits > 1, s);
+    else if (a.splits > 1) hipLaunchKernelGGL(HIP_KERNEL_NAME(distill_join_kernel<CAP>), dim3((uint32_t)a.R), dim3(T), 0, s, a);
 }
 
 bool grad_ok(const void *logits, int type, int64_t V, int64_t ld, const void *grad, int64_t ld_grad) {
@@ -460,18 +622,16 @@ ICQ_EXPORT int icq_distill(const void *logits, int type, int64_t R, int64_t V, i
     a.splits = splits_of(R, V, cu);
     const size_t parts = part_bytes(R, a.splits);
     if (!workspace || (uintptr_t)workspace % ICQ_ALIGN != 0 || workspace_bytes < parts + part_bytes(R, 1)) return ICQ_ERR_WORKSPACE;
-    a.part = static_cast<float4 *>(workspace);
+    a.part = static_cast<Part *>(workspace);
     a.loss = loss;
     a.stats = stats ? reinterpret_cast<float4 *>(stats) : reinterpret_cast<float4 *>(static_cast<char *>(workspace) + parts);
     a.grad_loss = grad_loss; a.grad = grad; a.ld_grad = ld_grad;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const dim3 grid((uint32_t)(R * a.splits));
+    const bool few = topk <= SHORT;
     ICQ_FOR_TYPE(type,
-        if (teacher_lse) hipLaunchKernelGGL(HIP_KERNEL_NAME(distill_forward_kernel<TYPE, true>), grid, dim3(T), 0, s, a);
-        else hipLaunchKernelGGL(HIP_KERNEL_NAME(distill_forward_kernel<TYPE, false>), grid, dim3(T), 0, s, a);
-        if (a.splits > 1) hipLaunchKernelGGL(HIP_KERNEL_NAME(distill_join_kernel<TYPE>), dim3((uint32_t)R), dim3(T), 0, s, a))
-    const int rc = icq_check_launch();
-    return rc == ICQ_OK && grad ? launch_backward(a, type, s) : rc;
+        if (teacher_lse) few ? launch_distill<TYPE, true, SHORT>(a, s) : launch_distill<TYPE, true, ICQ_MAX_TOPK>(a, s);
+        else few ? launch_distill<TYPE, false, SHORT>(a, s) : launch_distill<TYPE, false, ICQ_MAX_TOPK>(a, s))
+    return icq_check_launch();
 }
 
 ICQ_EXPORT int icq_distill_backward(const void *logits, int type, int64_t R, int64_t V, int64_t ld, float scale, const uint32_t *ids,
@@ -486,5 +646,7 @@ ICQ_EXPORT int icq_distill_backward(const void *logits, int type, int64_t R, int
     a.splits = splits_of(R, V, cu);
     a.stats = reinterpret_cast<float4 *>(const_cast<float *>(stats));
     a.grad_loss = grad_loss; a.grad = grad; a.ld_grad = ld_grad;
-    return launch_backward(a, type, static_cast<hipStream_t>(stream));
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    ICQ_FOR_TYPE(type, topk <= SHORT ? launch_backward<TYPE, SHORT>(a, false, s) : launch_backward<TYPE, ICQ_MAX_TOPK>(a, false, s))
+    return icq_check_launch();
 }
