@@ -78,14 +78,15 @@ template <int CAP>
 struct List {
     uint32_t id[CAP];
     float p[CAP], log_p[CAP];
+    float x[CAP];                  // the student's logit
     uint32_t slot_id[2 * CAP];     // the ids, by hash
     float red[16];
     uint32_t twice;
 };
 
-// Fills the list; returns the number of entries (distinct ids) and the sum of their probabilities.  All threads of the block.
-template <int CAP, int N>
-__device__ int load_list(const Distill &a, int64_t row, List<CAP> &l, float &sum_p) {
+// Fills the list (x: the row's logits, read at those listed places that `in` takes, early: they share lines with what is read next); returns the number of entries (distinct ids) and the sum of their probabilities.  All threads of the block.
+template <int TYPE, int CAP, int N, typename In>
+__device__ int load_list(const Distill &a, int64_t row, const typename IcqElem<TYPE>::raw *x, List<CAP> &l, float &sum_p, In in) {
     constexpr int n = N, PLACES = (CAP + N - 1) / N;
     const int tid = threadIdx.x;
     for (int i = tid; i < a.slots; i += n) l.slot_id[i] = ICQ_PAD_ID;
@@ -97,6 +98,7 @@ __device__ int load_list(const Distill &a, int64_t row, List<CAP> &l, float &sum
         const bool entry = (int64_t)id < a.V && !(z == -INFINITY);
         l.id[j] = entry ? id : ICQ_PAD_ID;
         l.p[j] = entry ? z : -INFINITY;
+        if (entry && in(id)) l.x[j] = IcqElem<TYPE>::get(x[id]);
         if (entry) top = fmaxf(top, z);
     }
     top = block_max<N>(top, l.red);                       // (its barriers also cover the tables)
@@ -219,14 +221,14 @@ __device__ __forceinline__ Run block_run(Run a, float a2, float *red) {
     return b;
 }
 
-// What the loss needs of the listed items in [from, to) of the row, relative to the maximum m: sum of p (x - m).
-template <int TYPE, int CAP, int N, typename In>
-__device__ __forceinline__ float listed_sum(const Distill &a, const typename IcqElem<TYPE>::raw *x, List<CAP> &l, float m, float *p_sum, In in) {
+// What the loss needs of those listed items that `in` takes, relative to the maximum m: sum of p (x - m).
+template <int CAP, int N, typename In>
+__device__ __forceinline__ float listed_sum(const Distill &a, List<CAP> &l, float m, float *p_sum, In in) {
     float sum = 0.0f, ps = 0.0f;
     for (int j = threadIdx.x; j < a.topk; j += N) {
         const float p = l.p[j];
         if (l.id[j] != ICQ_PAD_ID && !(p == 0.0f) && in(l.id[j])) {
-            sum += p * (IcqElem<TYPE>::get(x[l.id[j]]) - m);
+            sum += p * (l.x[j] - m);
             ps += p;
         }
     }
@@ -350,9 +352,10 @@ __global__ __launch_bounds__(T) void distill_forward_kernel(Distill a) {
     const int64_t row = blockIdx.x / (uint32_t)a.splits;
     const typename E::raw *x = static_cast<const typename E::raw *>(a.x) + row * a.ld;
     float sum_p = 0.0f;
-    const int entries = load_list<CAP, T>(a, row, l, sum_p);
     const Span s = span_of<TYPE>(x, a.V);
     const Slice c = slice_of(s, k, a.splits);
+    const auto in = [&](uint32_t id) { return in_slice(s, c, id, E::PER); };
+    const int entries = load_list<TYPE, CAP, T>(a, row, x, l, sum_p, in);
     Run run = {-FLT_MAX, 0.0f, 0.0f};
     for (int64_t i = c.e0 + tid; i < c.e1; i += T) {
         const int64_t v = i < s.head ? i : i + s.body * E::PER;
@@ -362,11 +365,11 @@ __global__ __launch_bounds__(T) void distill_forward_kernel(Distill a) {
     run_over<TYPE, REST, CAP, T>(run, a, l, s_bits, reinterpret_cast<const uint4 *>(x + s.head), s.head, c.b0, c.b1);
     run = block_run<T>(run, a.a2, l.red);
     if (a.splits == 1) {
-        const float listed = listed_sum<TYPE, CAP, T>(a, x, l, run.m, nullptr, [](uint32_t) { return true; });
+        const float listed = listed_sum<CAP, T>(a, l, run.m, nullptr, [](uint32_t) { return true; });
         finish_row<CAP, T>(a, row, l, entries, sum_p, run, listed, true);
     } else {
         float p;
-        const float listed = listed_sum<TYPE, CAP, T>(a, x, l, run.m, &p, [&](uint32_t id) { return in_slice(s, c, id, E::PER); });
+        const float listed = listed_sum<CAP, T>(a, l, run.m, &p, in);
         if (tid == 0) {
             const Part part = {run.m, run.s, run.r, listed, p, {0.0f, 0.0f, 0.0f}};
             a.part[row * a.splits + k] = part;
@@ -393,12 +396,12 @@ __device__ Run join_row(const Distill &a, int64_t row, List<CAP> &l, float &list
     return run;
 }
 
-template <int CAP>
+template <int TYPE, int CAP>
 __global__ __launch_bounds__(T) void distill_join_kernel(Distill a) {
     __shared__ List<CAP> l;
     const int64_t row = blockIdx.x;
     float sum_p, listed;
-    const int entries = load_list<CAP, T>(a, row, l, sum_p);
+    const int entries = load_list<TYPE, CAP, T>(a, row, nullptr, l, sum_p, [](uint32_t) { return false; });
     const Run run = join_row<CAP, T>(a, row, l, listed);
     finish_row<CAP, T>(a, row, l, entries, sum_p, run, listed, true);
 }
@@ -419,7 +422,9 @@ __global__ __launch_bounds__(T) void distill_backward_kernel(Distill a) {
     else { s.head = (int)a.V; s.body = 0; s.tail = 0; }
     const Slice c = slice_of(s, k, a.splits);
     float sum_p, listed;
-    const int entries = load_list<CAP, T>(a, row, l, sum_p);
+    // (listed items of other slices may have their gradients already, where those take the logits' place)
+    const auto in = [&](uint32_t id) { return in_slice(s, c, id, PER); };
+    const int entries = load_list<TYPE, CAP, T>(a, row, x, l, sum_p, in);
     float4 st;
     if (JOIN) {
         const Run run = join_row<CAP, T>(a, row, l, listed);
@@ -435,14 +440,14 @@ __global__ __launch_bounds__(T) void distill_backward_kernel(Distill a) {
         return;
     }
     const float g = (a.grad_loss ? a.grad_loss[row] : 1.0f) * a.scale, q0 = 1.0f / st.y, f = q0 * st.z * g;
-    // the listed items of this slice, before anything is written (the gradient may take the logits' place)
+    // the listed items of this slice
     float mine[PLACES];
     uint32_t here[PLACES];
 #pragma unroll
     for (int u = 0; u < PLACES; ++u) {
         const int j = u * T + tid;
-        here[u] = j < a.topk && l.id[j] != ICQ_PAD_ID && in_slice(s, c, l.id[j], PER) ? l.id[j] : ICQ_PAD_ID;
-        if (here[u] != ICQ_PAD_ID) mine[u] = (ex2((E::get(x[here[u]]) - st.x) * a.a2) * q0 - l.p[j]) * g;
+        here[u] = j < a.topk && l.id[j] != ICQ_PAD_ID && in(l.id[j]) ? l.id[j] : ICQ_PAD_ID;
+        if (here[u] != ICQ_PAD_ID) mine[u] = (ex2((l.x[j] - st.x) * a.a2) * q0 - l.p[j]) * g;
     }
     __syncthreads();
     for (int64_t i = c.e0 + tid; i < c.e1; i += T) {
@@ -488,7 +493,7 @@ __global__ __launch_bounds__(N, NV <= 4 ? 5 : 4) void distill_row_kernel(Distill
     const int64_t v1 = tid < s.head ? tid : tid + s.body * PER;
     const float y1 = single ? E::get(x[v1]) : 0.0f;
     float sum_p;
-    const int entries = load_list<CAP, N>(a, row, l, sum_p);
+    const int entries = load_list<TYPE, CAP, N>(a, row, x, l, sum_p, [](uint32_t) { return true; });
     Run run = {-FLT_MAX, 0.0f, 0.0f};
     if (single) run_add<1, REST>(run, &y1, REST && on_list(l, a.slots, (uint32_t)v1) ? 1u : 0u, a.a2);
     if (REST) mark<CAP, N>(a, l, s_bits, s.head, (int64_t)held * PER);
@@ -502,7 +507,7 @@ __global__ __launch_bounds__(N, NV <= 4 ? 5 : 4) void distill_row_kernel(Distill
         }
     run_over<TYPE, REST, CAP, N>(run, a, l, s_bits, body, s.head, held, s.body);
     run = block_run<N>(run, a.a2, l.red);
-    const float listed = listed_sum<TYPE, CAP, N>(a, x, l, run.m, nullptr, [](uint32_t) { return true; });
+    const float listed = listed_sum<CAP, N>(a, l, run.m, nullptr, [](uint32_t) { return true; });
     const float4 st = finish_row<CAP, N>(a, row, l, entries, sum_p, run, listed, true);
     const bool counts = st.w != 0.0f;
     const float g = (a.grad_loss ? a.grad_loss[row] : 1.0f) * a.scale, q0 = 1.0f / st.y, f = q0 * st.z * g;
@@ -512,7 +517,7 @@ __global__ __launch_bounds__(N, NV <= 4 ? 5 : 4) void distill_row_kernel(Distill
     for (int u = 0; u < PLACES; ++u) {
         const int j = u * N + tid;
         here[u] = counts && j < a.topk ? l.id[j] : ICQ_PAD_ID;
-        if (here[u] != ICQ_PAD_ID) mine[u] = (ex2((E::get(x[here[u]]) - st.x) * a.a2) * q0 - l.p[j]) * g;
+        if (here[u] != ICQ_PAD_ID) mine[u] = (ex2((l.x[j] - st.x) * a.a2) * q0 - l.p[j]) * g;
     }
     __syncthreads();
     const uint4 zero = make_uint4(0, 0, 0, 0);
@@ -535,8 +540,9 @@ __global__ __launch_bounds__(N, NV <= 4 ? 5 : 4) void distill_row_kernel(Distill
         if (here[u] != ICQ_PAD_ID) out[here[u]] = E::put(mine[u]);
 }
 
-// Slices per row: enough blocks for the chip, none shorter than 8192 elements.
+// Slices per row: one where there is a row for every compute unit, else enough blocks for the chip, none shorter than 8192 elements.
 int splits_of(int64_t R, int64_t V, int num_cu) {
+    if (R >= num_cu) return 1;
     const int64_t want = (8ll * num_cu + R - 1) / (R > 0 ? R : 1), most = V / 8192;
     const int64_t n = want < most ? want : most;
     return (int)(n < 1 ? 1 : n > 1024 ? 1024 : n);
@@ -583,17 +589,18 @@ template <int TYPE, bool REST, int CAP>
 void launch_distill(const Distill &a, hipStream_t s) {
     constexpr int SIZE = sizeof(typename IcqElem<TYPE>::raw);
     if (a.grad && a.splits == 1 && same_phase(a, SIZE)) {
-        // threads and held groups by the row's length: 16 KB, 64 KB, 128 KB and the rest twice
+        // threads and held groups by the row's length: 16, 32, 64 KB, 128 KB and the rest twice
         auto go = [&](auto kernel, int n) { hipLaunchKernelGGL(kernel, dim3((uint32_t)a.R), dim3(n), 0, s, a); };
         const int64_t bytes = a.V * SIZE;
         if (bytes <= 256 * 4 * 16) go(distill_row_kernel<TYPE, REST, CAP, 256, 4>, 256);
+        else if (bytes <= 256 * 8 * 16) go(distill_row_kernel<TYPE, REST, CAP, 256, 8>, 256);
         else if (bytes <= 512 * 8 * 16) go(distill_row_kernel<TYPE, REST, CAP, 512, 8>, 512);
         else go(distill_row_kernel<TYPE, REST, CAP, 512, 16>, 512);
         return;
     }
     hipLaunchKernelGGL(HIP_KERNEL_NAME(distill_forward_kernel<TYPE, REST, CAP>), dim3((uint32_t)(a.R * a.splits)), dim3(T), 0, s, a);
     if (a.grad) launch_backward<TYPE, CAP>(a, a.splits > 1, s);
-    else if (a.splits > 1) hipLaunchKernelGGL(HIP_KERNEL_NAME(distill_join_kernel<CAP>), dim3((uint32_t)a.R), dim3(T), 0, s, a);
+    else if (a.splits > 1) hipLaunchKernelGGL(HIP_KERNEL_NAME(distill_join_kernel<TYPE, CAP>), dim3((uint32_t)a.R), dim3(T), 0, s, a);
 }
 
 bool grad_ok(const void *logits, int type, int64_t V, int64_t ld, const void *grad, int64_t ld_grad) {
