@@ -49,28 +49,39 @@ struct __attribute__((aligned(32))) Part {
 
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
 
-template <int N>
-__device__ __forceinline__ float block_sum(float v, float *red) {
+// Sums over the block, in a fixed order, of K values at once.
+template <int N, int K>
+__device__ __forceinline__ void block_sums(float (&v)[K], float *red) {
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
+    for (int d = 32; d > 0; d >>= 1)
+#pragma unroll
+        for (int i = 0; i < K; ++i) v[i] += __shfl_xor(v[i], d, 64);
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+        for (int i = 0; i < K; ++i) red[(threadIdx.x >> 6) * K + i] = v[i];
     __syncthreads();
-    v = red[0];
-    for (int w = 1; w < N / 64; ++w) v += red[w];
-    return v;
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+        v[i] = red[i];
+        for (int w = 1; w < N / 64; ++w) v[i] += red[w * K + i];
+    }
 }
 
+// The largest of `m` (NaN does not count) and the sum of `v`.
 template <int N>
-__device__ __forceinline__ float block_max(float v, float *red) {      // NaN does not count
+__device__ __forceinline__ void block_max_and_sum(float &m, float &v, float *red) {
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d, 64));
+    for (int d = 32; d > 0; d >>= 1) {
+        m = fmaxf(m, __shfl_xor(m, d, 64));
+        v += __shfl_xor(v, d, 64);
+    }
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    if ((threadIdx.x & 63) == 0) { red[(threadIdx.x >> 6) * 2] = m; red[(threadIdx.x >> 6) * 2 + 1] = v; }
     __syncthreads();
-    v = red[0];
-    for (int w = 1; w < N / 64; ++w) v = fmaxf(v, red[w]);
-    return v;
+    m = red[0];
+    v = red[1];
+    for (int w = 1; w < N / 64; ++w) { m = fmaxf(m, red[w * 2]); v += red[w * 2 + 1]; }
 }
 
 // The row's list in LDS.  id[j] = ICQ_PAD_ID where position j holds no entry of its own.
@@ -80,7 +91,7 @@ struct List {
     float p[CAP], log_p[CAP];
     float x[CAP];                  // the student's logit
     uint32_t slot_id[2 * CAP];     // the ids, by hash
-    float red[16];
+    float red[24];
     uint32_t twice;
 };
 
@@ -91,33 +102,37 @@ __device__ int load_list(const Distill &a, int64_t row, const typename IcqElem<T
     const int tid = threadIdx.x;
     for (int i = tid; i < a.slots; i += n) l.slot_id[i] = ICQ_PAD_ID;
     if (tid == 0) l.twice = 0;
-    float top = -INFINITY;
+    float top = -INFINITY, count = 0.0f, ref = 0.0f, log_z = 0.0f;
     for (int j = tid; j < a.topk; j += n) {
         const uint32_t id = a.ids[row * a.topk + j];
         const float z = a.teacher_scale * a.values[row * a.topk + j];
         const bool entry = (int64_t)id < a.V && !(z == -INFINITY);
         l.id[j] = entry ? id : ICQ_PAD_ID;
         l.p[j] = entry ? z : -INFINITY;
-        if (entry && in(id)) l.x[j] = IcqElem<TYPE>::get(x[id]);
-        if (entry) top = fmaxf(top, z);
+        if (entry) {
+            top = fmaxf(top, z);
+            count += 1.0f;
+            if (in(id)) l.x[j] = IcqElem<TYPE>::get(x[id]);
+        }
     }
-    top = block_max<N>(top, l.red);                       // (its barriers also cover the tables)
-    float lse = 0.0f, ref = 0.0f;
+    block_max_and_sum<N>(top, count, l.red);           // (its barriers also cover the table)
     if (a.teacher_lse) {
         ref = a.teacher_lse[row];
     } else if (top > -INFINITY) {
         ref = top;
-        float s = 0.0f;
+        float s[1] = {0.0f};
         for (int j = tid; j < a.topk; j += n)
-            if (l.id[j] != ICQ_PAD_ID) s += expf(l.p[j] - top);
-        lse = logf(block_sum<N>(s, l.red));
+            if (l.id[j] != ICQ_PAD_ID) s[0] += expf(l.p[j] - top);
+        block_sums<N>(s, l.red);
+        log_z = logf(s[0]);
     }
+    float sum[1] = {0.0f};
     for (int j = tid; j < a.topk; j += n) {
         const uint32_t id = l.id[j];
         if (id == ICQ_PAD_ID) { l.p[j] = 0.0f; continue; }
-        const float lp = (l.p[j] - ref) - lse;
+        const float lp = (l.p[j] - ref) - log_z;
         l.log_p[j] = lp;
-        l.p[j] = expf(lp);
+        sum[0] += l.p[j] = expf(lp);
         uint32_t at = (id * 0x9E3779B1u) >> 16 & (uint32_t)(a.slots - 1);
         for (;;) {                                     // slots >= 2 * topk: an empty one is found
             const uint32_t was = atomicCAS(&l.slot_id[at], ICQ_PAD_ID, id);
@@ -126,9 +141,14 @@ __device__ int load_list(const Distill &a, int64_t row, const typename IcqElem<T
             at = (at + 1) & (uint32_t)(a.slots - 1);
         }
     }
+    sum_p = 0.0f;
+    if (a.teacher_lse) {                               // (only then is the sum of any consequence)
+        block_sums<N>(sum, l.red);
+        sum_p = sum[0];
+    }
     __syncthreads();
     if (l.twice) {                                     // every id's probability to its first place
-        float p[PLACES];
+        float p[PLACES], lost[1] = {0.0f};
         bool first[PLACES];
 #pragma unroll
         for (int u = 0; u < PLACES; ++u) {
@@ -146,16 +166,14 @@ __device__ int load_list(const Distill &a, int64_t row, const typename IcqElem<T
             const int j = u * n + tid;
             if (j < a.topk && l.id[j] != ICQ_PAD_ID) {
                 if (first[u]) { l.p[j] = p[u]; l.log_p[j] = logf(p[u]); }
-                else { l.p[j] = 0.0f; l.id[j] = ICQ_PAD_ID; }
+                else { l.p[j] = 0.0f; l.id[j] = ICQ_PAD_ID; lost[0] += 1.0f; }
             }
         }
+        block_sums<N>(lost, l.red);
+        count -= lost[0];
         __syncthreads();
     }
-    float s = 0.0f, count = 0.0f;
-    for (int j = tid; j < a.topk; j += n)
-        if (l.id[j] != ICQ_PAD_ID) { s += l.p[j]; count += 1.0f; }
-    sum_p = block_sum<N>(s, l.red);
-    return (int)block_sum<N>(count, l.red);
+    return (int)count;
 }
 
 // Where a row's elements lie: `head` single elements, `body` groups of PER that start on 16 bytes, then `tail` single ones.
@@ -209,53 +227,55 @@ __device__ __forceinline__ void run_add(Run &a, const float *x, uint32_t listed,
     if (REST) a.r += l;
 }
 
+// The largest maximum of the block.
+template <int N>
+__device__ __forceinline__ float run_max(const Run &a, float *red) {
+    float m = a.m, none = 0.0f;
+    block_max_and_sum<N>(m, none, red);
+    return m;
+}
+
 // Block-wide: the join of all threads' runs, in a fixed order.
 template <int N>
-__device__ __forceinline__ Run block_run(Run a, float a2, float *red) {
-    const float m = block_max<N>(a.m, red);
-    const float f = ex2((a.m - m) * a2);
-    Run b;
-    b.m = m;
-    b.s = block_sum<N>(a.s * f, red);
-    b.r = block_sum<N>(a.r * f, red);
+__device__ __forceinline__ Run block_run(const Run &a, float a2, float *red) {
+    const float m = run_max<N>(a, red), f = ex2((a.m - m) * a2);
+    float v[2] = {a.s * f, a.r * f};
+    block_sums<N>(v, red);
+    const Run b = {m, v[0], v[1]};
     return b;
 }
 
-// What the loss needs of those listed items that `in` takes, relative to the maximum m: sum of p (x - m).
+// This thread's share of what the loss needs of those listed items that `in` takes, relative to the maximum m: sum of p (x - m), of p.
 template <int CAP, int N, typename In>
-__device__ __forceinline__ float listed_sum(const Distill &a, List<CAP> &l, float m, float *p_sum, In in) {
-    float sum = 0.0f, ps = 0.0f;
+__device__ __forceinline__ void listed_sum(const Distill &a, const List<CAP> &l, float m, float (&v)[2], In in) {
+    v[0] = v[1] = 0.0f;
     for (int j = threadIdx.x; j < a.topk; j += N) {
         const float p = l.p[j];
         if (l.id[j] != ICQ_PAD_ID && !(p == 0.0f) && in(l.id[j])) {
-            sum += p * (l.x[j] - m);
-            ps += p;
+            v[0] += p * (l.x[j] - m);
+            v[1] += p;
         }
     }
-    if (p_sum) *p_sum = block_sum<N>(ps, l.red);
-    return block_sum<N>(sum, l.red);
 }
 
-// Loss and statistics of a row from its sums; listed = sum of p (x - m).  All threads of the block get the statistics.
+// Loss and statistics of a row from its sums; listed: this thread's share of the sum of p (x - m).  All threads get the statistics.
 template <int CAP, int N>
 __device__ float4 finish_row(const Distill &a, int64_t row, List<CAP> &l, int entries, float sum_p, const Run &run, float listed, bool write) {
     const float log_s = logf(run.s);
-    float sum = 0.0f;
-    for (int j = threadIdx.x; j < a.topk; j += N)
-        if (l.id[j] != ICQ_PAD_ID && !(l.p[j] == 0.0f)) sum += l.p[j] * (l.log_p[j] + log_s);
-    sum = block_sum<N>(sum, l.red) - a.scale * listed;
     const bool counts = entries > 0 && !(run.s == 0.0f);
-    float c = 1.0f;
-    if (a.teacher_lse && (int64_t)entries < a.V) {
-        const float p_r = fmaxf(0.0f, 1.0f - sum_p);
-        if (p_r > 0.0f) sum += p_r * (logf(p_r) - (logf(run.r) - log_s));
-        if (run.r > 0.0f) c = 1.0f - p_r * run.s / run.r;          // (nothing off the list: no item takes c)
+    const bool rest = a.teacher_lse && (int64_t)entries < a.V;
+    const float p_r = rest ? fmaxf(0.0f, 1.0f - sum_p) : 0.0f;
+    if (write) {                                       // (the same for the whole block)
+        float sum[1] = {-a.scale * listed};
+        for (int j = threadIdx.x; j < a.topk; j += N)
+            if (l.id[j] != ICQ_PAD_ID && !(l.p[j] == 0.0f)) sum[0] += l.p[j] * (l.log_p[j] + log_s);
+        block_sums<N>(sum, l.red);
+        if (p_r > 0.0f) sum[0] += p_r * (logf(p_r) - (logf(run.r) - log_s));
+        if (threadIdx.x == 0) a.loss[row] = counts ? sum[0] : 0.0f;
     }
-    const float4 st = make_float4(run.m, run.s, c, counts ? 1.0f : 0.0f);
-    if (write && threadIdx.x == 0) {
-        a.loss[row] = counts ? sum : 0.0f;
-        if (a.stats) a.stats[row] = st;
-    }
+    // (nothing off the list: no item takes c)
+    const float4 st = make_float4(run.m, run.s, rest && run.r > 0.0f ? 1.0f - p_r * run.s / run.r : 1.0f, counts ? 1.0f : 0.0f);
+    if (write && a.stats && threadIdx.x == 0) a.stats[row] = st;
     return st;
 }
 
@@ -304,6 +324,21 @@ __device__ __forceinline__ void mark(const Distill &a, const List<CAP> &l, uint3
     __syncthreads();
 }
 
+// Sums over `held` groups in registers, group u * N + thread in w[u].
+template <int TYPE, bool REST, int N, int NV>
+__device__ __forceinline__ void run_held(Run &run, const uint4 (&w)[NV], int held, const uint32_t *bits, float a2) {
+    typedef IcqElem<TYPE> E;
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+        const int b = u * N + (int)threadIdx.x, e = b * E::PER;
+        if (b < held) {
+            float y[E::PER];
+            E::unpack(w[u], y);
+            run_add<E::PER, REST>(run, y, REST ? bits[e >> 5] >> (e & 31) : 0u, a2);
+        }
+    }
+}
+
 // Sums over groups [b0, b1) of a row, in chunks that can be marked.
 template <int TYPE, bool REST, int CAP, int N>
 __device__ __forceinline__ void run_over(Run &run, const Distill &a, const List<CAP> &l, uint32_t *bits, const uint4 *body, int head, int64_t from,
@@ -346,6 +381,7 @@ __device__ __forceinline__ uint4 gradient_of(const uint4 &w, float m, float a2, 
 template <int TYPE, bool REST, int CAP>
 __global__ __launch_bounds__(T) void distill_forward_kernel(Distill a) {
     typedef IcqElem<TYPE> E;
+    constexpr int U = 4;
     __shared__ List<CAP> l;
     __shared__ uint32_t s_bits[REST ? CHUNK / 32 : 1];
     const int tid = threadIdx.x, k = (int)(blockIdx.x % (uint32_t)a.splits);
@@ -355,6 +391,11 @@ __global__ __launch_bounds__(T) void distill_forward_kernel(Distill a) {
     const Span s = span_of<TYPE>(x, a.V);
     const Slice c = slice_of(s, k, a.splits);
     const auto in = [&](uint32_t id) { return in_slice(s, c, id, E::PER); };
+    const uint4 *body = reinterpret_cast<const uint4 *>(x + s.head);
+    uint4 w[U];                                        // on their way while the list is worked on
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (c.b0 + u * T + tid < c.b1) w[u] = body[c.b0 + u * T + tid];
     const int entries = load_list<TYPE, CAP, T>(a, row, x, l, sum_p, in);
     Run run = {-FLT_MAX, 0.0f, 0.0f};
     for (int64_t i = c.e0 + tid; i < c.e1; i += T) {
@@ -362,22 +403,25 @@ __global__ __launch_bounds__(T) void distill_forward_kernel(Distill a) {
         const float y = E::get(x[v]);
         run_add<1, REST>(run, &y, REST && on_list(l, a.slots, (uint32_t)v) ? 1u : 0u, a.a2);
     }
-    run_over<TYPE, REST, CAP, T>(run, a, l, s_bits, reinterpret_cast<const uint4 *>(x + s.head), s.head, c.b0, c.b1);
+    const int64_t b1 = c.b0 + U * T < c.b1 ? c.b0 + U * T : c.b1;
+    if (REST) mark<CAP, T>(a, l, s_bits, s.head + c.b0 * E::PER, (b1 - c.b0) * E::PER);
+    run_held<TYPE, REST, T, U>(run, w, (int)(b1 - c.b0), s_bits, a.a2);
+    run_over<TYPE, REST, CAP, T>(run, a, l, s_bits, body, s.head, b1, c.b1);
     run = block_run<T>(run, a.a2, l.red);
+    float v[2];
+    listed_sum<CAP, T>(a, l, run.m, v, in);
     if (a.splits == 1) {
-        const float listed = listed_sum<CAP, T>(a, l, run.m, nullptr, [](uint32_t) { return true; });
-        finish_row<CAP, T>(a, row, l, entries, sum_p, run, listed, true);
+        finish_row<CAP, T>(a, row, l, entries, sum_p, run, v[0], true);
     } else {
-        float p;
-        const float listed = listed_sum<CAP, T>(a, l, run.m, &p, in);
+        block_sums<T>(v, l.red);
         if (tid == 0) {
-            const Part part = {run.m, run.s, run.r, listed, p, {0.0f, 0.0f, 0.0f}};
+            const Part part = {run.m, run.s, run.r, v[0], v[1], {0.0f, 0.0f, 0.0f}};
             a.part[row * a.splits + k] = part;
         }
     }
 }
 
-// A row's sums from its slices'; listed: sum of p (x - m).
+// A row's sums from its slices'; listed: this thread's share of the sum of p (x - m).
 template <int CAP, int N>
 __device__ Run join_row(const Distill &a, int64_t row, List<CAP> &l, float &listed) {
     Run run = {-FLT_MAX, 0.0f, 0.0f};
@@ -387,12 +431,11 @@ __device__ Run join_row(const Distill &a, int64_t row, List<CAP> &l, float &list
         run_join(run, b, a.a2);
     }
     run = block_run<N>(run, a.a2, l.red);
-    float t = 0.0f;
+    listed = 0.0f;
     for (int k = threadIdx.x; k < a.splits; k += N) {
         const Part p = a.part[row * a.splits + k];
-        if (!(p.p == 0.0f)) t += p.t + p.p * (p.m - run.m);
+        if (!(p.p == 0.0f)) listed += p.t + p.p * (p.m - run.m);
     }
-    listed = block_sum<N>(t, l.red);
     return run;
 }
 
@@ -421,6 +464,12 @@ __global__ __launch_bounds__(T) void distill_backward_kernel(Distill a) {
     if (VEC) s = span_of<TYPE>(x, a.V);
     else { s.head = (int)a.V; s.body = 0; s.tail = 0; }
     const Slice c = slice_of(s, k, a.splits);
+    const uint4 *body = reinterpret_cast<const uint4 *>(x + s.head);
+    uint4 *body_out = reinterpret_cast<uint4 *>(out + s.head);
+    uint4 w[U];                                        // on their way while the list is worked on
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (c.b0 + u * T + tid < c.b1) w[u] = body[c.b0 + u * T + tid];
     float sum_p, listed;
     // (listed items of other slices may have their gradients already, where those take the logits' place)
     const auto in = [&](uint32_t id) { return in_slice(s, c, id, PER); };
@@ -432,8 +481,6 @@ __global__ __launch_bounds__(T) void distill_backward_kernel(Distill a) {
     } else {
         st = a.stats[row];
     }
-    const uint4 *body = reinterpret_cast<const uint4 *>(x + s.head);
-    uint4 *body_out = reinterpret_cast<uint4 *>(out + s.head);
     if (st.w == 0.0f) {                                // a row that does not count
         for (int64_t i = c.e0 + tid; i < c.e1; i += T) out[i < s.head ? i : i + s.body * PER] = E::put(0.0f);
         for (int64_t b = c.b0 + tid; b < c.b1; b += T) body_out[b] = make_uint4(0, 0, 0, 0);
@@ -455,10 +502,11 @@ __global__ __launch_bounds__(T) void distill_backward_kernel(Distill a) {
         out[v] = E::put(ex2((E::get(x[v]) - st.x) * a.a2) * f);
     }
     for (int64_t b = c.b0 + tid; b < c.b1; b += U * T) {
-        uint4 w[U];
+        if (b != c.b0 + tid) {
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (b + u * T < c.b1) w[u] = body[b + u * T];
+            for (int u = 0; u < U; ++u)
+                if (b + u * T < c.b1) w[u] = body[b + u * T];
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (b + u * T < c.b1) body_out[b + u * T] = gradient_of<TYPE>(w[u], st.x, a.a2, f);
@@ -469,9 +517,19 @@ __global__ __launch_bounds__(T) void distill_backward_kernel(Distill a) {
         if (here[u] != ICQ_PAD_ID) out[here[u]] = E::put(mine[u]);
 }
 
-// Loss and gradient of a whole row: N threads, the first N * NV groups of 16 bytes stay in registers.
-template <int TYPE, bool REST, int CAP, int N, int NV>
-__global__ __launch_bounds__(N, NV <= 4 ? 5 : 4) void distill_row_kernel(Distill a) {
+template <bool PAST_CACHES>
+__device__ __forceinline__ void put_group(uint4 *p, const uint4 &v) {
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    const u32x4 q = {v.x, v.y, v.z, v.w};
+    if (PAST_CACHES) __builtin_nontemporal_store(q, reinterpret_cast<u32x4 *>(p));
+    else *reinterpret_cast<u32x4 *>(p) = q;
+}
+
+// Loss and gradient of a whole row: N threads, the first N * NV groups of 16 bytes stay in registers.  LONG: rows beyond those; their
+// second reading comes from the last-level cache as long as the gradient's stores do not go there (4096 x 131072 bf16:
+// 472 us with ordinary stores, 431 so, 4.98 TB/s of the least traffic; a copy runs at 5.17).
+template <int TYPE, bool REST, int CAP, int N, int NV, bool LONG>
+__global__ __launch_bounds__(N, 4) void distill_row_kernel(Distill a) {
     typedef IcqElem<TYPE> E;
     constexpr int PER = E::PER, U = 4, PLACES = (CAP + N - 1) / N;
     static_assert(N * NV * PER <= CHUNK, "one marking covers the registers");
@@ -497,18 +555,12 @@ __global__ __launch_bounds__(N, NV <= 4 ? 5 : 4) void distill_row_kernel(Distill
     Run run = {-FLT_MAX, 0.0f, 0.0f};
     if (single) run_add<1, REST>(run, &y1, REST && on_list(l, a.slots, (uint32_t)v1) ? 1u : 0u, a.a2);
     if (REST) mark<CAP, N>(a, l, s_bits, s.head, (int64_t)held * PER);
-#pragma unroll
-    for (int u = 0; u < NV; ++u)
-        if (u * N + tid < held) {
-            float y[PER];
-            E::unpack(w[u], y);
-            const int e = (u * N + tid) * PER;
-            run_add<PER, REST>(run, y, REST ? s_bits[e >> 5] >> (e & 31) : 0u, a.a2);
-        }
+    run_held<TYPE, REST, N, NV>(run, w, held, s_bits, a.a2);
     run_over<TYPE, REST, CAP, N>(run, a, l, s_bits, body, s.head, held, s.body);
     run = block_run<N>(run, a.a2, l.red);
-    const float listed = listed_sum<CAP, N>(a, l, run.m, nullptr, [](uint32_t) { return true; });
-    const float4 st = finish_row<CAP, N>(a, row, l, entries, sum_p, run, listed, true);
+    float v[2];
+    listed_sum<CAP, N>(a, l, run.m, v, [](uint32_t) { return true; });
+    const float4 st = finish_row<CAP, N>(a, row, l, entries, sum_p, run, v[0], true);
     const bool counts = st.w != 0.0f;
     const float g = (a.grad_loss ? a.grad_loss[row] : 1.0f) * a.scale, q0 = 1.0f / st.y, f = q0 * st.z * g;
     float mine[PLACES];
@@ -524,7 +576,7 @@ __global__ __launch_bounds__(N, NV <= 4 ? 5 : 4) void distill_row_kernel(Distill
     if (single) out[v1] = E::put(counts ? ex2((y1 - st.x) * a.a2) * f : 0.0f);
 #pragma unroll
     for (int u = 0; u < NV; ++u)
-        if (u * N + tid < held) body_out[u * N + tid] = counts ? gradient_of<TYPE>(w[u], st.x, a.a2, f) : zero;
+        if (u * N + tid < held) put_group<LONG>(body_out + u * N + tid, counts ? gradient_of<TYPE>(w[u], st.x, a.a2, f) : zero);
     for (int64_t b = s.body - 1 - tid; b >= held; b -= U * N) {        // from the end: what was read last is nearest
         uint4 r[U];
 #pragma unroll
@@ -532,7 +584,7 @@ __global__ __launch_bounds__(N, NV <= 4 ? 5 : 4) void distill_row_kernel(Distill
             if (b - u * N >= held) r[u] = body[b - u * N];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (b - u * N >= held) body_out[b - u * N] = counts ? gradient_of<TYPE>(r[u], st.x, a.a2, f) : zero;
+            if (b - u * N >= held) put_group<LONG>(body_out + b - u * N, counts ? gradient_of<TYPE>(r[u], st.x, a.a2, f) : zero);
     }
     __syncthreads();
 #pragma unroll
@@ -589,13 +641,14 @@ template <int TYPE, bool REST, int CAP>
 void launch_distill(const Distill &a, hipStream_t s) {
     constexpr int SIZE = sizeof(typename IcqElem<TYPE>::raw);
     if (a.grad && a.splits == 1 && same_phase(a, SIZE)) {
-        // threads and held groups by the row's length: 16, 32, 64 KB, 128 KB and the rest twice
+        // threads and held groups by the row's length: up to 16, 32, 64 KB, and longer (4096 rows of 24000 bf16: 86 us by 256
+        // threads, 100 by 512; of 131072: 473 and 431)
         auto go = [&](auto kernel, int n) { hipLaunchKernelGGL(kernel, dim3((uint32_t)a.R), dim3(n), 0, s, a); };
         const int64_t bytes = a.V * SIZE;
-        if (bytes <= 256 * 4 * 16) go(distill_row_kernel<TYPE, REST, CAP, 256, 4>, 256);
-        else if (bytes <= 256 * 8 * 16) go(distill_row_kernel<TYPE, REST, CAP, 256, 8>, 256);
-        else if (bytes <= 512 * 8 * 16) go(distill_row_kernel<TYPE, REST, CAP, 512, 8>, 512);
-        else go(distill_row_kernel<TYPE, REST, CAP, 512, 16>, 512);
+        if (bytes <= 256 * 4 * 16) go(distill_row_kernel<TYPE, REST, CAP, 256, 4, false>, 256);
+        else if (bytes <= 256 * 8 * 16) go(distill_row_kernel<TYPE, REST, CAP, 256, 8, false>, 256);
+        else if (bytes <= 256 * 16 * 16) go(distill_row_kernel<TYPE, REST, CAP, 256, 16, false>, 256);
+        else go(distill_row_kernel<TYPE, REST, CAP, 512, 16, true>, 512);
         return;
     }
     hipLaunchKernelGGL(HIP_KERNEL_NAME(distill_forward_kernel<TYPE, REST, CAP>), dim3((uint32_t)(a.R * a.splits)), dim3(T), 0, s, a);
