@@ -12,7 +12,7 @@ struct Product {
     int64_t ldo;
     float *part;               // [splits][M][N] partial sums where splits > 1
     int splits, per;           // blocks along K per split
-    int vec;                   // four consecutive results can be stored at once
+    int vec;                   // rows of the result start on 16 bytes
 };
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));

@@ -112,7 +112,7 @@ ICQ_EXPORT int icq_block_matmul(const uint8_t *a, int a_format, int64_t lda, con
     p.splits = plan.splits;
     p.per = (p.kb + p.splits - 1) / p.splits;
     p.part = static_cast<float *>(workspace);
-    p.vec = (uintptr_t)out % (4 * size) == 0 && ldo % 4 == 0;
+    p.vec = (uintptr_t)out % 16 == 0 && ldo * size % 16 == 0;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const dim3 by_four((uint32_t)((N + 1023) / 1024), (uint32_t)(M < 32768 ? M : 32768), (uint32_t)((M + 32767) / 32768));
     if (K == 0) {

@@ -15,7 +15,7 @@ struct Shape {
     static constexpr int NI = NI_, NJ = NJ_, WM = WM_, WN = WN_, THREADS = 64 * WM * WN, T = 32 * NI * WM;
     static constexpr int STAGE = 2 * T * 128;                                 // bytes of a stage
     static constexpr int LDS_BYTES = 2 * STAGE + 3 * 8 * T * 4;
-    static_assert(32 * NJ * WN == T && THREADS == 2 * T && NJ == 2, "square tiles, two threads a row; a stage's four parts over two columns twice");
+    static_assert(32 * NJ * WN == T && THREADS == 2 * T && NJ == 2 && 2 * STAGE / (WM * WN) >= 32 * 68 * 4, "square tiles, two threads a row; a stage's four parts over two columns twice");
 };
 typedef Shape<4, 2, 2, 4> Wide;
 typedef Shape<2, 2, 2, 2> Small;
@@ -57,6 +57,42 @@ __device__ __forceinline__ i32x4 bytes_from(const uint8_t *p) {
 // else here uses it.)
 __device__ __forceinline__ void load_to_lds(const i32x4 &base, uint32_t off, int by, uint32_t to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(off), "s"(base), "s"(by) : "memory");
+}
+
+// 32 rows and 64 columns of the result from a wavefront's accumulators, whole rows at a time: in the accumulators a lane has four
+// neighbours of one row and the lanes 32 rows, whose stores would be 16 bytes here and there.  vec: rows start on 16 bytes.
+template <int TYPE>
+__device__ __forceinline__ void store_rows(uint8_t *turn, const f32x16 (&acc)[2], void *out, int64_t ldo, bool vec, int64_t M, int64_t N, int64_t m0, int64_t n0,
+                                           int lane) {
+    typedef IcqElem<TYPE> E;
+    typedef typename E::raw raw;
+    constexpr int PER = E::PER, STRIDE = 64 + PER;                            // (16 bytes more than a row: other banks)
+    const int at = lane & 31, half = lane >> 5;
+    raw *mine = reinterpret_cast<raw *>(turn);
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            raw *to = mine + at * STRIDE + j * 32 + 8 * g + 4 * half;
+            const float v[4] = {acc[j][4 * g], acc[j][4 * g + 1], acc[j][4 * g + 2], acc[j][4 * g + 3]};
+            if constexpr (TYPE == ICQ_F32) *reinterpret_cast<uint4 *>(to) = E::pack(v);
+            else *reinterpret_cast<uint2 *>(to) = make_uint2(E::pack2(v[0], v[1]), E::pack2(v[2], v[3]));
+        }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    raw *to = static_cast<raw *>(out);
+    if (vec && n0 + 64 <= N) {
+        constexpr int LANES = 64 / PER, ROWS_AT_ONCE = 64 / LANES;
+        const int c = lane % LANES * PER;
+#pragma unroll
+        for (int r = lane / LANES; r < 32; r += ROWS_AT_ONCE)
+            if (m0 + r < M) *reinterpret_cast<uint4 *>(to + (m0 + r) * ldo + n0 + c) = *reinterpret_cast<const uint4 *>(mine + r * STRIDE + c);
+    } else if (n0 + lane < N) {
+#pragma unroll 8
+        for (int r = 0; r < 32; ++r)
+            if (m0 + r < M) to[(m0 + r) * ldo + n0 + lane] = mine[r * STRIDE + lane];
+    }
 }
 
 template <typename S, int FA, int FB, bool ROWS, int MODE>
@@ -250,26 +286,15 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product p, int t
             __builtin_amdgcn_sched_barrier(0);
         }
     }
+    __syncthreads();                                                          // (a wavefront's part of the stages takes its results)
+    uint8_t *turn = smem + wave * (2 * S::STAGE / WAVES);
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-        const int64_t m = m0 + wm + i * 32 + at;
-        if (m >= p.M) continue;
-#pragma unroll
-        for (int j = 0; j < NJ; ++j)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int64_t n = n0 + wn + j * 32 + 8 * g + 4 * half;
-                const icq_f32x4 v = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-                if (p.splits > 1) {
-                    store_part(p, blockIdx.y, m, n, v);
-                } else if (MODE == EXACT) {
-                    store4<ICQ_F32>(p, m, n, v);
-                } else if (out_type == ICQ_BF16) {
-                    store4<ICQ_BF16>(p, m, n, v);
-                } else {
-                    store4<ICQ_F16>(p, m, n, v);
-                }
-            }
+        const int64_t m = m0 + wm + i * 32, n = n0 + wn;
+        if (p.splits > 1) store_rows<ICQ_F32>(turn, acc[i], p.part + (int64_t)blockIdx.y * p.M * p.N, p.N, p.N % 4 == 0, p.M, p.N, m, n, lane);
+        else if (MODE == EXACT) store_rows<ICQ_F32>(turn, acc[i], p.out, p.ldo, p.vec, p.M, p.N, m, n, lane);
+        else if (out_type == ICQ_BF16) store_rows<ICQ_BF16>(turn, acc[i], p.out, p.ldo, p.vec, p.M, p.N, m, n, lane);
+        else store_rows<ICQ_F16>(turn, acc[i], p.out, p.ldo, p.vec, p.M, p.N, m, n, lane);
     }
 }
 
