@@ -22,7 +22,6 @@ struct Quantize {
     float *scales, *scales_t;
     int across, down;          // blocks of 128 along a row, along a column
     int pow2;
-    int vec;                   // rows of x start on 16 bytes
 };
 
 // Magnitude's bits for the largest-value search: 0 for infinities and NaN.
@@ -51,9 +50,11 @@ template <int TYPE>
 __device__ __forceinline__ void load8(const Quantize &a, int64_t r, int64_t c, float *x) {
     typedef IcqElem<TYPE> E;
     const typename E::raw *p = static_cast<const typename E::raw *>(a.x) + r * a.ldx + c;
-    if (a.vec && c + 8 <= a.cols) {
+    if (c + 8 <= a.cols) {
+        uint4 v[8 / E::PER];
+        __builtin_memcpy(v, p, sizeof v);              // (wherever the row starts: the memory pipe takes 16 bytes from any address)
 #pragma unroll
-        for (int h = 0; h < 8 / E::PER; ++h) E::unpack(reinterpret_cast<const uint4 *>(p)[h], x + h * E::PER);
+        for (int h = 0; h < 8 / E::PER; ++h) E::unpack(v[h], x + h * E::PER);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = c + i < a.cols ? E::get(p[i]) : 0.0f;
@@ -95,7 +96,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(Quantize a, int64_t 
 template <int TYPE, int FORMAT, bool TILE>
 __global__ __launch_bounds__(256) void quantize_tile_kernel(Quantize a) {
     __shared__ uint32_t s_max[4][128];
-    __shared__ __attribute__((aligned(16))) uint8_t s_turn[128][144];
+    __shared__ __attribute__((aligned(16))) uint8_t s_turn[128][128];         // column c's 8-byte piece h at place h ^ (c / 8)
     const int g = threadIdx.x & 15, h = threadIdx.x >> 4, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int bc = blockIdx.x % a.across, br = blockIdx.x / a.across;
     const int64_t r0 = (int64_t)br * 128 + 8 * h, c0 = (int64_t)bc * 128 + 8 * g;
@@ -175,15 +176,17 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(Quantize a) {
         float y[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] = x[i][j];
-        *reinterpret_cast<uint2 *>(&s_turn[8 * g + j][8 * h]) = codes8<FORMAT>(y, inv_t[j]);
+        *reinterpret_cast<uint2 *>(&s_turn[8 * g + j][8 * (h ^ g)]) = codes8<FORMAT>(y, inv_t[j]);
     }
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
         const int at = u * 256 + threadIdx.x, c = at >> 3, piece = (at & 7) * 16;
         const int64_t col = (int64_t)bc * 128 + c, row = (int64_t)br * 128 + piece;
-        if (col < a.cols && row < tall)
-            *reinterpret_cast<uint4 *>(a.codes_t + col * a.ld_t + row) = *reinterpret_cast<const uint4 *>(&s_turn[c][piece]);
+        if (col < a.cols && row < tall) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(&s_turn[c][piece ^ ((c >> 4) << 4)]);
+            *reinterpret_cast<uint4 *>(a.codes_t + col * a.ld_t + row) = (c & 8) ? make_uint4(v.z, v.w, v.x, v.y) : v;
+        }
     }
 }
 
@@ -224,7 +227,6 @@ ICQ_EXPORT int icq_block_quantize(const void *x, int x_type, int64_t rows, int64
     a.across = (int)((cols + 127) / 128);
     a.down = (int)((rows + 127) / 128);
     a.pow2 = scaling == ICQ_SCALES_POW2;
-    a.vec = (uintptr_t)x % 16 == 0 && ldx * size % 16 == 0;
     if ((block_rows != 1 || codes_t) && (int64_t)a.across * a.down > 0x7fffffff) return ICQ_ERR_ARG;
     hipStream_t s = static_cast<hipStream_t>(stream);
     int rc = ICQ_OK;
