@@ -91,101 +91,192 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(Quantize a, int64_t 
     if ((threadIdx.x & 15u) == 0) a.scales[r * a.across + block] = s;
 }
 
+// Eight values of one row as they were loaded, and the bits of their magnitudes: pairs of halves, or words.
+template <int TYPE>
+struct Eight {
+    static constexpr int WORDS = TYPE == ICQ_F32 ? 8 : 4;
+    uint32_t w[WORDS];
+};
+
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+
+// The larger magnitudes, pair by pair or word by word.
+template <int TYPE>
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+    if constexpr (TYPE == ICQ_F32) return max(a, b);
+    else return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+
+template <int TYPE>
+__device__ __forceinline__ uint32_t magnitude(uint32_t w) { return w & (TYPE == ICQ_F32 ? 0x7fffffffu : 0x7fff7fffu); }
+
+// Magnitudes' bits of infinities and NaN replaced by zero.
+template <int TYPE>
+__device__ __forceinline__ uint32_t finite_only(uint32_t m) {
+    if constexpr (TYPE == ICQ_F32) return m < 0x7f800000u ? m : 0u;
+    else {
+        constexpr uint32_t inf = TYPE == ICQ_F16 ? 0x7c00u : 0x7f80u;
+        return ((m & 0xffffu) < inf ? m & 0xffffu : 0u) | ((m >> 16) < inf ? m & 0xffff0000u : 0u);
+    }
+}
+
+// A magnitude's bits as those of a float.
+template <int TYPE>
+__device__ __forceinline__ uint32_t float_bits(uint32_t half) {
+    if constexpr (TYPE == ICQ_F32) return half;
+    else if constexpr (TYPE == ICQ_F16) return __float_as_uint((float)__builtin_bit_cast(_Float16, (uint16_t)half));
+    else return half << 16;
+}
+
+// The largest of 16 neighbouring lanes, in all of them.
+template <int TYPE>
+__device__ __forceinline__ uint32_t largest_of_16(uint32_t m) {
+    m = larger<TYPE>(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x128, 0xf, 0xf, true));      // rotations by 8, 4, 2, 1 lanes
+    m = larger<TYPE>(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x124, 0xf, 0xf, true));
+    m = larger<TYPE>(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x122, 0xf, 0xf, true));
+    return larger<TYPE>(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x121, 0xf, 0xf, true));
+}
+
+template <int TYPE>
+__device__ __forceinline__ Eight<TYPE> read8(const Quantize &a, int64_t r, int64_t c) {
+    typedef typename IcqElem<TYPE>::raw raw;
+    Eight<TYPE> v;
+#pragma unroll
+    for (int i = 0; i < Eight<TYPE>::WORDS; ++i) v.w[i] = 0;
+    if (r >= a.rows) return v;
+    const raw *p = static_cast<const raw *>(a.x) + r * a.ldx + c;
+    if (c + 8 <= a.cols) __builtin_memcpy(v.w, p, sizeof v.w);
+    else
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (c + i < a.cols) {
+                if constexpr (TYPE == ICQ_F32) v.w[i] = __float_as_uint(p[i]);
+                else v.w[i >> 1] |= (uint32_t)__builtin_bit_cast(uint16_t, p[i]) << (16 * (i & 1));
+            }
+    return v;
+}
+
+template <int TYPE>
+__device__ __forceinline__ void values8(const Eight<TYPE> &v, float *x) {
+#pragma unroll
+    for (int h = 0; h < Eight<TYPE>::WORDS / 4; ++h) IcqElem<TYPE>::unpack(make_uint4(v.w[4 * h], v.w[4 * h + 1], v.w[4 * h + 2], v.w[4 * h + 3]), x + 4 * h);
+}
+
 // A 128 x 128 tile per block; thread (g, h) holds rows 8 h .. 8 h + 7 of columns 8 g .. 8 g + 7.
-// TILE: one scale for the whole tile, else one per row and column of it.
+// TILE: one scale for the whole tile, else one per row and column of it, each worked out by one thread.
 template <int TYPE, int FORMAT, bool TILE>
 __global__ __launch_bounds__(256) void quantize_tile_kernel(Quantize a) {
-    __shared__ uint32_t s_max[4][128];
+    constexpr int WORDS = Eight<TYPE>::WORDS;
+    __shared__ __attribute__((aligned(16))) uint32_t s_cols[4][128];          // largest magnitudes: of a wavefront's rows in each column,
+    __shared__ __attribute__((aligned(16))) uint32_t s_rows[128];             // of each row
+    __shared__ __attribute__((aligned(16))) float s_inv[256];                 // the columns' reciprocal scales, then the rows'
     __shared__ __attribute__((aligned(16))) uint8_t s_turn[128][128];         // column c's 8-byte piece h at place h ^ (c / 8)
-    const int g = threadIdx.x & 15, h = threadIdx.x >> 4, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int tid = threadIdx.x, g = tid & 15, h = tid >> 4, wave = tid >> 6, lane = tid & 63;
     const int bc = blockIdx.x % a.across, br = blockIdx.x / a.across;
     const int64_t r0 = (int64_t)br * 128 + 8 * h, c0 = (int64_t)bc * 128 + 8 * g;
-    float x[8][8];
+    Eight<TYPE> v[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if (r0 + i < a.rows) load8<TYPE>(a, r0 + i, c0, x[i]);
-        else
+    for (int i = 0; i < 8; ++i) v[i] = read8<TYPE>(a, r0 + i, c0);
+    uint32_t col[WORDS], row[8];
+    const auto largest = [&](auto bits) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[i][j] = 0.0f;
-    }
+        for (int k = 0; k < WORDS; ++k) col[k] = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            row[i] = 0;
+#pragma unroll
+            for (int k = 0; k < WORDS; ++k) {
+                const uint32_t m = bits(v[i].w[k]);
+                col[k] = larger<TYPE>(col[k], m);
+                row[i] = larger<TYPE>(row[i], m);
+            }
+        }
+    };
+    largest([](uint32_t w) { return magnitude<TYPE>(w); });
+    uint32_t odd = 0;
+#pragma unroll
+    for (int k = 0; k < WORDS; ++k) odd |= finite_only<TYPE>(col[k]) ^ col[k];
+    if (odd) largest([](uint32_t w) { return finite_only<TYPE>(magnitude<TYPE>(w)); });
     const int64_t wide = (a.cols + 15) & ~(int64_t)15, tall = (a.rows + 15) & ~(int64_t)15;
-    float tile_s = 0.0f, tile_inv = 0.0f;
     if constexpr (TILE) {
         uint32_t m = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) m = max(m, size_bits(x[i][j]));
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d, 64));
-        if (lane == 0) s_max[wave][0] = m;
-        __syncthreads();
-        m = max(max(s_max[0][0], s_max[1][0]), max(s_max[2][0], s_max[3][0]));
-        block_scale<FORMAT>(m, a.pow2, tile_s, tile_inv);
-        if (threadIdx.x == 0) {
-            if (a.codes) a.scales[(int64_t)br * a.across + bc] = tile_s;
-            if (a.codes_t) a.scales_t[(int64_t)bc * a.down + br] = tile_s;
-        }
-    }
-    if (a.codes) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            float s = tile_s, inv = tile_inv;
-            if constexpr (!TILE) {
-                uint32_t m = 0;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) m = max(m, size_bits(x[i][j]));
-#pragma unroll
-                for (int d = 1; d < 16; d <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d, 16));
-                block_scale<FORMAT>(m, a.pow2, s, inv);
-            }
-            if (r0 + i < a.rows) {
-                if (c0 < wide) *reinterpret_cast<uint2 *>(a.codes + (r0 + i) * a.ld + c0) = codes8<FORMAT>(x[i], inv);
-                if (!TILE && g == 0) a.scales[(r0 + i) * a.across + bc] = s;
-            }
-        }
-    }
-    if (!a.codes_t) return;
-    float inv_t[8];
-    if constexpr (!TILE) {
-        uint32_t m[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            m[j] = 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) m[j] = max(m[j], size_bits(x[i][j]));
-            m[j] = max(m[j], (uint32_t)__shfl_xor((int)m[j], 16, 64));
-            m[j] = max(m[j], (uint32_t)__shfl_xor((int)m[j], 32, 64));
-            if (lane < 16) s_max[wave][8 * g + j] = m[j];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int c = 8 * g + j;
-            const uint32_t all = max(max(s_max[0][c], s_max[1][c]), max(s_max[2][c], s_max[3][c]));
-            float s;
-            block_scale<FORMAT>(all, a.pow2, s, inv_t[j]);
-            if (h == 0 && c0 + j < a.cols) a.scales_t[(c0 + j) * a.down + br] = s;
-        }
+        for (int k = 0; k < WORDS; ++k) m = larger<TYPE>(m, col[k]);
+        m = largest_of_16<TYPE>(m);
+        m = larger<TYPE>(m, (uint32_t)__shfl_xor((int)m, 16, 64));
+        m = larger<TYPE>(m, (uint32_t)__shfl_xor((int)m, 32, 64));
+        if (TYPE != ICQ_F32) m = max(m & 0xffffu, m >> 16);
+        if (lane == 0) s_rows[wave] = m;
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) inv_t[j] = tile_inv;
+        for (int i = 0; i < 8; ++i) {
+            uint32_t m = largest_of_16<TYPE>(row[i]);
+            if (TYPE != ICQ_F32) m = max(m & 0xffffu, m >> 16);
+            if (g == i) s_rows[8 * h + i] = m;
+        }
+#pragma unroll
+        for (int k = 0; k < WORDS; ++k) {
+            uint32_t m = larger<TYPE>(col[k], (uint32_t)__shfl_xor((int)col[k], 16, 64));
+            m = larger<TYPE>(m, (uint32_t)__shfl_xor((int)m, 32, 64));
+            if (lane < 16) {
+                if (TYPE == ICQ_F32) s_cols[wave][8 * g + k] = m;
+                else *reinterpret_cast<uint2 *>(&s_cols[wave][8 * g + 2 * k]) = make_uint2(m & 0xffffu, m >> 16);
+            }
+        }
     }
+    __syncthreads();
+    float inv_r[8], inv_c[8];
+    if constexpr (TILE) {
+        const uint32_t m = max(max(s_rows[0], s_rows[1]), max(s_rows[2], s_rows[3]));
+        float s, inv;
+        block_scale<FORMAT>(float_bits<TYPE>(m), a.pow2, s, inv);
+        if (tid == 0) {
+            if (a.codes) a.scales[(int64_t)br * a.across + bc] = s;
+            if (a.codes_t) a.scales_t[(int64_t)bc * a.down + br] = s;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) inv_r[i] = inv_c[i] = inv;
+    } else {
+        const int at = tid & 127;
+        const uint32_t m = tid < 128 ? max(max(s_cols[0][at], s_cols[1][at]), max(s_cols[2][at], s_cols[3][at])) : s_rows[at];
+        float s, inv;
+        block_scale<FORMAT>(float_bits<TYPE>(m), a.pow2, s, inv);
+        s_inv[tid] = inv;
+        const int64_t r = (int64_t)br * 128 + at, c = (int64_t)bc * 128 + at;
+        if (tid < 128) {
+            if (a.codes_t && c < a.cols) a.scales_t[c * a.down + br] = s;
+        } else if (a.codes && r < a.rows) {
+            a.scales[r * a.across + bc] = s;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            inv_c[i] = s_inv[8 * g + i];
+            inv_r[i] = s_inv[128 + 8 * h + i];
+        }
+    }
+    float x[8][8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        values8<TYPE>(v[i], x[i]);
+        if (a.codes && r0 + i < a.rows && c0 < wide) *reinterpret_cast<uint2 *>(a.codes + (r0 + i) * a.ld + c0) = codes8<FORMAT>(x[i], inv_r[i]);
+    }
+    if (!a.codes_t) return;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         float y[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] = x[i][j];
-        *reinterpret_cast<uint2 *>(&s_turn[8 * g + j][8 * (h ^ g)]) = codes8<FORMAT>(y, inv_t[j]);
+        *reinterpret_cast<uint2 *>(&s_turn[8 * g + j][8 * (h ^ g)]) = codes8<FORMAT>(y, inv_c[j]);
     }
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-        const int at = u * 256 + threadIdx.x, c = at >> 3, piece = (at & 7) * 16;
-        const int64_t col = (int64_t)bc * 128 + c, row = (int64_t)br * 128 + piece;
-        if (col < a.cols && row < tall) {
-            const uint4 v = *reinterpret_cast<const uint4 *>(&s_turn[c][piece ^ ((c >> 4) << 4)]);
-            *reinterpret_cast<uint4 *>(a.codes_t + col * a.ld_t + row) = (c & 8) ? make_uint4(v.z, v.w, v.x, v.y) : v;
+        const int at = u * 256 + tid, c = at >> 3, piece = (at & 7) * 16;
+        const int64_t out = (int64_t)bc * 128 + c, from = (int64_t)br * 128 + piece;
+        if (out < a.cols && from < tall) {
+            const uint4 q = *reinterpret_cast<const uint4 *>(&s_turn[c][piece ^ ((c >> 4) << 4)]);
+            *reinterpret_cast<uint4 *>(a.codes_t + out * a.ld_t + from) = (c & 8) ? make_uint4(q.z, q.w, q.x, q.y) : q;
         }
     }
 }
