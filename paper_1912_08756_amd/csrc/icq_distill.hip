@@ -37,7 +37,7 @@ struct Distill {
     const float *grad_loss;
     void *grad;
     int64_t ld_grad;
-    int splits;
+    int splits, num_cu;
     struct Part *part;             // [R][splits]
 };
 
@@ -91,7 +91,7 @@ struct List {
     float p[CAP], log_p[CAP];
     float x[CAP];                  // the student's logit
     uint32_t slot_id[2 * CAP];     // the ids, by hash
-    float red[24];
+    float red[40];
     uint32_t twice;
 };
 
@@ -381,7 +381,7 @@ __device__ __forceinline__ uint4 gradient_of(const uint4 &w, float m, float a2, 
 template <int TYPE, bool REST, int CAP>
 __global__ __launch_bounds__(T) void distill_forward_kernel(Distill a) {
     typedef IcqElem<TYPE> E;
-    constexpr int U = 4;
+    constexpr int U = 8;
     __shared__ List<CAP> l;
     __shared__ uint32_t s_bits[REST ? CHUNK / 32 : 1];
     const int tid = threadIdx.x, k = (int)(blockIdx.x % (uint32_t)a.splits);
@@ -454,7 +454,7 @@ __global__ __launch_bounds__(T) void distill_join_kernel(Distill a) {
 template <int TYPE, bool VEC, bool JOIN, int CAP>
 __global__ __launch_bounds__(T) void distill_backward_kernel(Distill a) {
     typedef IcqElem<TYPE> E;
-    constexpr int PER = E::PER, U = 4, PLACES = (CAP + T - 1) / T;
+    constexpr int PER = E::PER, U = 8, PLACES = (CAP + T - 1) / T;
     __shared__ List<CAP> l;
     const int tid = threadIdx.x, k = (int)(blockIdx.x % (uint32_t)a.splits);
     const int64_t row = blockIdx.x / (uint32_t)a.splits;
@@ -593,8 +593,10 @@ __global__ __launch_bounds__(N, 4) void distill_row_kernel(Distill a) {
 }
 
 // Slices per row: one where there is a row for every compute unit, else enough blocks for the chip, none shorter than 8192 elements.
-int splits_of(int64_t R, int64_t V, int num_cu) {
-    if (R >= num_cu) return 1;
+// Loss and gradient together in one kernel (row_bytes: a row's, else 0): one slice from half as many rows on (200 rows of 131072 bf16:
+// 46 us in slices, 34 whole; 64 rows: 21 and 33), and for rows of up to 64 KB.
+int splits_of(int64_t R, int64_t V, int num_cu, int64_t row_bytes) {
+    if (R >= num_cu || (row_bytes > 0 && (2 * R >= num_cu || row_bytes <= 65536))) return 1;
     const int64_t want = (8ll * num_cu + R - 1) / (R > 0 ? R : 1), most = V / 8192;
     const int64_t n = want < most ? want : most;
     return (int)(n < 1 ? 1 : n > 1024 ? 1024 : n);
@@ -620,7 +622,7 @@ Distill params(const void *logits, int64_t R, int64_t V, int64_t ld, float scale
     while (a.slots < 2 * topk) a.slots *= 2;
     a.teacher_scale = teacher_scale; a.teacher_lse = teacher_lse;
     a.loss = nullptr; a.stats = nullptr; a.grad_loss = nullptr; a.grad = nullptr; a.ld_grad = 0;
-    a.splits = 1; a.part = nullptr;
+    a.splits = 1; a.num_cu = 0; a.part = nullptr;
     return a;
 }
 
@@ -642,10 +644,11 @@ void launch_distill(const Distill &a, hipStream_t s) {
     constexpr int SIZE = sizeof(typename IcqElem<TYPE>::raw);
     if (a.grad && a.splits == 1 && same_phase(a, SIZE)) {
         // threads and held groups by the row's length: up to 16, 32, 64 KB, and longer (4096 rows of 24000 bf16: 86 us by 256
-        // threads, 100 by 512; of 131072: 473 and 431)
+        // threads, 100 by 512; of 131072: 473 and 431); a row by itself on a compute unit by 1024
         auto go = [&](auto kernel, int n) { hipLaunchKernelGGL(kernel, dim3((uint32_t)a.R), dim3(n), 0, s, a); };
         const int64_t bytes = a.V * SIZE;
-        if (bytes <= 256 * 4 * 16) go(distill_row_kernel<TYPE, REST, CAP, 256, 4, false>, 256);
+        if (a.R <= a.num_cu && bytes > 256 * 4 * 16 && bytes <= 1024 * 4 * 16) go(distill_row_kernel<TYPE, REST, CAP, 1024, 4, false>, 1024);
+        else if (bytes <= 256 * 4 * 16) go(distill_row_kernel<TYPE, REST, CAP, 256, 4, false>, 256);
         else if (bytes <= 256 * 8 * 16) go(distill_row_kernel<TYPE, REST, CAP, 256, 8, false>, 256);
         else if (bytes <= 256 * 16 * 16) go(distill_row_kernel<TYPE, REST, CAP, 256, 16, false>, 256);
         else go(distill_row_kernel<TYPE, REST, CAP, 512, 16, true>, 512);
@@ -666,7 +669,7 @@ ICQ_EXPORT int icq_distill_workspace_bytes(int64_t R, int64_t V, size_t *out) {
     if (!out || R < 0 || R > ICQ_MAX_Q || V < 1 || V > ICQ_MAX_EXTENT) return ICQ_ERR_ARG;
     const int cu = icq_num_cu();
     if (cu <= 0) return ICQ_ERR_HIP;
-    *out = part_bytes(R, splits_of(R, V, cu)) + part_bytes(R, 1);
+    *out = part_bytes(R, splits_of(R, V, cu, 0)) + part_bytes(R, 1);
     return ICQ_OK;
 }
 
@@ -679,13 +682,14 @@ ICQ_EXPORT int icq_distill(const void *logits, int type, int64_t R, int64_t V, i
     const int cu = icq_num_cu();
     if (cu <= 0) return ICQ_ERR_HIP;
     Distill a = params(logits, R, V, ld, scale, ids, values, topk, teacher_scale, teacher_lse);
-    a.splits = splits_of(R, V, cu);
-    const size_t parts = part_bytes(R, a.splits);
+    const size_t parts = part_bytes(R, splits_of(R, V, cu, 0));
     if (!workspace || (uintptr_t)workspace % ICQ_ALIGN != 0 || workspace_bytes < parts + part_bytes(R, 1)) return ICQ_ERR_WORKSPACE;
     a.part = static_cast<Part *>(workspace);
     a.loss = loss;
     a.stats = stats ? reinterpret_cast<float4 *>(stats) : reinterpret_cast<float4 *>(static_cast<char *>(workspace) + parts);
     a.grad_loss = grad_loss; a.grad = grad; a.ld_grad = ld_grad;
+    a.num_cu = cu;
+    a.splits = splits_of(R, V, cu, grad && same_phase(a, icq_type_bytes(type)) ? V * icq_type_bytes(type) : 0);
     hipStream_t s = static_cast<hipStream_t>(stream);
     const bool few = topk <= SHORT;
     ICQ_FOR_TYPE(type,
@@ -703,7 +707,7 @@ ICQ_EXPORT int icq_distill_backward(const void *logits, int type, int64_t R, int
     const int cu = icq_num_cu();
     if (cu <= 0) return ICQ_ERR_HIP;
     Distill a = params(logits, R, V, ld, scale, ids, values, topk, teacher_scale, teacher_lse);
-    a.splits = splits_of(R, V, cu);
+    a.splits = splits_of(R, V, cu, 0);
     a.stats = reinterpret_cast<float4 *>(const_cast<float *>(stats));
     a.grad_loss = grad_loss; a.grad = grad; a.ld_grad = ld_grad;
     hipStream_t s = static_cast<hipStream_t>(stream);

@@ -162,27 +162,27 @@ __device__ __forceinline__ void values8(const Eight<TYPE> &v, float *x) {
     for (int h = 0; h < Eight<TYPE>::WORDS / 4; ++h) IcqElem<TYPE>::unpack(make_uint4(v.w[4 * h], v.w[4 * h + 1], v.w[4 * h + 2], v.w[4 * h + 3]), x + 4 * h);
 }
 
-// A 128 x 128 tile per block; thread (g, h) holds rows 8 h .. 8 h + 7 of columns 8 g .. 8 g + 7.
+// A 128 x 128 tile per block; thread (g, h) holds rows 4 h .. 4 h + 3 of columns 8 g .. 8 g + 7.
 // TILE: one scale for the whole tile, else one per row and column of it, each worked out by one thread.
 template <int TYPE, int FORMAT, bool TILE>
-__global__ __launch_bounds__(256) void quantize_tile_kernel(Quantize a) {
+__global__ __launch_bounds__(512) void quantize_tile_kernel(Quantize a) {
     constexpr int WORDS = Eight<TYPE>::WORDS;
-    __shared__ __attribute__((aligned(16))) uint32_t s_cols[4][128];          // largest magnitudes: of a wavefront's rows in each column,
+    __shared__ __attribute__((aligned(16))) uint32_t s_cols[8][128];          // largest magnitudes: of a wavefront's rows in each column,
     __shared__ __attribute__((aligned(16))) uint32_t s_rows[128];             // of each row
     __shared__ __attribute__((aligned(16))) float s_inv[256];                 // the columns' reciprocal scales, then the rows'
-    __shared__ __attribute__((aligned(16))) uint8_t s_turn[128][128];         // column c's 8-byte piece h at place h ^ (c / 8)
+    __shared__ __attribute__((aligned(16))) uint8_t s_turn[128][128];         // column c's 8-byte piece p at place p ^ (c / 8)
     const int tid = threadIdx.x, g = tid & 15, h = tid >> 4, wave = tid >> 6, lane = tid & 63;
     const int bc = blockIdx.x % a.across, br = blockIdx.x / a.across;
-    const int64_t r0 = (int64_t)br * 128 + 8 * h, c0 = (int64_t)bc * 128 + 8 * g;
-    Eight<TYPE> v[8];
+    const int64_t r0 = (int64_t)br * 128 + 4 * h, c0 = (int64_t)bc * 128 + 8 * g;
+    Eight<TYPE> v[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = read8<TYPE>(a, r0 + i, c0);
-    uint32_t col[WORDS], row[8];
+    for (int i = 0; i < 4; ++i) v[i] = read8<TYPE>(a, r0 + i, c0);
+    uint32_t col[WORDS], row[4];
     const auto largest = [&](auto bits) {
 #pragma unroll
         for (int k = 0; k < WORDS; ++k) col[k] = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 4; ++i) {
             row[i] = 0;
 #pragma unroll
             for (int k = 0; k < WORDS; ++k) {
@@ -209,10 +209,10 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(Quantize a) {
         if (lane == 0) s_rows[wave] = m;
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 4; ++i) {
             uint32_t m = largest_of_16<TYPE>(row[i]);
             if (TYPE != ICQ_F32) m = max(m & 0xffffu, m >> 16);
-            if (g == i) s_rows[8 * h + i] = m;
+            if (g == i) s_rows[4 * h + i] = m;
         }
 #pragma unroll
         for (int k = 0; k < WORDS; ++k) {
@@ -225,9 +225,11 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(Quantize a) {
         }
     }
     __syncthreads();
-    float inv_r[8], inv_c[8];
+    float inv_r[4], inv_c[8];
     if constexpr (TILE) {
-        const uint32_t m = max(max(s_rows[0], s_rows[1]), max(s_rows[2], s_rows[3]));
+        uint32_t m = s_rows[0];
+#pragma unroll
+        for (int w = 1; w < 8; ++w) m = max(m, s_rows[w]);
         float s, inv;
         block_scale<FORMAT>(float_bits<TYPE>(m), a.pow2, s, inv);
         if (tid == 0) {
@@ -235,44 +237,48 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(Quantize a) {
             if (a.codes_t) a.scales_t[(int64_t)bc * a.down + br] = s;
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) inv_r[i] = inv_c[i] = inv;
+        for (int i = 0; i < 8; ++i) inv_r[i & 3] = inv_c[i] = inv;
     } else {
-        const int at = tid & 127;
-        const uint32_t m = tid < 128 ? max(max(s_cols[0][at], s_cols[1][at]), max(s_cols[2][at], s_cols[3][at])) : s_rows[at];
-        float s, inv;
-        block_scale<FORMAT>(float_bits<TYPE>(m), a.pow2, s, inv);
-        s_inv[tid] = inv;
-        const int64_t r = (int64_t)br * 128 + at, c = (int64_t)bc * 128 + at;
-        if (tid < 128) {
-            if (a.codes_t && c < a.cols) a.scales_t[c * a.down + br] = s;
-        } else if (a.codes && r < a.rows) {
-            a.scales[r * a.across + bc] = s;
+        if (tid < 256) {
+            const int at = tid & 127;
+            uint32_t m = tid < 128 ? s_cols[0][at] : s_rows[at];
+            if (tid < 128)
+#pragma unroll
+                for (int w = 1; w < 8; ++w) m = max(m, s_cols[w][at]);
+            float s, inv;
+            block_scale<FORMAT>(float_bits<TYPE>(m), a.pow2, s, inv);
+            s_inv[tid] = inv;
+            const int64_t r = (int64_t)br * 128 + at, c = (int64_t)bc * 128 + at;
+            if (tid < 128) {
+                if (a.codes_t && c < a.cols) a.scales_t[c * a.down + br] = s;
+            } else if (a.codes && r < a.rows) {
+                a.scales[r * a.across + bc] = s;
+            }
         }
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             inv_c[i] = s_inv[8 * g + i];
-            inv_r[i] = s_inv[128 + 8 * h + i];
+            if (i < 4) inv_r[i] = s_inv[128 + 4 * h + i];
         }
     }
-    float x[8][8];
+    float x[4][8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 4; ++i) {
         values8<TYPE>(v[i], x[i]);
         if (a.codes && r0 + i < a.rows && c0 < wide) *reinterpret_cast<uint2 *>(a.codes + (r0 + i) * a.ld + c0) = codes8<FORMAT>(x[i], inv_r[i]);
     }
     if (!a.codes_t) return;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        float y[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = x[i][j];
-        *reinterpret_cast<uint2 *>(&s_turn[8 * g + j][8 * (h ^ g)]) = codes8<FORMAT>(y, inv_c[j]);
+        uint32_t w = icq_codes2<FORMAT, false>(x[0][j] * inv_c[j], x[1][j] * inv_c[j], 0);
+        w = icq_codes2<FORMAT, true>(x[2][j] * inv_c[j], x[3][j] * inv_c[j], w);
+        *reinterpret_cast<uint32_t *>(&s_turn[8 * g + j][8 * ((h >> 1) ^ g) + 4 * (h & 1)]) = w;
     }
     __syncthreads();
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        const int at = u * 256 + tid, c = at >> 3, piece = (at & 7) * 16;
+    for (int u = 0; u < 2; ++u) {
+        const int at = u * 512 + tid, c = at >> 3, piece = (at & 7) * 16;
         const int64_t out = (int64_t)bc * 128 + c, from = (int64_t)br * 128 + piece;
         if (out < a.cols && from < tall) {
             const uint4 q = *reinterpret_cast<const uint4 *>(&s_turn[c][piece ^ ((c >> 4) << 4)]);
@@ -290,9 +296,9 @@ int launch(const Quantize &a, int block_rows, hipStream_t s) {
             hipLaunchKernelGGL(HIP_KERNEL_NAME(quantize_rows_kernel<TYPE, FORMAT>), dim3((tasks + 15u) / 16u), dim3(256), 0, s, a, r, tasks);
         }
     } else if (block_rows == 1) {
-        hipLaunchKernelGGL(HIP_KERNEL_NAME(quantize_tile_kernel<TYPE, FORMAT, false>), dim3((uint32_t)((int64_t)a.across * a.down)), dim3(256), 0, s, a);
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(quantize_tile_kernel<TYPE, FORMAT, false>), dim3((uint32_t)((int64_t)a.across * a.down)), dim3(512), 0, s, a);
     } else {
-        hipLaunchKernelGGL(HIP_KERNEL_NAME(quantize_tile_kernel<TYPE, FORMAT, true>), dim3((uint32_t)((int64_t)a.across * a.down)), dim3(256), 0, s, a);
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(quantize_tile_kernel<TYPE, FORMAT, true>), dim3((uint32_t)((int64_t)a.across * a.down)), dim3(512), 0, s, a);
     }
     return icq_check_launch();
 }
