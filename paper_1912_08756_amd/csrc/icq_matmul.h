@@ -12,7 +12,6 @@ struct Product {
     int64_t ldo;
     float *part;               // [splits][M][N] partial sums where splits > 1
     int splits, per;           // blocks along K per split
-    int vec;                   // rows of the result start on 16 bytes
 };
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -38,9 +37,12 @@ __device__ __forceinline__ void store4(const Product &p, int64_t m, int64_t n, c
     typedef IcqElem<TYPE> E;
     typedef typename E::raw raw;
     raw *o = static_cast<raw *>(p.out) + m * p.ldo + n;
-    if (p.vec && n + 4 <= p.N) {
-        if constexpr (TYPE == ICQ_F32) *reinterpret_cast<icq_f32x4 *>(o) = v;
-        else *reinterpret_cast<uint2 *>(o) = make_uint2(E::pack2(v[0], v[1]), E::pack2(v[2], v[3]));
+    if (n + 4 <= p.N) {                                // (the memory pipe takes 8 or 16 bytes to any address)
+        if constexpr (TYPE == ICQ_F32) __builtin_memcpy(o, &v, 16);
+        else {
+            const uint2 w = make_uint2(E::pack2(v[0], v[1]), E::pack2(v[2], v[3]));
+            __builtin_memcpy(o, &w, 8);
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -68,8 +70,10 @@ __device__ __forceinline__ uint4 first_bytes(const uint4 &v, int n) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// The product in tiles of 256 x 256 (wide) or 128 x 128, p.splits parts of the contraction (icq_matmul_tiles.hip).
-int icq_launch_product_tiles(const Product &p, bool wide, int a_format, int b_format, bool rows, bool pow2, int out_type, hipStream_t s);
+// The product in tiles of 256 x 256 (not into f32), or of 128 x 128 with two stages in the LDS or four, p.splits parts of the contraction
+// (icq_matmul_tiles.hip).
+enum icq_tiles { ICQ_TILES_WIDE, ICQ_TILES_SMALL, ICQ_TILES_DEEP };
+int icq_launch_product_tiles(const Product &p, icq_tiles tiles, int a_format, int b_format, bool rows, bool pow2, int out_type, hipStream_t s);
 // The product of at most ICQ_FEW_ROWS rows of a (icq_matmul_few.hip).
 #define ICQ_FEW_ROWS 32
 int icq_product_few_splits(int64_t N, int64_t K, int num_cu);

@@ -23,8 +23,12 @@ __global__ __launch_bounds__(256) void product_join_kernel(Product p) {
     const int64_t total = p.M * p.N;
     const float *from = p.part + m * p.N + n;
     icq_f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (p.N % 4 == 0) {
-        for (int k = 0; k < p.splits; ++k) s += *reinterpret_cast<const icq_f32x4 *>(from + k * total);
+    if (n + 4 <= p.N) {
+        for (int k = 0; k < p.splits; ++k) {
+            icq_f32x4 v;
+            __builtin_memcpy(&v, from + k * total, 16);
+            s += v;
+        }
     } else {
         for (int k = 0; k < p.splits; ++k)
 #pragma unroll
@@ -34,17 +38,20 @@ __global__ __launch_bounds__(256) void product_join_kernel(Product p) {
     store4<TYPE>(p, m, n, s);
 }
 
-// How a product is computed: `few` rows; else in tiles of 256 x 256 or 128 x 128, the contraction in `splits` parts.
+// How a product is computed: `few` rows; else in tiles, the contraction in `splits` parts.
 struct Plan {
-    bool few, wide;
+    bool few;
+    icq_tiles tiles;
     int splits;
 };
 
 // Tiles: the plan of the least time by a model of it, in us.  A step (one scale block) of a 256 x 256 tile takes 1.8, of two 128 x 128
-// tiles that share a compute unit 1.2 and of one by itself 0.75; with the widened codes of a 32-bit result 1.9 and 1.1.  A split
-// writes and reads its sums at 4 TB/s and costs a launch.
+// tiles that share a compute unit 1.2 and of one by itself DEEP_FAST; with the widened codes of a 32-bit result 1.9 and DEEP_EXACT.  A
+// split writes and reads its sums at 4 TB/s and costs a launch.
+constexpr double DEEP_FAST = 0.5, DEEP_EXACT = 0.9;
+
 Plan plan_of(int64_t M, int64_t N, int64_t K, bool exact, int num_cu) {
-    Plan best = {M <= ICQ_FEW_ROWS, false, 1};
+    Plan best = {M <= ICQ_FEW_ROWS, ICQ_TILES_SMALL, 1};
     if (best.few) {
         best.splits = icq_product_few_splits(N, K, num_cu);
         return best;
@@ -55,17 +62,15 @@ Plan plan_of(int64_t M, int64_t N, int64_t K, bool exact, int num_cu) {
         const int64_t T = wide ? 256 : 128, tiles = ((M + T - 1) / T) * ((N + T - 1) / T);
         for (int splits = 1; splits <= 16 && (splits == 1 || kb >= 4 * splits); splits *= 2) {
             const int64_t blocks = tiles * splits, steps = (kb + splits - 1) / splits;
-            double us;
-            if (wide) {
-                us = (double)((blocks + num_cu - 1) / num_cu) * steps * 1.8;
-            } else {
-                const int64_t pairs = blocks / (2 * num_cu), left = blocks % (2 * num_cu);
-                us = steps * ((exact ? 1.9 : 1.2) * (pairs + (left > num_cu ? 1 : 0)) + (left > 0 && left <= num_cu ? (exact ? 1.1 : 0.75) : 0.0));
-            }
+            const bool deep = !wide && blocks <= num_cu;
+            double us = steps;
+            if (wide) us *= 1.8 * ((blocks + num_cu - 1) / num_cu);
+            else if (deep) us *= exact ? DEEP_EXACT : DEEP_FAST;
+            else us *= (exact ? 1.9 : 1.2) * ((blocks + 2 * num_cu - 1) / (2 * num_cu));
             if (splits > 1) us += 5.0 + (double)splits * M * N * 8 / 4e6;
             if (least < 0.0 || us < least) {
                 least = us;
-                best.wide = wide;
+                best.tiles = wide ? ICQ_TILES_WIDE : deep ? ICQ_TILES_DEEP : ICQ_TILES_SMALL;
                 best.splits = splits;
             }
         }
@@ -112,7 +117,6 @@ ICQ_EXPORT int icq_block_matmul(const uint8_t *a, int a_format, int64_t lda, con
     p.splits = plan.splits;
     p.per = (p.kb + p.splits - 1) / p.splits;
     p.part = static_cast<float *>(workspace);
-    p.vec = (uintptr_t)out % 16 == 0 && ldo * size % 16 == 0;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const dim3 by_four((uint32_t)((N + 1023) / 1024), (uint32_t)(M < 32768 ? M : 32768), (uint32_t)((M + 32767) / 32768));
     if (K == 0) {
@@ -124,7 +128,7 @@ ICQ_EXPORT int icq_block_matmul(const uint8_t *a, int a_format, int64_t lda, con
         return ICQ_ERR_WORKSPACE;
     const bool rows = b_block_rows == 1;
     const int rc = plan.few ? icq_launch_product_few(p, cu, a_format, b_format, rows, out_type, s)
-                            : icq_launch_product_tiles(p, plan.wide, a_format, b_format, rows, scaling == ICQ_SCALES_POW2, out_type, s);
+                            : icq_launch_product_tiles(p, plan.tiles, a_format, b_format, rows, scaling == ICQ_SCALES_POW2, out_type, s);
     if (rc != ICQ_OK || p.splits == 1) return rc;
     ICQ_FOR_TYPE(out_type, hipLaunchKernelGGL(HIP_KERNEL_NAME(product_join_kernel<TYPE>), by_four, dim3(256), 0, s, p))
     return icq_check_launch();

@@ -9,16 +9,17 @@
 
 namespace {
 
-// Rows and columns of a wavefront's part in units of 32, wavefronts along m and n.
-template <int NI_, int NJ_, int WM_, int WN_>
+// Rows and columns of a wavefront's part in units of 32, wavefronts along m and n, stages in the LDS.
+template <int NI_, int NJ_, int WM_, int WN_, int DEPTH_>
 struct Shape {
-    static constexpr int NI = NI_, NJ = NJ_, WM = WM_, WN = WN_, THREADS = 64 * WM * WN, T = 32 * NI * WM;
+    static constexpr int NI = NI_, NJ = NJ_, WM = WM_, WN = WN_, DEPTH = DEPTH_, THREADS = 64 * WM * WN, T = 32 * NI * WM;
     static constexpr int STAGE = 2 * T * 128;                                 // bytes of a stage
-    static constexpr int LDS_BYTES = 2 * STAGE + 3 * 8 * T * 4;
-    static_assert(32 * NJ * WN == T && THREADS == 2 * T && NJ == 2 && 2 * STAGE / (WM * WN) >= 32 * 68 * 4, "square tiles, two threads a row; a stage's four parts over two columns twice");
+    static constexpr int LDS_BYTES = DEPTH * STAGE + 3 * 8 * T * 4;
+    static_assert(32 * NJ * WN == T && THREADS == 2 * T && NJ == 2 && DEPTH * STAGE / (WM * WN) >= 32 * 68 * 4, "square tiles, two threads a row; a stage's four parts over two columns twice");
 };
-typedef Shape<4, 2, 2, 4> Wide;
-typedef Shape<2, 2, 2, 2> Small;
+typedef Shape<4, 2, 2, 4, 2> Wide;
+typedef Shape<2, 2, 2, 2, 2> Small;    // two blocks share a compute unit
+typedef Shape<2, 2, 2, 2, 4> Deep;     // one has it to itself
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
@@ -41,28 +42,29 @@ __device__ __forceinline__ icq_i32x8 two_pieces(const uint8_t *row, int c0, int 
     return f;
 }
 
-constexpr int ALL_LOADS = 0x0f70;          // s_waitcnt vmcnt(0), the other counters left
+// s_waitcnt: at most n loads still under way, the other counters left alone
+constexpr int loads_left(int n) { return 0x0f70 | (n & 15) | (n >> 4) << 14; }
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 // A buffer descriptor of the memory from p on (a wavefront's own: scalar).
-__device__ __forceinline__ i32x4 bytes_from(const uint8_t *p) {
+__device__ __forceinline__ i32x4 bytes_from(const void *p) {
     const uint64_t u = reinterpret_cast<uint64_t>(p);
     i32x4 r = {__builtin_amdgcn_readfirstlane((int)(uint32_t)u), __builtin_amdgcn_readfirstlane((int)(uint32_t)(u >> 32) & 0xffff), -1, 0x00027000};
     return r;
 }
 
 // 16 bytes per lane from base + off + by into the LDS at `to` + 16 * lane.  Written out because the compiler makes every later LDS read
-// wait for loads of its own built-in; they have no destination registers, and the waits for them are those of ALL_LOADS.  (M0: nothing
+// wait for loads of its own built-in; they have no destination registers, and the waits for them are those of loads_left(0).  (M0: nothing
 // else here uses it.)
 __device__ __forceinline__ void load_to_lds(const i32x4 &base, uint32_t off, int by, uint32_t to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(off), "s"(base), "s"(by) : "memory");
 }
 
 // 32 rows and 64 columns of the result from a wavefront's accumulators, whole rows at a time: in the accumulators a lane has four
-// neighbours of one row and the lanes 32 rows, whose stores would be 16 bytes here and there.  vec: rows start on 16 bytes.
+// neighbours of one row and the lanes 32 rows, whose stores would be 16 bytes here and there.
 template <int TYPE>
-__device__ __forceinline__ void store_rows(uint8_t *turn, const f32x16 (&acc)[2], void *out, int64_t ldo, bool vec, int64_t M, int64_t N, int64_t m0, int64_t n0,
+__device__ __forceinline__ void store_rows(uint8_t *turn, const f32x16 (&acc)[2], void *out, int64_t ldo, int64_t M, int64_t N, int64_t m0, int64_t n0,
                                            int lane) {
     typedef IcqElem<TYPE> E;
     typedef typename E::raw raw;
@@ -81,25 +83,34 @@ __device__ __forceinline__ void store_rows(uint8_t *turn, const f32x16 (&acc)[2]
         }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    raw *to = static_cast<raw *>(out);
-    if (vec && n0 + 64 <= N) {
-        constexpr int LANES = 64 / PER, ROWS_AT_ONCE = 64 / LANES;
-        const int c = lane % LANES * PER;
+    constexpr int LANES = 64 / PER, ROWS_AT_ONCE = 64 / LANES;
+    const int c = lane % LANES * PER;
+    raw *to = static_cast<raw *>(out) + (m0 + lane / LANES) * ldo + n0 + c;
+    const int left = (int)min((int64_t)PER, N - n0 - c), rows = (int)min((int64_t)32, M - m0);
 #pragma unroll
-        for (int r = lane / LANES; r < 32; r += ROWS_AT_ONCE)
-            if (m0 + r < M) *reinterpret_cast<uint4 *>(to + (m0 + r) * ldo + n0 + c) = *reinterpret_cast<const uint4 *>(mine + r * STRIDE + c);
-    } else if (n0 + lane < N) {
-#pragma unroll 8
-        for (int r = 0; r < 32; ++r)
-            if (m0 + r < M) to[(m0 + r) * ldo + n0 + lane] = mine[r * STRIDE + lane];
+    for (int r0 = 0; r0 < 32; r0 += ROWS_AT_ONCE, to += ROWS_AT_ONCE * ldo) {
+        const int r = r0 + lane / LANES;
+        const raw *from = mine + r * STRIDE + c;
+        if (r >= rows) continue;
+        if (left == PER) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(from);
+            __builtin_memcpy(to, &v, 16);                                     // (to any address)
+        } else {
+            for (int e = 0; e < left; ++e) to[e] = from[e];
+        }
     }
+}
+
+// The same for 4 bytes per lane, to `to` + 4 * lane.
+__device__ __forceinline__ void load_word_to_lds(const i32x4 &base, uint32_t off, int by, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(to), "v"(off), "s"(base), "s"(by) : "memory");
 }
 
 template <typename S, int FA, int FB, bool ROWS, int MODE>
 __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product p, int tiles_m, int tiles_n, int out_type) {
-    constexpr int T = S::T, NI = S::NI, NJ = S::NJ, WAVES = S::THREADS / 64;
+    constexpr int T = S::T, NI = S::NI, NJ = S::NJ, DEPTH = S::DEPTH, WAVES = S::THREADS / 64, LOADS = 8;        // of a wavefront for a stage
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
-    float *s_scales = reinterpret_cast<float *>(smem + 2 * S::STAGE);         // [3][four blocks along K][a: T, b: T]
+    float *s_scales = reinterpret_cast<float *>(smem + DEPTH * S::STAGE);     // [3][four blocks along K][a: T, b: T]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     // XCD blockIdx % 8 takes a contiguous share of the tiles, eight tiles of m at a time
     const int total = tiles_m * tiles_n, q8 = total / 8, r8 = total % 8, xcd = blockIdx.x % 8, at8 = blockIdx.x / 8;
@@ -157,6 +168,16 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product p, int t
             for (int k = 0; k < 4; ++k) f.v[k] = scale_row[min(kb + k, p.kb - 1)];
         }
         return f;
+    };
+    // the same straight into the LDS, a block along K at a time: loads of the compiler's own would have to be waited for with all others,
+    // and four stages are to stay under way (two are not: at the barrier nothing is)
+    const i32x4 rsrc_scale = bytes_from(wave < WAVES / 2 ? p.sa + m0 * p.kb : p.sb + (ROWS ? n0 : n0 >> 7) * p.kb);
+    const uint32_t off_scale = (uint32_t)((tid < T ? min((int64_t)tid, p.M - 1 - m0)
+                                                   : ROWS ? min((int64_t)(tid - T), p.N - 1 - n0) : min((int64_t)(tid & 1), ((p.N - 1) >> 7) - (n0 >> 7))) * p.kb * 4);
+    auto scales_to_lds = [&](int third, int kb) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            load_word_to_lds(rsrc_scale, off_scale, min(kb + k, p.kb - 1) * 4, DEPTH * S::STAGE + ((third * 4 + k) * 2 * T + wave * 64) * 4);
     };
     auto write_scales = [&](int third, const Four &f) {
 #pragma unroll
@@ -217,29 +238,42 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product p, int t
     if (k0 < k1) {
 #pragma unroll
         for (int u = 0; u < 4; ++u) load_part(k0, 0, u, k0 == whole ? beyond : 0);
-        write_scales(0, read_scales(k0));
-        __builtin_amdgcn_s_waitcnt(ALL_LOADS);
-        __syncthreads();
+        if constexpr (DEPTH > 2) scales_to_lds(0, k0);
+        else write_scales(0, read_scales(k0));
     }
+    uint32_t back = 0;                                                        // of the stage under way
     if (k0 < kw) {
-        Four next = read_scales(min(k0 + 4, last));
-        uint32_t back = min(k0 + 1, last) == whole ? beyond : 0;
-        load_part(min(k0 + 1, last), 1, 0, back);
-        load_part(min(k0 + 1, last), 1, 1, back);
+#pragma unroll
+        for (int d = 1; d < DEPTH; ++d) {
+            back = min(k0 + d, last) == whole ? beyond : 0;
+#pragma unroll
+            for (int u = 0; u < (d == DEPTH - 1 ? 2 : 4); ++u) load_part(min(k0 + d, last), d, u, back);
+        }
+        __builtin_amdgcn_s_waitcnt(loads_left((DEPTH - 2) * LOADS + LOADS / 2));
+    } else {
+        __builtin_amdgcn_s_waitcnt(loads_left(0));
+    }
+    __syncthreads();
+    if (k0 < kw) {
+        Four next;
+        if constexpr (DEPTH == 2) next = read_scales(min(k0 + 4, last));
         read_a(0, 0, s_scales);
 #pragma unroll
         for (int j = 0; j < NJ; ++j) read_b(j, 0, s_scales);
-        int kb = k0, third = 0;
+        int kb = k0, third = 0, buf = 0;
         do {                                                                  // four blocks: their scales are in the LDS
             block = third * 4;
             third = third == 2 ? 0 : third + 1;
-            write_scales(third, next);                                        // (nobody reads that third any more: two barriers since)
-            next = read_scales(min(kb + 8, last));
+            if constexpr (DEPTH > 2) scales_to_lds(third, min(kb + 4, last)); // (nobody reads that third any more: four barriers since)
+            else {
+                write_scales(third, next);
+                next = read_scales(min(kb + 8, last));
+            }
             const int end = min(kb + 4, kw);
             // no branch in the loop: behind one, the compiler would put off matrix instructions and keep their fragments;
             // the last steps request the last stage again
             do {
-                const int buf = (kb - k0) & 1;
+                const int next_buf = buf == DEPTH - 1 ? 0 : buf + 1, last_buf = buf == 0 ? DEPTH - 1 : buf - 1;
                 const float *sc = s_scales + block * 2 * T;
                 block = block == 11 ? 0 : block + 1;
                 const float *sc_next = s_scales + block * 2 * T;
@@ -248,32 +282,34 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product p, int t
                     if (i < NI - 1) {
                         read_a(i + 1, buf, sc);
                     } else {
-                        __builtin_amdgcn_s_waitcnt(ALL_LOADS);
-                        __syncthreads();
+                        __builtin_amdgcn_s_waitcnt(loads_left((DEPTH - 2) * LOADS));      // the next stage is here, later ones may not be
+                        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup", "local");
+                        __builtin_amdgcn_s_barrier();
                     }
 #pragma unroll
                     for (int j = 0; j < NJ; ++j) {
                         // a stage's requests are spread over four parts of the multiplication: all at once they hold up the wavefront
-                        if (i == 0) load_part(min(kb + 1, last), buf ^ 1, 2 + j, back);
+                        if (i == 0) load_part(min(kb + DEPTH - 1, last), last_buf, 2 + j, back);
                         if (i == NI - 1) {
-                            back = min(kb + 2, last) == whole ? beyond : 0;
-                            load_part(min(kb + 2, last), buf, j, back);
+                            back = min(kb + DEPTH, last) == whole ? beyond : 0;
+                            load_part(min(kb + DEPTH, last), buf, j, back);
                         }
                         multiply(i, j, sc);
                         if (i == NI - 1) {                                    // the next step's first fragments (after the last step: not used)
-                            if (j == 0) read_a(0, buf ^ 1, sc_next);
-                            read_b(j, buf ^ 1, sc_next);
+                            if (j == 0) read_a(0, next_buf, sc_next);
+                            read_b(j, next_buf, sc_next);
                         }
                         __builtin_amdgcn_sched_barrier(0);                    // (later fragments would be read early, beyond the registers)
                     }
                 }
+                buf = next_buf;
             } while (++kb < end);
         } while (kb < kw);
-        __builtin_amdgcn_s_waitcnt(ALL_LOADS);
+        __builtin_amdgcn_s_waitcnt(loads_left(0));
         __syncthreads();
     }
     if (k0 < k1 && kw < k1) {                                                // the ragged end: its stage has arrived
-        const int buf = (kw - k0) & 1;
+        const int buf = (kw - k0) % DEPTH;
         const float *sc = s_scales + block * 2 * T;
         clear_beyond(buf);
 #pragma unroll
@@ -287,14 +323,14 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product p, int t
         }
     }
     __syncthreads();                                                          // (a wavefront's part of the stages takes its results)
-    uint8_t *turn = smem + wave * (2 * S::STAGE / WAVES);
+    uint8_t *turn = smem + wave * (DEPTH * S::STAGE / WAVES);
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
         const int64_t m = m0 + wm + i * 32, n = n0 + wn;
-        if (p.splits > 1) store_rows<ICQ_F32>(turn, acc[i], p.part + (int64_t)blockIdx.y * p.M * p.N, p.N, p.N % 4 == 0, p.M, p.N, m, n, lane);
-        else if (MODE == EXACT) store_rows<ICQ_F32>(turn, acc[i], p.out, p.ldo, p.vec, p.M, p.N, m, n, lane);
-        else if (out_type == ICQ_BF16) store_rows<ICQ_BF16>(turn, acc[i], p.out, p.ldo, p.vec, p.M, p.N, m, n, lane);
-        else store_rows<ICQ_F16>(turn, acc[i], p.out, p.ldo, p.vec, p.M, p.N, m, n, lane);
+        if (p.splits > 1) store_rows<ICQ_F32>(turn, acc[i], p.part + (int64_t)blockIdx.y * p.M * p.N, p.N, p.M, p.N, m, n, lane);
+        else if (MODE == EXACT) store_rows<ICQ_F32>(turn, acc[i], p.out, p.ldo, p.M, p.N, m, n, lane);
+        else if (out_type == ICQ_BF16) store_rows<ICQ_BF16>(turn, acc[i], p.out, p.ldo, p.M, p.N, m, n, lane);
+        else store_rows<ICQ_F16>(turn, acc[i], p.out, p.ldo, p.M, p.N, m, n, lane);
     }
 }
 
@@ -325,6 +361,7 @@ int launch_formats(const Product &p, int fa, int fb, bool rows, bool pow2, int o
 
 }  // namespace
 
-int icq_launch_product_tiles(const Product &p, bool wide, int fa, int fb, bool rows, bool pow2, int out_type, hipStream_t s) {
-    return wide ? launch_formats<Wide>(p, fa, fb, rows, pow2, out_type, s) : launch_formats<Small>(p, fa, fb, rows, pow2, out_type, s);
+int icq_launch_product_tiles(const Product &p, icq_tiles tiles, int fa, int fb, bool rows, bool pow2, int out_type, hipStream_t s) {
+    if (tiles == ICQ_TILES_WIDE) return launch_formats<Wide>(p, fa, fb, rows, pow2, out_type, s);
+    return tiles == ICQ_TILES_DEEP ? launch_formats<Deep>(p, fa, fb, rows, pow2, out_type, s) : launch_formats<Small>(p, fa, fb, rows, pow2, out_type, s);
 }

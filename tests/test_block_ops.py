@@ -222,6 +222,42 @@ def test_large_products(M, N, K, block, pow2, out):
 
 
 @gpu
+@pytest.mark.parametrize("M,N,K", [(4096, 4096, 300), (4099, 3970, 128), (8192, 2100, 1280)])
+@pytest.mark.parametrize("block,pow2,fa", [(128, False, "e4m3"), (128, True, "e5m2"), (1, False, "e5m2"), (1, True, "e4m3")])
+def test_products_of_many_tiles(M, N, K, block, pow2, fa):
+    _check_product(*_torch(), M, N, K, fa, "e4m3", block, pow2, "bf16" if K > 128 else "f16")
+
+
+@gpu
+@pytest.mark.parametrize("steps", range(1, 15))
+@pytest.mark.parametrize("tail", [0, 1, 16, 100])
+@pytest.mark.parametrize("M,N", [(40, 130), (1300, 3900)])
+def test_every_number_of_scale_blocks(steps, tail, M, N):
+    """The pipelines' beginnings and ends: one to fifteen blocks along the contraction, the last one whole or ragged."""
+    torch, b = _torch()
+    K = 128 * steps + tail
+    g = torch.Generator(device="cuda").manual_seed(K)
+    a = torch.randint(-8, 9, (M, K), device="cuda", generator=g).float()      # small whole numbers: every sum is exact
+    w = torch.randint(-8, 9, (N, K), device="cuda", generator=g).float()
+    ac, wc = b.icq_block_codes(M, K), b.icq_block_codes(N, K)
+    ac.copy_(a.to(ac.dtype))
+    wc.copy_(w.to(wc.dtype))
+    blocks = -(-K // 128)
+    sa = torch.exp2(torch.randint(-3, 4, (M, blocks), device="cuda", generator=g).float())
+    sw = torch.exp2(torch.randint(-3, 4, (-(-N // 128), blocks), device="cuda", generator=g).float())
+    full = sa.repeat_interleave(128, 1)[:, :K] * a
+    want = full.double() @ (sw.repeat_interleave(128, 1)[:, :K].repeat_interleave(128, 0)[:N] * w).double().t()
+    ws = torch.empty(max(1, b.icq_block_matmul_workspace_bytes(M, N, K)), dtype=torch.uint8, device="cuda")
+    for pow2 in (False, True):
+        y = torch.empty((M, N), device="cuda")
+        b.icq_block_matmul(ac, sa, wc, sw, y, ws, pow2=pow2)
+        assert torch.equal(y.double(), want)                                  # below 2^24 in units of 2^-6
+        z = torch.empty((M, N), dtype=torch.bfloat16, device="cuda")
+        b.icq_block_matmul(ac, sa, wc, sw, z, ws, pow2=pow2)
+        assert torch.equal(z, want.float().bfloat16())
+
+
+@gpu
 @pytest.mark.parametrize("M,N", [(5, 70), (70, 333), (600, 1500)])
 def test_product_into_a_wider_buffer_from_slices(M, N):
     torch, b = _torch()
