@@ -597,7 +597,7 @@ __global__ __launch_bounds__(N, 4) void distill_row_kernel(Distill a) {
 // 46 us in slices, 34 whole; 64 rows: 21 and 33), and for rows of up to 64 KB.
 int splits_of(int64_t R, int64_t V, int num_cu, int64_t row_bytes) {
     if (R >= num_cu || (row_bytes > 0 && (2 * R >= num_cu || row_bytes <= 65536))) return 1;
-    const int64_t want = (8ll * num_cu + R - 1) / (R > 0 ? R : 1), most = V / 8192;
+    const int64_t want = (4ll * num_cu + R - 1) / (R > 0 ? R : 1), most = V / 8192;
     const int64_t n = want < most ? want : most;
     return (int)(n < 1 ? 1 : n > 1024 ? 1024 : n);
 }

@@ -45,11 +45,10 @@ struct Plan {
     int splits;
 };
 
-// Tiles: the plan of the least time by a model of it, in us.  A step (one scale block) of a 256 x 256 tile takes 1.8, of two 128 x 128
-// tiles that share a compute unit 1.2 and of one by itself DEEP_FAST; with the widened codes of a 32-bit result 1.9 and DEEP_EXACT.  A
-// split writes and reads its sums at 4 TB/s and costs a launch.
-constexpr double DEEP_FAST = 0.5, DEEP_EXACT = 0.9;
-
+// Tiles: the plan of the least time by a model of it, in us, from times of every form on 128 to 8192 rows.  A step (one scale block) of a
+// 256 x 256 tile takes 1.8, of two 128 x 128 tiles that share a compute unit 1.2, of one by itself 0.5 to 0.6, the more of them the longer;
+// with the widened codes of a 32-bit result 1.9 and 0.6 to 1.2.  A split writes and reads its sums at 4.4 TB/s and costs a launch.
+// (1024 x 1024 x 4096 into bf16: 22.3 in one part, 19.4 in two, 18.8 in four, 29.4 in eight.)
 Plan plan_of(int64_t M, int64_t N, int64_t K, bool exact, int num_cu) {
     Plan best = {M <= ICQ_FEW_ROWS, ICQ_TILES_SMALL, 1};
     if (best.few) {
@@ -65,9 +64,9 @@ Plan plan_of(int64_t M, int64_t N, int64_t K, bool exact, int num_cu) {
             const bool deep = !wide && blocks <= num_cu;
             double us = steps;
             if (wide) us *= 1.8 * ((blocks + num_cu - 1) / num_cu);
-            else if (deep) us *= exact ? DEEP_EXACT : DEEP_FAST;
+            else if (deep) us *= exact ? 0.6 + 0.6 * blocks / num_cu : 0.5 + 0.1 * blocks / num_cu;
             else us *= (exact ? 1.9 : 1.2) * ((blocks + 2 * num_cu - 1) / (2 * num_cu));
-            if (splits > 1) us += 5.0 + (double)splits * M * N * 8 / 4e6;
+            if (splits > 1) us += 2.5 + (double)splits * M * N * 8 / 4.4e6;
             if (least < 0.0 || us < least) {
                 least = us;
                 best.tiles = wide ? ICQ_TILES_WIDE : deep ? ICQ_TILES_DEEP : ICQ_TILES_SMALL;
