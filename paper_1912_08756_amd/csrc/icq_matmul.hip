@@ -45,31 +45,38 @@ struct Plan {
     int splits;
 };
 
-// Tiles: the plan of the least time by a model of it, in us, from times of every form on 128 to 8192 rows.  A step (one scale block) of a
-// 256 x 256 tile takes 1.8, of two 128 x 128 tiles that share a compute unit 1.2, of one by itself 0.5 to 0.6, the more of them the longer;
-// with the widened codes of a 32-bit result 1.9 and 0.6 to 1.2.  A split writes and reads its sums at 4.4 TB/s and costs a launch.
-// (1024 x 1024 x 4096 into bf16: 22.3 in one part, 19.4 in two, 18.8 in four, 29.4 in eight.)
+// Tiles: the plan of the least time by a model of it, in us, from times of every form and number of parts on 33 to 8192 rows: 4.5 for a
+// launch with its first loads and last stores, and for a step (one scale block)
+//     256 x 256: 1.8 for a round of the chip, 1.2 and more for a part of one;
+//     128 x 128: 1.2 for two that share a compute unit, 0.5 to 0.6 for one by itself, the more of them the longer;
+//     64 x 64:   0.45 for two that share a compute unit, 0.3 for one by itself;
+// with the widened codes of a 32-bit result 1.9, 0.6 to 1.2, 0.66 and 0.45.  A split writes and reads its sums at 4.4 TB/s and costs a
+// launch.  (1024 x 1024 x 4096 into bf16: 128 x 128 in 1, 2, 4, 8 parts 23.1, 19.4, 19.1, 29.0; 64 x 64 in 1, 2, 4 parts 14.1, 18.6, 20.0.)
 Plan plan_of(int64_t M, int64_t N, int64_t K, bool exact, int num_cu) {
-    Plan best = {M <= ICQ_FEW_ROWS, ICQ_TILES_SMALL, 1};
+    Plan best = {icq_product_few_usable(M, N, num_cu), ICQ_TILES_SMALL, 1};
     if (best.few) {
         best.splits = icq_product_few_splits(N, K, num_cu);
         return best;
     }
     const int64_t kb = (K + 127) / 128;
     double least = -1.0;
-    for (int wide = exact ? 0 : 1; wide >= 0; --wide) {
-        const int64_t T = wide ? 256 : 128, tiles = ((M + T - 1) / T) * ((N + T - 1) / T);
+    for (int64_t T = exact ? 128 : 256; T >= 64; T /= 2) {
+        const int64_t tiles = ((M + T - 1) / T) * ((N + T - 1) / T);
         for (int splits = 1; splits <= 16 && (splits == 1 || kb >= 4 * splits); splits *= 2) {
-            const int64_t blocks = tiles * splits, steps = (kb + splits - 1) / splits;
-            const bool deep = !wide && blocks <= num_cu;
-            double us = steps;
-            if (wide) us *= 1.8 * ((blocks + num_cu - 1) / num_cu);
-            else if (deep) us *= exact ? 0.6 + 0.6 * blocks / num_cu : 0.5 + 0.1 * blocks / num_cu;
-            else us *= (exact ? 1.9 : 1.2) * ((blocks + 2 * num_cu - 1) / (2 * num_cu));
+            const int64_t blocks = tiles * splits, steps = (kb + splits - 1) / splits, rounds = blocks / (2 * num_cu), left = blocks % (2 * num_cu);
+            const bool alone = blocks <= num_cu;
+            // what a step of the last round adds: a pair's, a single tile's, nothing
+            const auto last = [&](double pair, double one) { return left > num_cu ? pair : left > 0 ? one : 0.0; };
+            const double share = (double)left / num_cu;
+            double us;
+            if (T == 256) us = 1.8 * (blocks / num_cu) + (blocks % num_cu > 0 ? 1.2 + 0.6 * (blocks % num_cu) / num_cu : 0.0);
+            else if (T == 128) us = exact ? 1.9 * rounds + last(1.9, 0.6 + 0.6 * share) : 1.2 * rounds + last(1.2, 0.5 + 0.1 * share);
+            else us = exact ? 0.66 * rounds + last(0.66, 0.45) : 0.45 * rounds + last(0.45, 0.3);
+            us *= steps;
             if (splits > 1) us += 2.5 + (double)splits * M * N * 8 / 4.4e6;
             if (least < 0.0 || us < least) {
                 least = us;
-                best.tiles = wide ? ICQ_TILES_WIDE : deep ? ICQ_TILES_DEEP : ICQ_TILES_SMALL;
+                best.tiles = T == 256 ? ICQ_TILES_WIDE : T == 64 ? ICQ_TILES_LITTLE : alone ? ICQ_TILES_DEEP : ICQ_TILES_SMALL;
                 best.splits = splits;
             }
         }
@@ -79,7 +86,7 @@ Plan plan_of(int64_t M, int64_t N, int64_t K, bool exact, int num_cu) {
 
 bool extents_ok(int64_t M, int64_t N, int64_t K) {
     return M >= 0 && N >= 0 && K >= 0 && M <= ICQ_MAX_EXTENT && N <= ICQ_MAX_EXTENT && K <= ICQ_MAX_EXTENT &&
-           ((M + 127) / 128) * ((N + 127) / 128) <= 0x7fffffff;
+           ((M + 63) / 64) * ((N + 63) / 64) <= 0x7fffffff;
 }
 
 }  // namespace

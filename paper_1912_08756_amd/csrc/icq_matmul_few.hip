@@ -123,13 +123,12 @@ __global__ __launch_bounds__(64 * WAVES) void product_few_kernel(Product p, int 
 
 template <int FA, int FB, bool ROWS, bool EXACT>
 int launch(const Product &p, int num_cu, int out_type, hipStream_t s) {
-    // rows of b per block (also icq_product_few_splits): as many as the registers hold beside the next block's operands, where that still fills the chip
     auto go = [&](auto kernel, int nt) {
         hipLaunchKernelGGL(kernel, dim3((uint32_t)((p.N + 16 * nt - 1) / (16 * nt)), (uint32_t)p.splits), dim3(64 * WAVES), 0, s, p, out_type);
     };
-    const int64_t fill = 16 * (int64_t)num_cu;
-    if (p.M <= 16) p.N >= 4 * fill ? go(product_few_kernel<FA, FB, ROWS, EXACT, 1, 4>, 4) : go(product_few_kernel<FA, FB, ROWS, EXACT, 1, 1>, 1);
-    else p.N >= 2 * fill ? go(product_few_kernel<FA, FB, ROWS, EXACT, 2, 2>, 2) : go(product_few_kernel<FA, FB, ROWS, EXACT, 2, 1>, 1);
+    if (p.M > 16) go(product_few_kernel<FA, FB, ROWS, EXACT, 2, 1>, 1);
+    else if (p.N >= 64 * (int64_t)num_cu) go(product_few_kernel<FA, FB, ROWS, EXACT, 1, 4>, 4);     // (a's rows read a quarter as often)
+    else go(product_few_kernel<FA, FB, ROWS, EXACT, 1, 1>, 1);
     return icq_check_launch();
 }
 
@@ -140,6 +139,10 @@ int launch_formats(const Product &p, int num_cu, int fa, int fb, int out_type, h
 }
 
 }  // namespace
+
+// Up to 16 rows; up to 32 where b has 16 rows for a compute unit or fewer (32 x 4096 x 4096: 10.5 us, in tiles 13; 32 x 16384 x 4096: 24,
+// in tiles 14; 16 x 16384 x 4096: 14.4 here).
+bool icq_product_few_usable(int64_t M, int64_t N, int num_cu) { return M <= 16 || (M <= 32 && N <= 16 * (int64_t)num_cu); }
 
 // Parts of the contraction: where the rows of b leave more than half of the chip idle, as long as a wavefront keeps four steps.
 int icq_product_few_splits(int64_t N, int64_t K, int num_cu) {

@@ -1,4 +1,5 @@
-// Products of 8-bit matrices with block scales: tiles of 256 x 256 (eight wavefronts of 128 x 64) or 128 x 128 (four of 64 x 64).
+// Products of 8-bit matrices with block scales: tiles of 256 x 256 (eight wavefronts of 128 x 64), 128 x 128 (four of 64 x 64)
+// or 64 x 64 (four of 32 x 32).
 //
 // The operands' tiles of one scale block go from memory straight into the LDS, two stages deep; a row's eight 16-byte pieces are
 // permuted by its number, by the choice of each lane's address, so that 16 rows' pieces fall on all 64 banks.
@@ -12,14 +13,16 @@ namespace {
 // Rows and columns of a wavefront's part in units of 32, wavefronts along m and n, stages in the LDS.
 template <int NI_, int NJ_, int WM_, int WN_, int DEPTH_>
 struct Shape {
-    static constexpr int NI = NI_, NJ = NJ_, WM = WM_, WN = WN_, DEPTH = DEPTH_, THREADS = 64 * WM * WN, T = 32 * NI * WM;
+    static constexpr int NI = NI_, NJ = NJ_, WM = WM_, WN = WN_, DEPTH = DEPTH_, WAVES = WM * WN, THREADS = 64 * WAVES, T = 32 * NI * WM;
+    static constexpr int PARTS = T / (8 * WAVES), LOADS = 2 * PARTS;          // of a wavefront for a stage: eight rows of each operand a part
     static constexpr int STAGE = 2 * T * 128;                                 // bytes of a stage
     static constexpr int LDS_BYTES = DEPTH * STAGE + 3 * 8 * T * 4;
-    static_assert(32 * NJ * WN == T && THREADS == 2 * T && NJ == 2 && DEPTH * STAGE / (WM * WN) >= 32 * 68 * 4, "square tiles, two threads a row; a stage's four parts over two columns twice");
+    static_assert(32 * NJ * WN == T && THREADS >= 2 * T && PARTS == 2 * NJ && DEPTH * STAGE / WAVES >= 32 * (32 * NJ + 4) * 4, "square tiles, a thread for every row of a stage; a stage's parts over a wavefront's columns twice; results fit the stages");
 };
 typedef Shape<4, 2, 2, 4, 2> Wide;
 typedef Shape<2, 2, 2, 2, 2> Small;    // two blocks share a compute unit
 typedef Shape<2, 2, 2, 2, 4> Deep;     // one has it to itself
+typedef Shape<1, 1, 2, 2, 4> Little;   // 64 x 64: two blocks a compute unit
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
@@ -61,19 +64,19 @@ __device__ __forceinline__ void load_to_lds(const i32x4 &base, uint32_t off, int
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(off), "s"(base), "s"(by) : "memory");
 }
 
-// 32 rows and 64 columns of the result from a wavefront's accumulators, whole rows at a time: in the accumulators a lane has four
+// 32 rows and 32 NJ columns of the result from a wavefront's accumulators, whole rows at a time: in the accumulators a lane has four
 // neighbours of one row and the lanes 32 rows, whose stores would be 16 bytes here and there.
-template <int TYPE>
-__device__ __forceinline__ void store_rows(uint8_t *turn, const f32x16 (&acc)[2], void *out, int64_t ldo, int64_t M, int64_t N, int64_t m0, int64_t n0,
+template <int TYPE, int NJ>
+__device__ __forceinline__ void store_rows(uint8_t *turn, const f32x16 (&acc)[NJ], void *out, int64_t ldo, int64_t M, int64_t N, int64_t m0, int64_t n0,
                                            int lane) {
     typedef IcqElem<TYPE> E;
     typedef typename E::raw raw;
-    constexpr int PER = E::PER, STRIDE = 64 + PER;                            // (16 bytes more than a row: other banks)
+    constexpr int PER = E::PER, WIDTH = 32 * NJ, STRIDE = WIDTH + PER;                            // (16 bytes more than a row: other banks)
     const int at = lane & 31, half = lane >> 5;
     raw *mine = reinterpret_cast<raw *>(turn);
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < NJ; ++j)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             raw *to = mine + at * STRIDE + j * 32 + 8 * g + 4 * half;
@@ -83,7 +86,7 @@ __device__ __forceinline__ void store_rows(uint8_t *turn, const f32x16 (&acc)[2]
         }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    constexpr int LANES = 64 / PER, ROWS_AT_ONCE = 64 / LANES;
+    constexpr int LANES = WIDTH / PER, ROWS_AT_ONCE = 64 / LANES;
     const int c = lane % LANES * PER;
     raw *to = static_cast<raw *>(out) + (m0 + lane / LANES) * ldo + n0 + c;
     const int left = (int)min((int64_t)PER, N - n0 - c), rows = (int)min((int64_t)32, M - m0);
@@ -108,7 +111,9 @@ __device__ __forceinline__ void load_word_to_lds(const i32x4 &base, uint32_t off
 
 template <typename S, int FA, int FB, bool ROWS, int MODE>
 __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product p, int tiles_m, int tiles_n, int out_type) {
-    constexpr int T = S::T, NI = S::NI, NJ = S::NJ, DEPTH = S::DEPTH, WAVES = S::THREADS / 64, LOADS = 8;        // of a wavefront for a stage
+    constexpr int T = S::T, NI = S::NI, NJ = S::NJ, DEPTH = S::DEPTH, WAVES = S::WAVES, PARTS = S::PARTS, LOADS = S::LOADS;
+    // loads under way that the barrier need not wait for: those of the stages after the next
+    constexpr int LATER = (DEPTH - 2) * LOADS - (NI == 1 ? LOADS / 2 : 0);
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
     float *s_scales = reinterpret_cast<float *>(smem + DEPTH * S::STAGE);     // [3][four blocks along K][a: T, b: T]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -123,17 +128,17 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product p, int t
 
     // this lane's place in the tile loads: instruction u of a wavefront brings rows 8 (WAVES u + wave) .. + 7;
     // row r's piece c sits at place c ^ (r / 2 % 8)
-    uint32_t off_a[4], off_b[4];
+    uint32_t off_a[PARTS], off_b[PARTS];
     const int piece = (lane & 7) ^ ((4 * wave + (lane >> 4)) & 7);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < PARTS; ++u) {
         const int r = 8 * (WAVES * u + wave) + (lane >> 3);
         const int64_t ra = min((int64_t)r, p.M - 1 - m0), rb = min((int64_t)r, p.N - 1 - n0);
         off_a[u] = (uint32_t)(ra * p.lda) + piece * 16;
         off_b[u] = (uint32_t)(rb * p.ldb) + piece * 16;
     }
     const i32x4 rsrc_a = bytes_from(p.a + m0 * p.lda), rsrc_b = bytes_from(p.b + n0 * p.ldb);
-    auto load_part = [&](int kb, int buf, int u, uint32_t back) {                // a quarter of a stage
+    auto load_part = [&](int kb, int buf, int u, uint32_t back) {
         const uint32_t to = buf * S::STAGE + wave * 1024 + u * WAVES * 1024;
         load_to_lds(rsrc_a, off_a[u] - back, kb * 128, to);
         load_to_lds(rsrc_b, off_b[u] - back, kb * 128, to + T * 128);
@@ -141,7 +146,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product p, int t
     // the last block's bytes from K on become zero: thread t has row t of the stage (a's rows, then b's)
     auto clear_beyond = [&](int buf) {
         uint8_t *row = smem + buf * S::STAGE + tid * 128;
-        for (int c = ragged >> 4; c < 8; ++c) {
+        for (int c = ragged >> 4; c < 8 && tid < 2 * T; ++c) {
             uint4 *w = reinterpret_cast<uint4 *>(row + ((c ^ (tid >> 1 & 7)) << 4));
             *w = c * 16 < ragged ? first_bytes(*w, ragged & 15) : make_uint4(0, 0, 0, 0);
         }
@@ -154,7 +159,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product p, int t
         for (int c = 0; c < 2; ++c) place[h][c] = (4 * h + 2 * half + c) ^ (at >> 1 & 7);
     // thread t brings the scale of row t of the stage (a's rows, then b's)
     const float *scale_row = tid < T ? p.sa + min(m0 + tid, p.M - 1) * p.kb
-                                     : p.sb + (ROWS ? min(n0 + tid - T, p.N - 1) : min((n0 >> 7) + (tid & 1), (p.N - 1) >> 7)) * p.kb;
+                                     : p.sb + (ROWS ? min(n0 + tid % T, p.N - 1) : min((n0 >> 7) + (tid & 1), (p.N - 1) >> 7)) * p.kb;
     // ... of blocks kb .. kb + 3, as far as there are any
     struct Four { float v[4]; };
     auto read_scales = [&](int kb) {
@@ -171,10 +176,11 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product p, int t
     };
     // the same straight into the LDS, a block along K at a time: loads of the compiler's own would have to be waited for with all others,
     // and four stages are to stay under way (two are not: at the barrier nothing is)
-    const i32x4 rsrc_scale = bytes_from(wave < WAVES / 2 ? p.sa + m0 * p.kb : p.sb + (ROWS ? n0 : n0 >> 7) * p.kb);
+    const i32x4 rsrc_scale = bytes_from(wave < T / 64 ? p.sa + m0 * p.kb : p.sb + (ROWS ? n0 : n0 >> 7) * p.kb);
     const uint32_t off_scale = (uint32_t)((tid < T ? min((int64_t)tid, p.M - 1 - m0)
-                                                   : ROWS ? min((int64_t)(tid - T), p.N - 1 - n0) : min((int64_t)(tid & 1), ((p.N - 1) >> 7) - (n0 >> 7))) * p.kb * 4);
+                                                   : ROWS ? min((int64_t)(tid % T), p.N - 1 - n0) : min((int64_t)(tid & 1), ((p.N - 1) >> 7) - (n0 >> 7))) * p.kb * 4);
     auto scales_to_lds = [&](int third, int kb) {
+        if (wave >= 2 * T / 64) return;
 #pragma unroll
         for (int k = 0; k < 4; ++k)
             load_word_to_lds(rsrc_scale, off_scale, min(kb + k, p.kb - 1) * 4, DEPTH * S::STAGE + ((third * 4 + k) * 2 * T + wave * 64) * 4);
@@ -237,7 +243,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product p, int t
     int block = 0;
     if (k0 < k1) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) load_part(k0, 0, u, k0 == whole ? beyond : 0);
+        for (int u = 0; u < PARTS; ++u) load_part(k0, 0, u, k0 == whole ? beyond : 0);
         if constexpr (DEPTH > 2) scales_to_lds(0, k0);
         else write_scales(0, read_scales(k0));
     }
@@ -247,7 +253,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product p, int t
         for (int d = 1; d < DEPTH; ++d) {
             back = min(k0 + d, last) == whole ? beyond : 0;
 #pragma unroll
-            for (int u = 0; u < (d == DEPTH - 1 ? 2 : 4); ++u) load_part(min(k0 + d, last), d, u, back);
+            for (int u = 0; u < (d == DEPTH - 1 ? PARTS / 2 : PARTS); ++u) load_part(min(k0 + d, last), d, u, back);
         }
         __builtin_amdgcn_s_waitcnt(loads_left((DEPTH - 2) * LOADS + LOADS / 2));
     } else {
@@ -282,14 +288,14 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product p, int t
                     if (i < NI - 1) {
                         read_a(i + 1, buf, sc);
                     } else {
-                        __builtin_amdgcn_s_waitcnt(loads_left((DEPTH - 2) * LOADS));      // the next stage is here, later ones may not be
+                        __builtin_amdgcn_s_waitcnt(loads_left(LATER));                    // the next stage is here, later ones may not be
                         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup", "local");
                         __builtin_amdgcn_s_barrier();
                     }
 #pragma unroll
                     for (int j = 0; j < NJ; ++j) {
                         // a stage's requests are spread over four parts of the multiplication: all at once they hold up the wavefront
-                        if (i == 0) load_part(min(kb + DEPTH - 1, last), last_buf, 2 + j, back);
+                        if (i == 0) load_part(min(kb + DEPTH - 1, last), last_buf, NJ + j, back);
                         if (i == NI - 1) {
                             back = min(kb + DEPTH, last) == whole ? beyond : 0;
                             load_part(min(kb + DEPTH, last), buf, j, back);
@@ -327,10 +333,10 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product p, int t
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
         const int64_t m = m0 + wm + i * 32, n = n0 + wn;
-        if (p.splits > 1) store_rows<ICQ_F32>(turn, acc[i], p.part + (int64_t)blockIdx.y * p.M * p.N, p.N, p.M, p.N, m, n, lane);
-        else if (MODE == EXACT) store_rows<ICQ_F32>(turn, acc[i], p.out, p.ldo, p.M, p.N, m, n, lane);
-        else if (out_type == ICQ_BF16) store_rows<ICQ_BF16>(turn, acc[i], p.out, p.ldo, p.M, p.N, m, n, lane);
-        else store_rows<ICQ_F16>(turn, acc[i], p.out, p.ldo, p.M, p.N, m, n, lane);
+        if (p.splits > 1) store_rows<ICQ_F32, NJ>(turn, acc[i], p.part + (int64_t)blockIdx.y * p.M * p.N, p.N, p.M, p.N, m, n, lane);
+        else if (MODE == EXACT) store_rows<ICQ_F32, NJ>(turn, acc[i], p.out, p.ldo, p.M, p.N, m, n, lane);
+        else if (out_type == ICQ_BF16) store_rows<ICQ_BF16, NJ>(turn, acc[i], p.out, p.ldo, p.M, p.N, m, n, lane);
+        else store_rows<ICQ_F16, NJ>(turn, acc[i], p.out, p.ldo, p.M, p.N, m, n, lane);
     }
 }
 
@@ -344,7 +350,7 @@ int launch(const Product &p, bool pow2, int out_type, hipStream_t s) {
         return icq_check_launch();
     };
     if (out_type == ICQ_F32) {
-        if constexpr (S::NI == 2) return go(product_kernel<S, FA, FB, ROWS, EXACT>);
+        if constexpr (S::T <= 128) return go(product_kernel<S, FA, FB, ROWS, EXACT>);
         return ICQ_ERR_ARG;                                                   // (not asked for: widened fragments beside 128 accumulators do not fit the registers)
     }
     if (pow2) return go(product_kernel<S, FA, FB, ROWS, FAST_POW2>);
@@ -363,5 +369,6 @@ int launch_formats(const Product &p, int fa, int fb, bool rows, bool pow2, int o
 
 int icq_launch_product_tiles(const Product &p, icq_tiles tiles, int fa, int fb, bool rows, bool pow2, int out_type, hipStream_t s) {
     if (tiles == ICQ_TILES_WIDE) return launch_formats<Wide>(p, fa, fb, rows, pow2, out_type, s);
+    if (tiles == ICQ_TILES_LITTLE) return launch_formats<Little>(p, fa, fb, rows, pow2, out_type, s);
     return tiles == ICQ_TILES_DEEP ? launch_formats<Deep>(p, fa, fb, rows, pow2, out_type, s) : launch_formats<Small>(p, fa, fb, rows, pow2, out_type, s);
 }
