@@ -49,39 +49,58 @@ struct __attribute__((aligned(32))) Part {
 
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// Over the wavefront, in every lane: rotations within 16 lanes, then the four groups of 16.
+template <int BY>
+__device__ __forceinline__ float rotated(float v) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x120 + BY, 0xf, 0xf, true)); }
+
+__device__ __forceinline__ float wave_sum(float v) {
+    v += rotated<8>(v);
+    v += rotated<4>(v);
+    v += rotated<2>(v);
+    v += rotated<1>(v);
+    v += __shfl_xor(v, 16, 64);
+    return v + __shfl_xor(v, 32, 64);
+}
+
+__device__ __forceinline__ float wave_max(float v) {                  // NaN does not count
+    v = fmaxf(v, rotated<8>(v));
+    v = fmaxf(v, rotated<4>(v));
+    v = fmaxf(v, rotated<2>(v));
+    v = fmaxf(v, rotated<1>(v));
+    v = fmaxf(v, __shfl_xor(v, 16, 64));
+    return fmaxf(v, __shfl_xor(v, 32, 64));
+}
+
 // Sums over the block, in a fixed order, of K values at once.
 template <int N, int K>
 __device__ __forceinline__ void block_sums(float (&v)[K], float *red) {
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1)
-#pragma unroll
-        for (int i = 0; i < K; ++i) v[i] += __shfl_xor(v[i], d, 64);
+    for (int i = 0; i < K; ++i) v[i] = wave_sum(v[i]);
     __syncthreads();
     if ((threadIdx.x & 63) == 0)
 #pragma unroll
-        for (int i = 0; i < K; ++i) red[(threadIdx.x >> 6) * K + i] = v[i];
+        for (int i = 0; i < K; ++i) red[i * (N / 64) + (threadIdx.x >> 6)] = v[i];
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < K; ++i) {
-        v[i] = red[i];
-        for (int w = 1; w < N / 64; ++w) v[i] += red[w * K + i];
+        v[i] = red[i * (N / 64)];
+#pragma unroll
+        for (int w = 1; w < N / 64; ++w) v[i] += red[i * (N / 64) + w];
     }
 }
 
 // The largest of `m` (NaN does not count) and the sum of `v`.
 template <int N>
 __device__ __forceinline__ void block_max_and_sum(float &m, float &v, float *red) {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) {
-        m = fmaxf(m, __shfl_xor(m, d, 64));
-        v += __shfl_xor(v, d, 64);
-    }
+    m = wave_max(m);
+    v = wave_sum(v);
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) { red[(threadIdx.x >> 6) * 2] = m; red[(threadIdx.x >> 6) * 2 + 1] = v; }
+    if ((threadIdx.x & 63) == 0) { red[threadIdx.x >> 6] = m; red[N / 64 + (threadIdx.x >> 6)] = v; }
     __syncthreads();
     m = red[0];
-    v = red[1];
-    for (int w = 1; w < N / 64; ++w) { m = fmaxf(m, red[w * 2]); v += red[w * 2 + 1]; }
+    v = red[N / 64];
+#pragma unroll
+    for (int w = 1; w < N / 64; ++w) { m = fmaxf(m, red[w]); v += red[N / 64 + w]; }
 }
 
 // The row's list in LDS.  id[j] = ICQ_PAD_ID where position j holds no entry of its own.
@@ -91,7 +110,7 @@ struct List {
     float p[CAP], log_p[CAP];
     float x[CAP];                  // the student's logit
     uint32_t slot_id[2 * CAP];     // the ids, by hash
-    float red[40];
+    __attribute__((aligned(16))) float red[40];
     uint32_t twice;
 };
 
@@ -102,8 +121,13 @@ __device__ int load_list(const Distill &a, int64_t row, const typename IcqElem<T
     const int tid = threadIdx.x;
     for (int i = tid; i < a.slots; i += n) l.slot_id[i] = ICQ_PAD_ID;
     if (tid == 0) l.twice = 0;
-    float top = -INFINITY, count = 0.0f, ref = 0.0f, log_z = 0.0f;
-    for (int j = tid; j < a.topk; j += n) {
+    float top = -INFINITY, count = 0.0f, ref = a.teacher_lse ? a.teacher_lse[row] : 0.0f, log_z = 0.0f;
+    typename IcqElem<TYPE>::raw logit[PLACES];         // (not waited for before they are needed)
+#pragma unroll
+    for (int u = 0; u < PLACES; ++u) {
+        const int j = u * n + tid;
+        logit[u] = IcqElem<TYPE>::put(0.0f);
+        if (j >= a.topk) continue;
         const uint32_t id = a.ids[row * a.topk + j];
         const float z = a.teacher_scale * a.values[row * a.topk + j];
         const bool entry = (int64_t)id < a.V && !(z == -INFINITY);
@@ -112,13 +136,11 @@ __device__ int load_list(const Distill &a, int64_t row, const typename IcqElem<T
         if (entry) {
             top = fmaxf(top, z);
             count += 1.0f;
-            if (in(id)) l.x[j] = IcqElem<TYPE>::get(x[id]);
+            if (in(id)) logit[u] = x[id];
         }
     }
     block_max_and_sum<N>(top, count, l.red);           // (its barriers also cover the table)
-    if (a.teacher_lse) {
-        ref = a.teacher_lse[row];
-    } else if (top > -INFINITY) {
+    if (!a.teacher_lse && top > -INFINITY) {
         ref = top;
         float s[1] = {0.0f};
         for (int j = tid; j < a.topk; j += n)
@@ -141,6 +163,9 @@ __device__ int load_list(const Distill &a, int64_t row, const typename IcqElem<T
             at = (at + 1) & (uint32_t)(a.slots - 1);
         }
     }
+#pragma unroll
+    for (int u = 0; u < PLACES; ++u)
+        if (u * n + tid < a.topk) l.x[u * n + tid] = IcqElem<TYPE>::get(logit[u]);
     sum_p = 0.0f;
     if (a.teacher_lse) {                               // (only then is the sum of any consequence)
         block_sums<N>(sum, l.red);
@@ -471,6 +496,7 @@ __global__ __launch_bounds__(T) void distill_backward_kernel(Distill a) {
     for (int u = 0; u < U; ++u)
         if (c.b0 + u * T + tid < c.b1) w[u] = body[c.b0 + u * T + tid];
     float sum_p, listed;
+    const float g0 = a.grad_loss ? a.grad_loss[row] : 1.0f;
     // (listed items of other slices may have their gradients already, where those take the logits' place)
     const auto in = [&](uint32_t id) { return in_slice(s, c, id, PER); };
     const int entries = load_list<TYPE, CAP, T>(a, row, x, l, sum_p, in);
@@ -486,7 +512,7 @@ __global__ __launch_bounds__(T) void distill_backward_kernel(Distill a) {
         for (int64_t b = c.b0 + tid; b < c.b1; b += T) body_out[b] = make_uint4(0, 0, 0, 0);
         return;
     }
-    const float g = (a.grad_loss ? a.grad_loss[row] : 1.0f) * a.scale, q0 = 1.0f / st.y, f = q0 * st.z * g;
+    const float g = g0 * a.scale, q0 = 1.0f / st.y, f = q0 * st.z * g;
     // the listed items of this slice
     float mine[PLACES];
     uint32_t here[PLACES];
@@ -550,6 +576,7 @@ __global__ __launch_bounds__(N, 4) void distill_row_kernel(Distill a) {
     const bool single = tid < s.head + s.tail;         // (fewer than 16 of them)
     const int64_t v1 = tid < s.head ? tid : tid + s.body * PER;
     const float y1 = single ? E::get(x[v1]) : 0.0f;
+    const float g0 = a.grad_loss ? a.grad_loss[row] : 1.0f;
     float sum_p;
     const int entries = load_list<TYPE, CAP, N>(a, row, x, l, sum_p, [](uint32_t) { return true; });
     Run run = {-FLT_MAX, 0.0f, 0.0f};
@@ -562,7 +589,7 @@ __global__ __launch_bounds__(N, 4) void distill_row_kernel(Distill a) {
     listed_sum<CAP, N>(a, l, run.m, v, [](uint32_t) { return true; });
     const float4 st = finish_row<CAP, N>(a, row, l, entries, sum_p, run, v[0], true);
     const bool counts = st.w != 0.0f;
-    const float g = (a.grad_loss ? a.grad_loss[row] : 1.0f) * a.scale, q0 = 1.0f / st.y, f = q0 * st.z * g;
+    const float g = g0 * a.scale, q0 = 1.0f / st.y, f = q0 * st.z * g;
     float mine[PLACES];
     uint32_t here[PLACES];
 #pragma unroll
