@@ -140,21 +140,27 @@ __device__ int load_list(const Distill &a, int64_t row, const typename IcqElem<T
         }
     }
     block_max_and_sum<N>(top, count, l.red);           // (its barriers also cover the table)
-    if (!a.teacher_lse && top > -INFINITY) {
-        ref = top;
+    const bool own_sum = !a.teacher_lse && top > -INFINITY;
+    float part = 1.0f;
+    if (own_sum) {                                     // p as a share of the sum: they add up to one whatever the scores' size
         float s[1] = {0.0f};
         for (int j = tid; j < a.topk; j += n)
-            if (l.id[j] != ICQ_PAD_ID) s[0] += expf(l.p[j] - top);
+            if (l.id[j] != ICQ_PAD_ID) {
+                l.log_p[j] = l.p[j] - top;
+                s[0] += l.p[j] = expf(l.log_p[j]);
+            }
         block_sums<N>(s, l.red);
         log_z = logf(s[0]);
+        part = 1.0f / s[0];
     }
     float sum[1] = {0.0f};
     for (int j = tid; j < a.topk; j += n) {
         const uint32_t id = l.id[j];
         if (id == ICQ_PAD_ID) { l.p[j] = 0.0f; continue; }
-        const float lp = (l.p[j] - ref) - log_z;
+        const float lp = own_sum ? l.log_p[j] - log_z : l.p[j] - ref;
+        l.p[j] = own_sum ? l.p[j] * part : expf(lp);
         l.log_p[j] = lp;
-        sum[0] += l.p[j] = expf(lp);
+        sum[0] += l.p[j];
         uint32_t at = (id * 0x9E3779B1u) >> 16 & (uint32_t)(a.slots - 1);
         for (;;) {                                     // slots >= 2 * topk: an empty one is found
             const uint32_t was = atomicCAS(&l.slot_id[at], ICQ_PAD_ID, id);
