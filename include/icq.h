@@ -432,8 +432,8 @@ int icq_block_quantize(const void *x, int x_type, int64_t rows, int64_t cols, in
  * 2^-13 of the largest are lost (1.4e-5 of the result in the 2-norm for normal
  * values, below the result's rounding), a 32-bit out takes them all.  scaling =
  * ICQ_SCALES_POW2 promises that every scale is a power of two (as
- * icq_block_quantize makes them): the matrix instructions then apply them; of
- * other scales only the exponent would count.
+ * icq_block_quantize makes them): the matrix instructions of a 16-bit out then
+ * apply them, and of other scales only the exponent would count.
  * workspace: icq_block_matmul_workspace_bytes(M, N, K) bytes (may be 0: NULL),
  * 256-byte aligned.
  * With W held in 128 x 128 blocks as codes and codes_t, and G the gradient of

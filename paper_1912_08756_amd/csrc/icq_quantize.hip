@@ -7,9 +7,10 @@
 // the quotients and the product are single-precision operations rounded once each.  Infinities and NaN do not count for a and
 // become what the format has for them (e4m3 has no infinity: NaN).
 //
-// Both kernels read every value once and are bound by memory: rows alone need no more than the 16 lanes that hold a block
-// agreeing on its largest value; columns need a 128 x 128 tile in registers, whose codes turn round in the LDS so that
-// either output is written in whole 128-byte pieces.
+// Both kernels read every value once and are bound by memory (a copy of 1 GiB runs at 5.17 TB/s).  Rows alone need no more than the 16
+// lanes that hold a block agreeing on its largest value: 8192 x 8192 bf16 42 us, 4.8 TB/s; f32 57 us, 5.8 TB/s.  Columns need
+// a 128 x 128 tile in registers, whose codes turn round in the LDS so that either output is written in whole 128-byte pieces:
+// 8192 x 16000 bf16 both ways 117 us, 4.6 TB/s; 10007 x 4096 f32 in 128 x 128 blocks both ways 49.5 us, 5.0 TB/s.
 #include "icq_types.h"
 
 namespace {
@@ -163,7 +164,8 @@ __device__ __forceinline__ void values8(const Eight<TYPE> &v, float *x) {
 }
 
 // A 128 x 128 tile per block; thread (g, h) holds rows 4 h .. 4 h + 3 of columns 8 g .. 8 g + 7.
-// TILE: one scale for the whole tile, else one per row and column of it, each worked out by one thread.
+// TILE: one scale for the whole tile, else one per row and column of it, each worked out by one thread (by all that need it, with words
+// compared one by one: 139 us at 8192 x 16000 against 118; 256 threads of 8 x 8 values each: the same 118, small tiles slower).
 template <int TYPE, int FORMAT, bool TILE>
 __global__ __launch_bounds__(512) void quantize_tile_kernel(Quantize a) {
     constexpr int WORDS = Eight<TYPE>::WORDS;
