@@ -249,15 +249,22 @@ __device__ __forceinline__ void run_add(Run &a, const float *x, uint32_t listed,
         if (REST) a.r *= f;
         a.m = m;
     }
-    float s = 0.0f, l = 0.0f;
+    float s = 0.0f, e[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const float e = ex2((x[i] - m) * a2);
-        s += e;
-        if (REST) l += (listed >> i & 1u) ? 0.0f : e;
+        e[i] = ex2((x[i] - m) * a2);
+        s += e[i];
     }
     a.s += s;
-    if (REST) a.r += l;
+    if (REST) {
+        float l = s;
+        if (listed & ((1u << N) - 1u)) {               // (few groups: most take their whole sum)
+            l = 0.0f;
+#pragma unroll
+            for (int i = 0; i < N; ++i) l += (listed >> i & 1u) ? 0.0f : e[i];
+        }
+        a.r += l;
+    }
 }
 
 // The largest maximum of the block.
@@ -372,17 +379,18 @@ __device__ __forceinline__ void run_held(Run &run, const uint4 (&w)[NV], int hel
     }
 }
 
-// Sums over groups [b0, b1) of a row, in chunks that can be marked.
+// Sums over groups [first + done, to) of a row, in chunks that can be marked; the chunk from `first` on is marked already, so that the
+// loads behind the groups in registers do not wait for a marking of their own.
 template <int TYPE, bool REST, int CAP, int N>
-__device__ __forceinline__ void run_over(Run &run, const Distill &a, const List<CAP> &l, uint32_t *bits, const uint4 *body, int head, int64_t from,
-                                         int64_t to) {
+__device__ __forceinline__ void run_over(Run &run, const Distill &a, const List<CAP> &l, uint32_t *bits, const uint4 *body, int head, int64_t first,
+                                         int done, int64_t to) {
     typedef IcqElem<TYPE> E;
     constexpr int PER = E::PER, U = 4;
-    for (int64_t b0 = from; b0 < to; b0 += CHUNK / PER) {
+    for (int64_t b0 = first; b0 < to; b0 += CHUNK / PER, done = 0) {
         const int n = (int)(to - b0 < CHUNK / PER ? to - b0 : CHUNK / PER);
-        if (REST) mark<CAP, N>(a, l, bits, head + b0 * PER, (int64_t)n * PER);
+        if (REST && b0 > first) mark<CAP, N>(a, l, bits, head + b0 * PER, (int64_t)n * PER);
         const uint4 *at = body + b0;
-        for (int i = threadIdx.x; i < n; i += U * N) {
+        for (int i = done + (int)threadIdx.x; i < n; i += U * N) {
             uint4 w[U];
 #pragma unroll
             for (int u = 0; u < U; ++u)
@@ -411,8 +419,8 @@ __device__ __forceinline__ uint4 gradient_of(const uint4 &w, float m, float a2, 
 }
 
 // Sums of a row (splits == 1: and its loss) or of a slice of it.  REST: also those off the list.
-template <int TYPE, bool REST, int CAP>
-__global__ __launch_bounds__(T) void distill_forward_kernel(Distill a) {
+template <int TYPE, bool REST, int CAP, int N>
+__global__ __launch_bounds__(N) void distill_forward_kernel(Distill a) {
     typedef IcqElem<TYPE> E;
     constexpr int U = 8;
     __shared__ List<CAP> l;
@@ -428,25 +436,25 @@ __global__ __launch_bounds__(T) void distill_forward_kernel(Distill a) {
     uint4 w[U];                                        // on their way while the list is worked on
 #pragma unroll
     for (int u = 0; u < U; ++u)
-        if (c.b0 + u * T + tid < c.b1) w[u] = body[c.b0 + u * T + tid];
-    const int entries = load_list<TYPE, CAP, T>(a, row, x, l, sum_p, in);
+        if (c.b0 + u * N + tid < c.b1) w[u] = body[c.b0 + u * N + tid];
+    const int entries = load_list<TYPE, CAP, N>(a, row, x, l, sum_p, in);
     Run run = {-FLT_MAX, 0.0f, 0.0f};
-    for (int64_t i = c.e0 + tid; i < c.e1; i += T) {
+    for (int64_t i = c.e0 + tid; i < c.e1; i += N) {
         const int64_t v = i < s.head ? i : i + s.body * E::PER;
         const float y = E::get(x[v]);
         run_add<1, REST>(run, &y, REST && on_list(l, a.slots, (uint32_t)v) ? 1u : 0u, a.a2);
     }
-    const int64_t b1 = c.b0 + U * T < c.b1 ? c.b0 + U * T : c.b1;
-    if (REST) mark<CAP, T>(a, l, s_bits, s.head + c.b0 * E::PER, (b1 - c.b0) * E::PER);
-    run_held<TYPE, REST, T, U>(run, w, (int)(b1 - c.b0), s_bits, a.a2);
-    run_over<TYPE, REST, CAP, T>(run, a, l, s_bits, body, s.head, b1, c.b1);
-    run = block_run<T>(run, a.a2, l.red);
+    const int held = (int)(c.b1 - c.b0 < U * N ? c.b1 - c.b0 : U * N);
+    if (REST) mark<CAP, N>(a, l, s_bits, s.head + c.b0 * E::PER, c.b1 - c.b0 < CHUNK / E::PER ? (c.b1 - c.b0) * E::PER : CHUNK);
+    run_held<TYPE, REST, N, U>(run, w, held, s_bits, a.a2);
+    run_over<TYPE, REST, CAP, N>(run, a, l, s_bits, body, s.head, c.b0, held, c.b1);
+    run = block_run<N>(run, a.a2, l.red);
     float v[2];
-    listed_sum<CAP, T>(a, l, run.m, v, in);
+    listed_sum<CAP, N>(a, l, run.m, v, in);
     if (a.splits == 1) {
-        finish_row<CAP, T>(a, row, l, entries, sum_p, run, v[0], true);
+        finish_row<CAP, N>(a, row, l, entries, sum_p, run, v[0], true);
     } else {
-        block_sums<T>(v, l.red);
+        block_sums<N>(v, l.red);
         if (tid == 0) {
             const Part part = {run.m, run.s, run.r, v[0], v[1], {0.0f, 0.0f, 0.0f}};
             a.part[row * a.splits + k] = part;
@@ -589,9 +597,9 @@ __global__ __launch_bounds__(N, 4) void distill_row_kernel(Distill a) {
     const int entries = load_list<TYPE, CAP, N>(a, row, x, l, sum_p, [](uint32_t) { return true; });
     Run run = {-FLT_MAX, 0.0f, 0.0f};
     if (single) run_add<1, REST>(run, &y1, REST && on_list(l, a.slots, (uint32_t)v1) ? 1u : 0u, a.a2);
-    if (REST) mark<CAP, N>(a, l, s_bits, s.head, (int64_t)held * PER);
+    if (REST) mark<CAP, N>(a, l, s_bits, s.head, s.body < CHUNK / PER ? s.body * PER : CHUNK);
     run_held<TYPE, REST, N, NV>(run, w, held, s_bits, a.a2);
-    run_over<TYPE, REST, CAP, N>(run, a, l, s_bits, body, s.head, held, s.body);
+    run_over<TYPE, REST, CAP, N>(run, a, l, s_bits, body, s.head, 0, held, s.body);
     run = block_run<N>(run, a.a2, l.red);
     float v[2];
     listed_sum<CAP, N>(a, l, run.m, v, [](uint32_t) { return true; });
@@ -689,7 +697,11 @@ void launch_distill(const Distill &a, hipStream_t s) {
         else go(distill_row_kernel<TYPE, REST, CAP, 512, 16, true>, 512);
         return;
     }
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(distill_forward_kernel<TYPE, REST, CAP>), dim3((uint32_t)(a.R * a.splits)), dim3(T), 0, s, a);
+    const auto forward = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3((uint32_t)(a.R * a.splits)), dim3(threads), 0, s, a); };
+    // Whole rows of 256 KB and more by 512 threads (300 x 300000 f32: 74 us against 99 by 256, 1024 x 131072 bf16 53 and 55; shorter ones
+    // lose by it: 777 x 50021 f16 26.5 and 25.2, 8192 x 4096 f32 61 and 39).
+    if (a.splits == 1 && a.V * icq_type_bytes(TYPE) >= 262144) forward(distill_forward_kernel<TYPE, REST, CAP, 512>, 512);
+    else forward(distill_forward_kernel<TYPE, REST, CAP, T>, T);
     if (a.grad) launch_backward<TYPE, CAP>(a, a.splits > 1, s);
     else if (a.splits > 1) hipLaunchKernelGGL(HIP_KERNEL_NAME(distill_join_kernel<TYPE, CAP>), dim3((uint32_t)a.R), dim3(T), 0, s, a);
 }
