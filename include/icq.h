@@ -457,14 +457,16 @@ int icq_block_matmul(const uint8_t *a, int a_format, int64_t lda, const float *a
  *     loss[r] = sum_j p_j (log p_j - log q_j);
  *   teacher_lse [R]:  p_j = exp(z_j - teacher_lse[r]), the logsumexp of
  *     everything the teacher scored; what is left, p_r = max(0, 1 - sum_j p_j),
- *     is compared with the student's mass off the list, q_r:
+ *     is compared with the student's mass off the list, q_r, however small that is:
  *     loss[r] gains p_r (log p_r - log q_r)   (not if the list names all V items).
  *   grad[r][v] = grad_loss[r] * d loss[r] / d logits[r][v]
  *              = grad_loss[r] * scale * (q_v - p_v)      for listed items,
  *                grad_loss[r] * scale * c * q_v          for the others,
  *     c = 1, or 1 - p_r / q_r with teacher_lse; grad_loss NULL: 1.
  * A row without entries, or whose logits are all -inf, has loss 0 and gradient
- * 0.  A listed item of positive probability whose logit is -inf: loss +inf.
+ * 0.  The loss is +inf where a listed item of positive probability has a logit
+ * of -inf, and where p_r > 0 and the logits off the list are all -inf or the
+ * type's lowest finite value (masked places; their gradients are 0 then).
  * NaN, and logits of +inf, make the row's loss and gradient NaN.
  * icq_distill writes loss [R]; stats [R][4] fp32, 16-byte aligned, if not NULL
  * (what icq_distill_backward reads); and the gradient if grad is not NULL (in

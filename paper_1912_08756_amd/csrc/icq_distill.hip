@@ -5,9 +5,10 @@
 // with the sum of its probabilities).  p_j = exp(z_j - L), L = logsumexp of the list, or the caller's logsumexp over everything
 // the teacher scored; then the remaining mass p_r = max(0, 1 - sum p) faces the student's mass off the list, q_r.
 //     loss = sum_j p_j (log p_j - log q_j)  [+ p_r (log p_r - log q_r)]
-//     d loss / d x_v = scale (q_v - p_v) on the list, scale c q_v off it, c = 1 [1 - p_r / q_r].
-// Statistics and sums are held in 32 bits.  The mass off the list is summed directly (the listed items are marked bit by bit), not as
-// one minus the listed mass: a student that has learnt its list leaves little there.
+//     d loss / d x_v = scale (q_v - p_v) on the list, scale q_v [- scale p_r q_v / q_r] off it.
+// Statistics and sums are held in 32 bits.  The items off the list are summed by themselves, relative to a maximum of their own (the listed
+// ones are marked bit by bit and join from the list), not as one minus the listed mass: a student that has learnt its list leaves
+// little there, e^-100 and less under a large scale.  log q_r and q_v / q_r follow from that sum without q_r, which may be too small to hold.
 //
 // A row is a one-pass reduction (running maximum, sum rescaled when it moves) and one more pass for the gradient.  Loss and gradient of
 // many rows: a block per row, what the registers hold of it read once, the rest a second time.  Few rows are cut into slices whose
@@ -29,13 +30,14 @@ struct Distill {
     const void *x;
     int64_t R, V, ld;
     float scale, a2;               // a2 = scale * log2(e)
+    float lowest;                  // the type's lowest finite value: a mask, like -inf
     const uint32_t *ids;
     const float *values;
     int topk, slots;               // slots: size of the duplicate table, a power of two >= 2 * topk
     float teacher_scale;
     const float *teacher_lse;
     float *loss;
-    float4 *stats;                 // [R] maximum of x, sum of exp, c, 1 if the row counts
+    float4 *stats;                 // [R] maximum of x, sum of exp (0: the row does not count), base and factor of the off-list gradient
     const float *grad_loss;
     void *grad;
     int64_t ld_grad;
@@ -43,10 +45,15 @@ struct Distill {
     struct Part *part;             // [R][splits]
 };
 
+// Sums of a row or of a slice of it: maximum of x and the sum of exp(scale * (x - m)); the same of what is off the list.
+struct Sums {
+    float m, s, mr, r;
+};
+
 struct __attribute__((aligned(32))) Part {
-    float m, s, r;                 // maximum, sum, sum off the list
+    Sums sums;
     float t, p;                    // over the listed items of the slice: sum of p (x - m), sum of p
-    float unused[3];
+    float unused[2];
 };
 
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -226,62 +233,76 @@ __device__ __forceinline__ Span span_of(const void *row, int64_t V) {
     return s;
 }
 
-// Running maximum and sums of exp(scale * (x - maximum)).
+// Running maximum and sum of exp(scale * (x - maximum)).
 struct Run {
-    float m, s, r;                 // r: off the list
+    float m, s;
 };
 
 __device__ __forceinline__ void run_join(Run &a, const Run &b, float a2) {
-    const float m = fmaxf(a.m, b.m), fa = ex2((a.m - m) * a2), fb = ex2((b.m - m) * a2);
-    a.s = a.s * fa + b.s * fb;
-    a.r = a.r * fa + b.r * fb;
+    const float m = fmaxf(a.m, b.m);
+    a.s = a.s * ex2((a.m - m) * a2) + b.s * ex2((b.m - m) * a2);
     a.m = m;
 }
 
+// REST: but for the items that the low N bits of `listed` name.
 template <int N, bool REST>
-__device__ __forceinline__ void run_add(Run &a, const float *x, uint32_t listed, float a2) {
+__device__ __forceinline__ void run_add(Run &a, const float (&x)[N], uint32_t listed, float a2) {
+    float y[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) y[i] = x[i];
+    if (REST && (listed & ((1u << N) - 1u)))           // (few groups have any)
+#pragma unroll
+        for (int i = 0; i < N; ++i) y[i] = (listed >> i & 1u) ? -INFINITY : y[i];
     float m = a.m;
 #pragma unroll
-    for (int i = 0; i < N; ++i) m = fmaxf(m, x[i]);
+    for (int i = 0; i < N; ++i) m = fmaxf(m, y[i]);
     if (m > a.m) {
-        const float f = ex2((a.m - m) * a2);
-        a.s *= f;
-        if (REST) a.r *= f;
+        a.s *= ex2((a.m - m) * a2);
         a.m = m;
     }
-    float s = 0.0f, e[N];
+    float s = 0.0f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        e[i] = ex2((x[i] - m) * a2);
-        s += e[i];
-    }
+    for (int i = 0; i < N; ++i) s += ex2((y[i] - m) * a2);
     a.s += s;
-    if (REST) {
-        float l = s;
-        if (listed & ((1u << N) - 1u)) {               // (few groups: most take their whole sum)
-            l = 0.0f;
+}
+
+// The larger of two maxima each of the block.
+template <int N>
+__device__ __forceinline__ void block_max2(float &a, float &b, float *red) {
+    a = wave_max(a);
+    b = wave_max(b);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) { red[threadIdx.x >> 6] = a; red[N / 64 + (threadIdx.x >> 6)] = b; }
+    __syncthreads();
+    a = red[0];
+    b = red[N / 64];
 #pragma unroll
-            for (int i = 0; i < N; ++i) l += (listed >> i & 1u) ? 0.0f : e[i];
-        }
-        a.r += l;
+    for (int w = 1; w < N / 64; ++w) { a = fmaxf(a, red[w]); b = fmaxf(b, red[N / 64 + w]); }
+}
+
+// Block-wide, in a fixed order: the join of all threads' runs; REST: these are of what is off the list, and those listed items that `in`
+// takes join from the list.
+template <bool REST, int CAP, int N, typename In>
+__device__ __forceinline__ Sums block_run(const Run &a, const Distill &d, List<CAP> &l, In in) {
+    Sums b = {a.m, 0.0f, a.m, 0.0f};
+    if constexpr (!REST) {
+        float none = 0.0f;
+        block_max_and_sum<N>(b.m, none, l.red);
+        float v[1] = {a.s * ex2((a.m - b.m) * d.a2)};
+        block_sums<N>(v, l.red);
+        b.s = v[0];
+        b.mr = b.m;
+    } else {
+        for (int j = threadIdx.x; j < d.topk; j += N)
+            if (l.id[j] != ICQ_PAD_ID && in(l.id[j])) b.m = fmaxf(b.m, l.x[j]);
+        block_max2<N>(b.m, b.mr, l.red);
+        float v[2] = {a.s * ex2((a.m - b.mr) * d.a2), 0.0f};
+        for (int j = threadIdx.x; j < d.topk; j += N)
+            if (l.id[j] != ICQ_PAD_ID && in(l.id[j])) v[1] += ex2((l.x[j] - b.m) * d.a2);
+        block_sums<N>(v, l.red);
+        b.r = v[0];
+        b.s = v[0] * ex2((b.mr - b.m) * d.a2) + v[1];
     }
-}
-
-// The largest maximum of the block.
-template <int N>
-__device__ __forceinline__ float run_max(const Run &a, float *red) {
-    float m = a.m, none = 0.0f;
-    block_max_and_sum<N>(m, none, red);
-    return m;
-}
-
-// Block-wide: the join of all threads' runs, in a fixed order.
-template <int N>
-__device__ __forceinline__ Run block_run(const Run &a, float a2, float *red) {
-    const float m = run_max<N>(a, red), f = ex2((a.m - m) * a2);
-    float v[2] = {a.s * f, a.r * f};
-    block_sums<N>(v, red);
-    const Run b = {m, v[0], v[1]};
     return b;
 }
 
@@ -300,21 +321,28 @@ __device__ __forceinline__ void listed_sum(const Distill &a, const List<CAP> &l,
 
 // Loss and statistics of a row from its sums; listed: this thread's share of the sum of p (x - m).  All threads get the statistics.
 template <int CAP, int N>
-__device__ float4 finish_row(const Distill &a, int64_t row, List<CAP> &l, int entries, float sum_p, const Run &run, float listed, bool write) {
+__device__ float4 finish_row(const Distill &a, int64_t row, List<CAP> &l, int entries, float sum_p, const Sums &run, float listed, bool write) {
     const float log_s = logf(run.s);
     const bool counts = entries > 0 && !(run.s == 0.0f);
     const bool rest = a.teacher_lse && (int64_t)entries < a.V;
     const float p_r = rest ? fmaxf(0.0f, 1.0f - sum_p) : 0.0f;
+    // the sum off the list, zero where all of it is masked: it takes no gradient then (as it is, if that is NaN)
+    const float r = run.mr > a.lowest ? run.r : 0.0f * run.r;
     if (write) {                                       // (the same for the whole block)
         float sum[1] = {-a.scale * listed};
         for (int j = threadIdx.x; j < a.topk; j += N)
             if (l.id[j] != ICQ_PAD_ID && !(l.p[j] == 0.0f)) sum[0] += l.p[j] * (l.log_p[j] + log_s);
         block_sums<N>(sum, l.red);
-        if (p_r > 0.0f) sum[0] += p_r * (logf(p_r) - (logf(run.r) - log_s));
+        if (p_r > 0.0f) sum[0] += p_r * (logf(p_r) - (a.scale * (run.mr - run.m) + logf(r) - log_s));
         if (threadIdx.x == 0) a.loss[row] = counts ? sum[0] : 0.0f;
     }
-    // (nothing off the list: no item takes c)
-    const float4 st = make_float4(run.m, run.s, rest && run.r > 0.0f ? 1.0f - p_r * run.s / run.r : 1.0f, counts ? 1.0f : 0.0f);
+    // off the list q_v - p_r q_v / q_r = exp(scale (x_v - base)) factor
+    float base = run.m, factor = 1.0f / run.s;
+    if (a.teacher_lse) {
+        base = run.mr;
+        factor = r == 0.0f ? 0.0f : ex2((run.mr - run.m) * a.a2) / run.s - p_r / r;
+    }
+    const float4 st = make_float4(run.m, counts ? run.s : 0.0f, base, factor);
     if (write && a.stats && threadIdx.x == 0) a.stats[row] = st;
     return st;
 }
@@ -438,25 +466,25 @@ __global__ __launch_bounds__(N) void distill_forward_kernel(Distill a) {
     for (int u = 0; u < U; ++u)
         if (c.b0 + u * N + tid < c.b1) w[u] = body[c.b0 + u * N + tid];
     const int entries = load_list<TYPE, CAP, N>(a, row, x, l, sum_p, in);
-    Run run = {-FLT_MAX, 0.0f, 0.0f};
+    Run run = {-FLT_MAX, 0.0f};
     for (int64_t i = c.e0 + tid; i < c.e1; i += N) {
         const int64_t v = i < s.head ? i : i + s.body * E::PER;
-        const float y = E::get(x[v]);
-        run_add<1, REST>(run, &y, REST && on_list(l, a.slots, (uint32_t)v) ? 1u : 0u, a.a2);
+        const float y[1] = {E::get(x[v])};
+        run_add<1, REST>(run, y, REST && on_list(l, a.slots, (uint32_t)v) ? 1u : 0u, a.a2);
     }
     const int held = (int)(c.b1 - c.b0 < U * N ? c.b1 - c.b0 : U * N);
     if (REST) mark<CAP, N>(a, l, s_bits, s.head + c.b0 * E::PER, c.b1 - c.b0 < CHUNK / E::PER ? (c.b1 - c.b0) * E::PER : CHUNK);
     run_held<TYPE, REST, N, U>(run, w, held, s_bits, a.a2);
     run_over<TYPE, REST, CAP, N>(run, a, l, s_bits, body, s.head, c.b0, held, c.b1);
-    run = block_run<N>(run, a.a2, l.red);
+    const Sums sums = block_run<REST, CAP, N>(run, a, l, in);
     float v[2];
-    listed_sum<CAP, N>(a, l, run.m, v, in);
+    listed_sum<CAP, N>(a, l, sums.m, v, in);
     if (a.splits == 1) {
-        finish_row<CAP, N>(a, row, l, entries, sum_p, run, v[0], true);
+        finish_row<CAP, N>(a, row, l, entries, sum_p, sums, v[0], true);
     } else {
         block_sums<N>(v, l.red);
         if (tid == 0) {
-            const Part part = {run.m, run.s, run.r, v[0], v[1], {0.0f, 0.0f, 0.0f}};
+            const Part part = {sums, v[0], v[1], {0.0f, 0.0f}};
             a.part[row * a.splits + k] = part;
         }
     }
@@ -464,20 +492,26 @@ __global__ __launch_bounds__(N) void distill_forward_kernel(Distill a) {
 
 // A row's sums from its slices'; listed: this thread's share of the sum of p (x - m).
 template <int CAP, int N>
-__device__ Run join_row(const Distill &a, int64_t row, List<CAP> &l, float &listed) {
-    Run run = {-FLT_MAX, 0.0f, 0.0f};
+__device__ Sums join_row(const Distill &a, int64_t row, List<CAP> &l, float &listed) {
+    Run all = {-FLT_MAX, 0.0f}, off = {-FLT_MAX, 0.0f};
     for (int k = threadIdx.x; k < a.splits; k += N) {
-        const Part p = a.part[row * a.splits + k];
-        const Run b = {p.m, p.s, p.r};
-        run_join(run, b, a.a2);
+        const Sums p = a.part[row * a.splits + k].sums;
+        const Run pa = {p.m, p.s}, po = {p.mr, p.r};
+        run_join(all, pa, a.a2);
+        run_join(off, po, a.a2);
     }
-    run = block_run<N>(run, a.a2, l.red);
+    Sums b = {all.m, 0.0f, off.m, 0.0f};
+    block_max2<N>(b.m, b.mr, l.red);
+    float v[2] = {all.s * ex2((all.m - b.m) * a.a2), off.s * ex2((off.m - b.mr) * a.a2)};
+    block_sums<N>(v, l.red);
+    b.s = v[0];
+    b.r = v[1];
     listed = 0.0f;
     for (int k = threadIdx.x; k < a.splits; k += N) {
         const Part p = a.part[row * a.splits + k];
-        if (!(p.p == 0.0f)) listed += p.t + p.p * (p.m - run.m);
+        if (!(p.p == 0.0f)) listed += p.t + p.p * (p.sums.m - b.m);
     }
-    return run;
+    return b;
 }
 
 template <int TYPE, int CAP>
@@ -486,7 +520,7 @@ __global__ __launch_bounds__(T) void distill_join_kernel(Distill a) {
     const int64_t row = blockIdx.x;
     float sum_p, listed;
     const int entries = load_list<TYPE, CAP, T>(a, row, nullptr, l, sum_p, [](uint32_t) { return false; });
-    const Run run = join_row<CAP, T>(a, row, l, listed);
+    const Sums run = join_row<CAP, T>(a, row, l, listed);
     finish_row<CAP, T>(a, row, l, entries, sum_p, run, listed, true);
 }
 
@@ -518,17 +552,17 @@ __global__ __launch_bounds__(T) void distill_backward_kernel(Distill a) {
     const int entries = load_list<TYPE, CAP, T>(a, row, x, l, sum_p, in);
     float4 st;
     if (JOIN) {
-        const Run run = join_row<CAP, T>(a, row, l, listed);
+        const Sums run = join_row<CAP, T>(a, row, l, listed);
         st = finish_row<CAP, T>(a, row, l, entries, sum_p, run, listed, k == 0);
     } else {
         st = a.stats[row];
     }
-    if (st.w == 0.0f) {                                // a row that does not count
+    if (st.y == 0.0f) {                                // a row that does not count
         for (int64_t i = c.e0 + tid; i < c.e1; i += T) out[i < s.head ? i : i + s.body * PER] = E::put(0.0f);
         for (int64_t b = c.b0 + tid; b < c.b1; b += T) body_out[b] = make_uint4(0, 0, 0, 0);
         return;
     }
-    const float g = g0 * a.scale, q0 = 1.0f / st.y, f = q0 * st.z * g;
+    const float g = g0 * a.scale, q0 = 1.0f / st.y, f = st.w * g;
     // the listed items of this slice
     float mine[PLACES];
     uint32_t here[PLACES];
@@ -541,7 +575,7 @@ __global__ __launch_bounds__(T) void distill_backward_kernel(Distill a) {
     __syncthreads();
     for (int64_t i = c.e0 + tid; i < c.e1; i += T) {
         const int64_t v = i < s.head ? i : i + s.body * PER;
-        out[v] = E::put(ex2((E::get(x[v]) - st.x) * a.a2) * f);
+        out[v] = E::put(ex2((E::get(x[v]) - st.z) * a.a2) * f);
     }
     for (int64_t b = c.b0 + tid; b < c.b1; b += U * T) {
         if (b != c.b0 + tid) {
@@ -551,7 +585,7 @@ __global__ __launch_bounds__(T) void distill_backward_kernel(Distill a) {
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (b + u * T < c.b1) body_out[b + u * T] = gradient_of<TYPE>(w[u], st.x, a.a2, f);
+            if (b + u * T < c.b1) body_out[b + u * T] = gradient_of<TYPE>(w[u], st.z, a.a2, f);
     }
     __syncthreads();                                   // the listed items' values replace the ones just written
 #pragma unroll
@@ -591,21 +625,21 @@ __global__ __launch_bounds__(N, 4) void distill_row_kernel(Distill a) {
         if (u * N + tid < held) w[u] = body[u * N + tid];
     const bool single = tid < s.head + s.tail;         // (fewer than 16 of them)
     const int64_t v1 = tid < s.head ? tid : tid + s.body * PER;
-    const float y1 = single ? E::get(x[v1]) : 0.0f;
+    const float y1[1] = {single ? E::get(x[v1]) : 0.0f};
     const float g0 = a.grad_loss ? a.grad_loss[row] : 1.0f;
     float sum_p;
     const int entries = load_list<TYPE, CAP, N>(a, row, x, l, sum_p, [](uint32_t) { return true; });
-    Run run = {-FLT_MAX, 0.0f, 0.0f};
-    if (single) run_add<1, REST>(run, &y1, REST && on_list(l, a.slots, (uint32_t)v1) ? 1u : 0u, a.a2);
+    Run run = {-FLT_MAX, 0.0f};
+    if (single) run_add<1, REST>(run, y1, REST && on_list(l, a.slots, (uint32_t)v1) ? 1u : 0u, a.a2);
     if (REST) mark<CAP, N>(a, l, s_bits, s.head, s.body < CHUNK / PER ? s.body * PER : CHUNK);
     run_held<TYPE, REST, N, NV>(run, w, held, s_bits, a.a2);
     run_over<TYPE, REST, CAP, N>(run, a, l, s_bits, body, s.head, 0, held, s.body);
-    run = block_run<N>(run, a.a2, l.red);
+    const Sums sums = block_run<REST, CAP, N>(run, a, l, [](uint32_t) { return true; });
     float v[2];
-    listed_sum<CAP, N>(a, l, run.m, v, [](uint32_t) { return true; });
-    const float4 st = finish_row<CAP, N>(a, row, l, entries, sum_p, run, v[0], true);
-    const bool counts = st.w != 0.0f;
-    const float g = g0 * a.scale, q0 = 1.0f / st.y, f = q0 * st.z * g;
+    listed_sum<CAP, N>(a, l, sums.m, v, [](uint32_t) { return true; });
+    const float4 st = finish_row<CAP, N>(a, row, l, entries, sum_p, sums, v[0], true);
+    const bool counts = st.y != 0.0f;
+    const float g = g0 * a.scale, q0 = 1.0f / st.y, f = st.w * g;
     float mine[PLACES];
     uint32_t here[PLACES];
 #pragma unroll
@@ -616,10 +650,10 @@ __global__ __launch_bounds__(N, 4) void distill_row_kernel(Distill a) {
     }
     __syncthreads();
     const uint4 zero = make_uint4(0, 0, 0, 0);
-    if (single) out[v1] = E::put(counts ? ex2((y1 - st.x) * a.a2) * f : 0.0f);
+    if (single) out[v1] = E::put(counts ? ex2((y1[0] - st.z) * a.a2) * f : 0.0f);
 #pragma unroll
     for (int u = 0; u < NV; ++u)
-        if (u * N + tid < held) put_group<LONG>(body_out + u * N + tid, counts ? gradient_of<TYPE>(w[u], st.x, a.a2, f) : zero);
+        if (u * N + tid < held) put_group<LONG>(body_out + u * N + tid, counts ? gradient_of<TYPE>(w[u], st.z, a.a2, f) : zero);
     for (int64_t b = s.body - 1 - tid; b >= held; b -= U * N) {        // from the end: what was read last is nearest
         uint4 r[U];
 #pragma unroll
@@ -627,7 +661,7 @@ __global__ __launch_bounds__(N, 4) void distill_row_kernel(Distill a) {
             if (b - u * N >= held) r[u] = body[b - u * N];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (b - u * N >= held) put_group<LONG>(body_out + b - u * N, counts ? gradient_of<TYPE>(r[u], st.x, a.a2, f) : zero);
+            if (b - u * N >= held) put_group<LONG>(body_out + b - u * N, counts ? gradient_of<TYPE>(r[u], st.z, a.a2, f) : zero);
     }
     __syncthreads();
 #pragma unroll
@@ -655,11 +689,12 @@ bool shape_ok(const void *logits, int type, int64_t R, int64_t V, int64_t ld, fl
     return R == 0 || (logits && ids && values && (uintptr_t)logits % size == 0);
 }
 
-Distill params(const void *logits, int64_t R, int64_t V, int64_t ld, float scale, const uint32_t *ids, const float *values, int topk,
+Distill params(const void *logits, int type, int64_t R, int64_t V, int64_t ld, float scale, const uint32_t *ids, const float *values, int topk,
                float teacher_scale, const float *teacher_lse) {
     Distill a;
     a.x = logits; a.R = R; a.V = V; a.ld = ld;
     a.scale = scale; a.a2 = scale * LOG2E;
+    a.lowest = type == ICQ_F16 ? -65504.0f : type == ICQ_BF16 ? -0x1.fep127f : -FLT_MAX;
     a.ids = ids; a.values = values; a.topk = topk;
     a.slots = 32;
     while (a.slots < 2 * topk) a.slots *= 2;
@@ -728,7 +763,7 @@ ICQ_EXPORT int icq_distill(const void *logits, int type, int64_t R, int64_t V, i
     if (!loss || (uintptr_t)stats % 16 != 0 || (grad && !grad_ok(logits, type, V, ld, grad, ld_grad))) return ICQ_ERR_ARG;
     const int cu = icq_num_cu();
     if (cu <= 0) return ICQ_ERR_HIP;
-    Distill a = params(logits, R, V, ld, scale, ids, values, topk, teacher_scale, teacher_lse);
+    Distill a = params(logits, type, R, V, ld, scale, ids, values, topk, teacher_scale, teacher_lse);
     const size_t parts = part_bytes(R, splits_of(R, V, cu, 0));
     if (!workspace || (uintptr_t)workspace % ICQ_ALIGN != 0 || workspace_bytes < parts + part_bytes(R, 1)) return ICQ_ERR_WORKSPACE;
     a.part = static_cast<Part *>(workspace);
@@ -753,7 +788,7 @@ ICQ_EXPORT int icq_distill_backward(const void *logits, int type, int64_t R, int
     if (!stats || (uintptr_t)stats % 16 != 0 || !grad_ok(logits, type, V, ld, grad, ld_grad)) return ICQ_ERR_ARG;
     const int cu = icq_num_cu();
     if (cu <= 0) return ICQ_ERR_HIP;
-    Distill a = params(logits, R, V, ld, scale, ids, values, topk, teacher_scale, teacher_lse);
+    Distill a = params(logits, type, R, V, ld, scale, ids, values, topk, teacher_scale, teacher_lse);
     a.splits = splits_of(R, V, cu, 0);
     a.stats = reinterpret_cast<float4 *>(const_cast<float *>(stats));
     a.grad_loss = grad_loss; a.grad = grad; a.ld_grad = ld_grad;
