@@ -459,10 +459,17 @@ int icq_block_matmul(const uint8_t *a, int a_format, int64_t lda, const float *a
  *     everything the teacher scored; what is left, p_r = max(0, 1 - sum_j p_j),
  *     is compared with the student's mass off the list, q_r, however small that is:
  *     loss[r] gains p_r (log p_r - log q_r)   (not if the list names all V items).
- *   grad[r][v] = grad_loss[r] * d loss[r] / d logits[r][v]
- *              = grad_loss[r] * scale * (q_v - p_v)      for listed items,
+ *   grad[r][v] = grad_loss[r] * scale * (q_v - p_v)      for listed items,
  *                grad_loss[r] * scale * c * q_v          for the others,
  *     c = 1, or 1 - p_r / q_r with teacher_lse; grad_loss NULL: 1.
+ *     This is grad_loss[r] * d loss[r] / d logits[r][v] where the teacher's
+ *     masses add up to one, S = sum_j p_j + p_r = 1: without teacher_lse, and
+ *     with one that is what it is said to be, of scores of items below V.  S is
+ *     not 1 where teacher_lse lies below the logsumexp of the row's entries
+ *     (S = sum_j p_j > 1), or above it though the list names all V items (p_r
+ *     has nothing to face and is left out): there the derivative has S q_v in
+ *     the place of q_v, and what is written exceeds it by
+ *     grad_loss[r] * scale * (1 - S) q_v.
  * A row without entries, or whose logits are all -inf, has loss 0 and gradient
  * 0.  The loss is +inf where a listed item of positive probability has a logit
  * of -inf, and where p_r > 0 and the logits off the list are all -inf or the

@@ -5,7 +5,8 @@
 // with the sum of its probabilities).  p_j = exp(z_j - L), L = logsumexp of the list, or the caller's logsumexp over everything
 // the teacher scored; then the remaining mass p_r = max(0, 1 - sum p) faces the student's mass off the list, q_r.
 //     loss = sum_j p_j (log p_j - log q_j)  [+ p_r (log p_r - log q_r)]
-//     d loss / d x_v = scale (q_v - p_v) on the list, scale q_v [- scale p_r q_v / q_r] off it.
+//     gradient = scale (q_v - p_v) on the list, scale q_v [- scale p_r q_v / q_r] off it,
+// d loss / d x_v where the masses p add up to one (a caller's logsumexp may make them do otherwise: S q_v would stand in q_v's place).
 // Statistics and sums are held in 32 bits.  The items off the list are summed by themselves, relative to a maximum of their own (the listed
 // ones are marked bit by bit and join from the list), not as one minus the listed mass: a student that has learnt its list leaves
 // little there, e^-100 and less under a large scale.  log q_r and q_v / q_r follow from that sum without q_r, which may be too small to hold.
