@@ -474,7 +474,8 @@ int icq_block_matmul(const uint8_t *a, int a_format, int64_t lda, const float *a
  * 0.  The loss is +inf where a listed item of positive probability has a logit
  * of -inf, and where p_r > 0 and the logits off the list are all -inf or the
  * type's lowest finite value (masked places; their gradients are 0 then).
- * NaN, and logits of +inf, make the row's loss and gradient NaN.
+ * NaN in the logits, in an entry's score or in teacher_lse, and logits of +inf,
+ * make the loss and the whole gradient of a row with entries NaN.
  * icq_distill writes loss [R]; stats [R][4] fp32, 16-byte aligned, if not NULL
  * (what icq_distill_backward reads); and the gradient if grad is not NULL (in
  * logits' type; grad_loss is then used).  grad may be the logits' own memory

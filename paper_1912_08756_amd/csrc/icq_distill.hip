@@ -124,7 +124,7 @@ struct List {
     uint32_t twice;
 };
 
-// Fills the list (x: the row's logits, read at those listed places that `in` takes, early: they share lines with what is read next); returns the number of entries (distinct ids) and the sum of their probabilities.  All threads of the block.
+// Fills the list (x: the row's logits, read at those listed places that `in` takes, early: they share lines with what is read next); returns the number of entries (distinct ids) and the sum of their probabilities: without the caller's logsumexp one, or NaN where a score is.  All threads of the block.
 template <int TYPE, int CAP, int N, typename In>
 __device__ int load_list(const Distill &a, int64_t row, const typename IcqElem<TYPE>::raw *x, List<CAP> &l, float &sum_p, In in) {
     constexpr int n = N, PLACES = (CAP + N - 1) / N;
@@ -182,8 +182,8 @@ __device__ int load_list(const Distill &a, int64_t row, const typename IcqElem<T
 #pragma unroll
     for (int u = 0; u < PLACES; ++u)
         if (u * n + tid < a.topk) l.x[u * n + tid] = IcqElem<TYPE>::get(logit[u]);
-    sum_p = 0.0f;
-    if (a.teacher_lse) {                               // (only then is the sum of any consequence)
+    sum_p = own_sum ? part - part + 1.0f : top == -INFINITY && count > 0.0f ? NAN : 0.0f;      // (entries, and none of them a number)
+    if (a.teacher_lse) {                               // (only then is the sum itself of any consequence)
         block_sums<N>(sum, l.red);
         sum_p = sum[0];
     }
@@ -326,7 +326,7 @@ __device__ float4 finish_row(const Distill &a, int64_t row, List<CAP> &l, int en
     const float log_s = logf(run.s);
     const bool counts = entries > 0 && !(run.s == 0.0f);
     const bool rest = a.teacher_lse && (int64_t)entries < a.V;
-    const float p_r = rest ? fmaxf(0.0f, 1.0f - sum_p) : 0.0f;
+    const float p_r = rest ? (sum_p > 1.0f ? 0.0f : 1.0f - sum_p) : 0.0f;
     // the sum off the list, zero where all of it is masked: it takes no gradient then (as it is, if that is NaN)
     const float r = run.mr > a.lowest ? run.r : 0.0f * run.r;
     if (write) {                                       // (the same for the whole block)
@@ -343,7 +343,8 @@ __device__ float4 finish_row(const Distill &a, int64_t row, List<CAP> &l, int en
         base = run.mr;
         factor = r == 0.0f ? 0.0f : ex2((run.mr - run.m) * a.a2) / run.s - p_r / r;
     }
-    const float4 st = make_float4(run.m, counts ? run.s : 0.0f, base, factor);
+    const bool odd = sum_p != sum_p;                   // a NaN of the teacher's: in every item's gradient, as in the loss
+    const float4 st = make_float4(run.m, counts ? odd ? sum_p : run.s : 0.0f, base, odd ? sum_p : factor);
     if (write && a.stats && threadIdx.x == 0) a.stats[row] = st;
     return st;
 }
