@@ -167,14 +167,15 @@ __device__ __forceinline__ void values8(const Eight<TYPE> &v, float *x) {
 // TILE: one scale for the whole tile, else one per row and column of it, each worked out by one thread (by all that need it, with words
 // compared one by one: 139 us at 8192 x 16000 against 118; 256 threads of 8 x 8 values each: the same 118, small tiles slower).
 template <int TYPE, int FORMAT, bool TILE>
-__global__ __launch_bounds__(512) void quantize_tile_kernel(Quantize a) {
+__global__ __launch_bounds__(512) void quantize_tile_kernel(Quantize a, uint32_t first_tile) {
     constexpr int WORDS = Eight<TYPE>::WORDS;
     __shared__ __attribute__((aligned(16))) uint32_t s_cols[8][128];          // largest magnitudes: of a wavefront's rows in each column,
     __shared__ __attribute__((aligned(16))) uint32_t s_rows[128];             // of each row
     __shared__ __attribute__((aligned(16))) float s_inv[256];                 // the columns' reciprocal scales, then the rows'
     __shared__ __attribute__((aligned(16))) uint8_t s_turn[128][128];         // column c's 8-byte piece p at place p ^ (c / 8)
     const int tid = threadIdx.x, g = tid & 15, h = tid >> 4, wave = tid >> 6, lane = tid & 63;
-    const int bc = blockIdx.x % a.across, br = blockIdx.x / a.across;
+    const uint32_t tile = first_tile + blockIdx.x;
+    const int bc = (int)(tile % (uint32_t)a.across), br = (int)(tile / (uint32_t)a.across);
     const int64_t r0 = (int64_t)br * 128 + 4 * h, c0 = (int64_t)bc * 128 + 8 * g;
     Eight<TYPE> v[4];
 #pragma unroll
@@ -289,18 +290,24 @@ __global__ __launch_bounds__(512) void quantize_tile_kernel(Quantize a) {
     }
 }
 
+// A launch counts less than 2^32 threads: 2^31 of them at a time.
+constexpr int64_t ROW_TASKS = 1ll << 27, TILES = 1ll << 22;
+
 template <int TYPE, int FORMAT>
 int launch(const Quantize &a, int block_rows, hipStream_t s) {
     if (block_rows == 1 && !a.codes_t) {
-        const int64_t step = (int64_t)0x7fffffff / a.across;          // rows whose blocks 32 bits count
+        const int64_t step = ROW_TASKS / a.across;                    // (a.across is at most 2^24)
         for (int64_t r = 0; r < a.rows; r += step) {
             const uint32_t tasks = (uint32_t)((a.rows - r < step ? a.rows - r : step) * a.across);
             hipLaunchKernelGGL(HIP_KERNEL_NAME(quantize_rows_kernel<TYPE, FORMAT>), dim3((tasks + 15u) / 16u), dim3(256), 0, s, a, r, tasks);
         }
-    } else if (block_rows == 1) {
-        hipLaunchKernelGGL(HIP_KERNEL_NAME(quantize_tile_kernel<TYPE, FORMAT, false>), dim3((uint32_t)((int64_t)a.across * a.down)), dim3(512), 0, s, a);
-    } else {
-        hipLaunchKernelGGL(HIP_KERNEL_NAME(quantize_tile_kernel<TYPE, FORMAT, true>), dim3((uint32_t)((int64_t)a.across * a.down)), dim3(512), 0, s, a);
+        return icq_check_launch();
+    }
+    const int64_t tiles = (int64_t)a.across * a.down;
+    for (int64_t t = 0; t < tiles; t += TILES) {
+        const dim3 grid((uint32_t)(tiles - t < TILES ? tiles - t : TILES));
+        if (block_rows == 1) hipLaunchKernelGGL(HIP_KERNEL_NAME(quantize_tile_kernel<TYPE, FORMAT, false>), grid, dim3(512), 0, s, a, (uint32_t)t);
+        else hipLaunchKernelGGL(HIP_KERNEL_NAME(quantize_tile_kernel<TYPE, FORMAT, true>), grid, dim3(512), 0, s, a, (uint32_t)t);
     }
     return icq_check_launch();
 }
