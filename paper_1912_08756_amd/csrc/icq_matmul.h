@@ -59,6 +59,9 @@ __device__ __forceinline__ void store_part(const Product &p, int split, int64_t 
             if (n + e < p.N) o[e] = v[e];
 }
 
+// Blocks of up to 512 threads of one launch, a multiple of 8: the threads of a launch are counted in 32 bits.
+constexpr uint32_t ICQ_PRODUCT_BLOCKS = 1u << 22;
+
 // The first n < 16 of 16 bytes, zeros after them.
 __device__ __forceinline__ uint4 first_bytes(const uint4 &v, int n) {
     uint32_t w[4] = {v.x, v.y, v.z, v.w};

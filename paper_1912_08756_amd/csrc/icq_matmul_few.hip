@@ -6,6 +6,8 @@
 // 13.0 us, 5.2 TB/s of b; where b is small, by the launch and one chain of loads (1 x 4096 x 4096: 8 us with the host's share).
 #include "icq_matmul.h"
 
+#include <algorithm>
+
 namespace {
 
 constexpr int WAVES = 8;
@@ -29,10 +31,10 @@ struct Operands {
 };
 
 template <int FA, int FB, bool ROWS, bool EXACT, int MT, int NT>
-__global__ __launch_bounds__(64 * WAVES) void product_few_kernel(Product p, int out_type) {
+__global__ __launch_bounds__(64 * WAVES) void product_few_kernel(Product p, int out_type, uint32_t first_block) {
     __shared__ icq_f32x4 s_part[WAVES / 2][NT * MT][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, at = lane & 15, quarter = lane >> 4;
-    const int64_t n0 = (int64_t)blockIdx.x * (16 * NT);
+    const int64_t n0 = (int64_t)(first_block + blockIdx.x) * (16 * NT);
     const int whole = (int)(p.K / 128), ragged = (int)(p.K % 128);
     const uint8_t *row_a[MT], *row_b[NT];
 #pragma unroll
@@ -125,7 +127,9 @@ __global__ __launch_bounds__(64 * WAVES) void product_few_kernel(Product p, int 
 template <int FA, int FB, bool ROWS, bool EXACT>
 int launch(const Product &p, int num_cu, int out_type, hipStream_t s) {
     auto go = [&](auto kernel, int nt) {
-        hipLaunchKernelGGL(kernel, dim3((uint32_t)((p.N + 16 * nt - 1) / (16 * nt)), (uint32_t)p.splits), dim3(64 * WAVES), 0, s, p, out_type);
+        const uint32_t blocks = (uint32_t)((p.N + 16 * nt - 1) / (16 * nt));
+        for (uint32_t i = 0; i < blocks; i += ICQ_PRODUCT_BLOCKS)
+            hipLaunchKernelGGL(kernel, dim3(std::min(blocks - i, ICQ_PRODUCT_BLOCKS), (uint32_t)p.splits), dim3(64 * WAVES), 0, s, p, out_type, i);
     };
     if (p.M > 16) go(product_few_kernel<FA, FB, ROWS, EXACT, 2, 1>, 1);
     else if (p.N >= 64 * (int64_t)num_cu) go(product_few_kernel<FA, FB, ROWS, EXACT, 1, 4>, 4);     // (a's rows read a quarter as often)

@@ -14,6 +14,8 @@
 // (a quarter of the requests to the second-level cache); results stored in whole rows 470 -> 447, 2048 x 16384 x 960 91 -> 46.
 #include "icq_matmul.h"
 
+#include <algorithm>
+
 namespace {
 
 // Rows and columns of a wavefront's part in units of 32, wavefronts along m and n, stages in the LDS.
@@ -116,15 +118,16 @@ __device__ __forceinline__ void load_word_to_lds(const i32x4 &base, uint32_t off
 }
 
 template <typename S, int FA, int FB, bool ROWS, int MODE>
-__global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product p, int tiles_m, int tiles_n, int out_type) {
+__global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product p, int tiles_m, int tiles_n, int out_type, uint32_t first_block) {
     constexpr int T = S::T, NI = S::NI, NJ = S::NJ, DEPTH = S::DEPTH, WAVES = S::WAVES, PARTS = S::PARTS, LOADS = S::LOADS;
     // loads under way that the barrier need not wait for: those of the stages after the next
     constexpr int LATER = (DEPTH - 2) * LOADS - (NI == 1 ? LOADS / 2 : 0);
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
     float *s_scales = reinterpret_cast<float *>(smem + DEPTH * S::STAGE);     // [3][four blocks along K][a: T, b: T]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    // XCD blockIdx % 8 takes a contiguous share of the tiles, eight tiles of m at a time
-    const int total = tiles_m * tiles_n, q8 = total / 8, r8 = total % 8, xcd = blockIdx.x % 8, at8 = blockIdx.x / 8;
+    // XCD blockIdx % 8 takes a contiguous share of the tiles, eight tiles of m at a time (first_block: a multiple of 8)
+    const uint32_t block_id = first_block + blockIdx.x;
+    const int total = tiles_m * tiles_n, q8 = total / 8, r8 = total % 8, xcd = block_id % 8, at8 = block_id / 8;
     const int tile = xcd * q8 + (xcd < r8 ? xcd : r8) + at8;
     const int group = tile / (8 * tiles_n), in = tile % (8 * tiles_n), high = min(8, tiles_m - group * 8);
     const int64_t m0 = (int64_t)(group * 8 + in % high) * T, n0 = (int64_t)(in / high) * T;
@@ -349,10 +352,11 @@ __global__ __launch_bounds__(S::THREADS, 2) void product_kernel(Product p, int t
 template <typename S, int FA, int FB, bool ROWS>
 int launch(const Product &p, bool pow2, int out_type, hipStream_t s) {
     const int tm = (int)((p.M + S::T - 1) / S::T), tn = (int)((p.N + S::T - 1) / S::T);
-    const dim3 grid((uint32_t)((int64_t)tm * tn), (uint32_t)p.splits);
+    const uint32_t blocks = (uint32_t)((int64_t)tm * tn);
     auto go = [&](auto kernel) {
         if (icq_allow_lds(reinterpret_cast<const void *>(kernel), S::LDS_BYTES, true) != hipSuccess) return ICQ_ERR_HIP;
-        hipLaunchKernelGGL(kernel, grid, dim3(S::THREADS), S::LDS_BYTES, s, p, tm, tn, out_type);
+        for (uint32_t i = 0; i < blocks; i += ICQ_PRODUCT_BLOCKS)
+            hipLaunchKernelGGL(kernel, dim3(std::min(blocks - i, ICQ_PRODUCT_BLOCKS), (uint32_t)p.splits), dim3(S::THREADS), S::LDS_BYTES, s, p, tm, tn, out_type, i);
         return icq_check_launch();
     };
     if (out_type == ICQ_F32) {
