@@ -65,11 +65,12 @@ __device__ __forceinline__ i32x4 bytes_from(const void *p) {
     return r;
 }
 
+#pragma clang diagnostic ignored "-Winline-asm"       // (M0, which the next two name as overwritten, is no register of the allocator's: a warning each)
+
 // 16 bytes per lane from base + off + by into the LDS at `to` + 16 * lane.  Written out because the compiler makes every later LDS read
-// wait for loads of its own built-in; they have no destination registers, and the waits for them are those of loads_left(0).  (M0: nothing
-// else here uses it.)
+// wait for loads of its own built-in; they have no destination registers, and the waits for them are those of loads_left(0).
 __device__ __forceinline__ void load_to_lds(const i32x4 &base, uint32_t off, int by, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(off), "s"(base), "s"(by) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(off), "s"(base), "s"(by) : "memory", "m0");
 }
 
 // 32 rows and 32 NJ columns of the result from a wavefront's accumulators, whole rows at a time: in the accumulators a lane has four
@@ -114,7 +115,7 @@ __device__ __forceinline__ void store_rows(uint8_t *turn, const f32x16 (&acc)[NJ
 
 // The same for 4 bytes per lane, to `to` + 4 * lane.
 __device__ __forceinline__ void load_word_to_lds(const i32x4 &base, uint32_t off, int by, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(to), "v"(off), "s"(base), "s"(by) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(to), "v"(off), "s"(base), "s"(by) : "memory", "m0");
 }
 
 template <typename S, int FA, int FB, bool ROWS, int MODE>
