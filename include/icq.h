@@ -479,7 +479,8 @@ int icq_block_matmul(const uint8_t *a, int a_format, int64_t lda, const float *a
  * icq_distill writes loss [R]; stats [R][4] fp32, 16-byte aligned, if not NULL
  * (what icq_distill_backward reads); and the gradient if grad is not NULL (in
  * logits' type; grad_loss is then used).  grad may be the logits' own memory
- * (same pointer, ld_grad = ld), else the two must not overlap.
+ * (same pointer, ld_grad = ld), else their rows must not overlap
+ * (ICQ_ERR_ARG).
  * icq_distill_backward writes the gradient from the logits, the same lists and
  * the stats of an earlier icq_distill.
  * R <= ICQ_MAX_Q, 1 <= topk <= ICQ_MAX_TOPK; workspace (icq_distill):

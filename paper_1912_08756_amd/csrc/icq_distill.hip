@@ -16,6 +16,7 @@
 // partial results the gradient's launch joins.  The order of every sum is fixed, so a call gives the same bits each time.
 // Bound by memory where rows are many (4096 x 131072 bf16, loss and gradient 425 us, 5.05 TB/s of one reading and one writing; a copy
 // runs at 5.17), by the chain of loads and reductions of a launch where they are few (7 us; 8 x 10^6 f32: 24 us for two).
+#include "icq_overlap.h"
 #include "icq_types.h"
 
 #include <float.h>
@@ -743,8 +744,12 @@ void launch_distill(const Distill &a, hipStream_t s) {
     else if (a.splits > 1) hipLaunchKernelGGL(HIP_KERNEL_NAME(distill_join_kernel<TYPE, CAP>), dim3((uint32_t)a.R), dim3(T), 0, s, a);
 }
 
-bool grad_ok(const void *logits, int type, int64_t V, int64_t ld, const void *grad, int64_t ld_grad) {
-    return grad && ld_grad >= V && (uintptr_t)grad % icq_type_bytes(type) == 0 && (grad != logits || ld_grad == ld);
+// The logits' own memory, or none of it.
+bool grad_ok(const void *logits, int type, int64_t R, int64_t V, int64_t ld, const void *grad, int64_t ld_grad) {
+    const int64_t size = icq_type_bytes(type);
+    if (!grad || ld_grad < V || (uintptr_t)grad % size != 0) return false;
+    if (grad == logits) return ld_grad == ld;
+    return !icq_rows_overlap((uintptr_t)logits, ld * size, (uintptr_t)grad, ld_grad * size, R, V * size);
 }
 
 }  // namespace
@@ -762,7 +767,7 @@ ICQ_EXPORT int icq_distill(const void *logits, int type, int64_t R, int64_t V, i
                            const float *grad_loss, void *grad, int64_t ld_grad, void *workspace, size_t workspace_bytes, void *stream) {
     if (!shape_ok(logits, type, R, V, ld, scale, ids, values, topk, teacher_scale)) return ICQ_ERR_ARG;
     if (R == 0) return ICQ_OK;
-    if (!loss || (uintptr_t)stats % 16 != 0 || (grad && !grad_ok(logits, type, V, ld, grad, ld_grad))) return ICQ_ERR_ARG;
+    if (!loss || (uintptr_t)stats % 16 != 0 || (grad && !grad_ok(logits, type, R, V, ld, grad, ld_grad))) return ICQ_ERR_ARG;
     const int cu = icq_num_cu();
     if (cu <= 0) return ICQ_ERR_HIP;
     Distill a = params(logits, type, R, V, ld, scale, ids, values, topk, teacher_scale, teacher_lse);
@@ -787,7 +792,7 @@ ICQ_EXPORT int icq_distill_backward(const void *logits, int type, int64_t R, int
                                     const float *grad_loss, void *grad, int64_t ld_grad, void *stream) {
     if (!shape_ok(logits, type, R, V, ld, scale, ids, values, topk, teacher_scale)) return ICQ_ERR_ARG;
     if (R == 0) return ICQ_OK;
-    if (!stats || (uintptr_t)stats % 16 != 0 || !grad_ok(logits, type, V, ld, grad, ld_grad)) return ICQ_ERR_ARG;
+    if (!stats || (uintptr_t)stats % 16 != 0 || !grad_ok(logits, type, R, V, ld, grad, ld_grad)) return ICQ_ERR_ARG;
     const int cu = icq_num_cu();
     if (cu <= 0) return ICQ_ERR_HIP;
     Distill a = params(logits, type, R, V, ld, scale, ids, values, topk, teacher_scale, teacher_lse);
