@@ -447,7 +447,8 @@ int icq_block_matmul(const uint8_t *a, int a_format, int64_t lda, const float *a
 
 /*
  * Distillation from a teacher's lists.  Row r of logits [R][V] (element type
- * `type`) gives q = softmax(scale * logits), scale > 0; its list ids / values
+ * `type`) gives q = softmax(scale * logits), 0 < scale < 2.3e38 (scale log2(e)
+ * is held in 32 bits); its list ids / values
  * [R][topk] gives teacher scores z_j = teacher_scale * value_j.  The lists of
  * icq_search are such lists: ids, distances, teacher_scale = -1 / temperature.
  * An entry is a place whose id is below V and whose score is not -inf (padding

@@ -688,7 +688,7 @@ bool shape_ok(const void *logits, int type, int64_t R, int64_t V, int64_t ld, fl
               int topk, float teacher_scale) {
     const int size = icq_type_bytes(type);
     if (size == 0 || R < 0 || R > ICQ_MAX_Q || V < 1 || V > ICQ_MAX_EXTENT || ld < V || topk < 1 || topk > ICQ_MAX_TOPK) return false;
-    if (!(scale > 0.0f) || !(scale <= FLT_MAX) || !(teacher_scale >= -FLT_MAX && teacher_scale <= FLT_MAX)) return false;
+    if (!(scale > 0.0f) || !(scale * LOG2E <= FLT_MAX) || !(teacher_scale >= -FLT_MAX && teacher_scale <= FLT_MAX)) return false;
     return R == 0 || (logits && ids && values && (uintptr_t)logits % size == 0);
 }
 
