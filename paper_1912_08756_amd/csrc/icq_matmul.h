@@ -1,5 +1,6 @@
 // Shared by the kernels of icq_block_matmul.
 #pragma once
+#include "icq_matmul_plan.h"
 #include "icq_types.h"
 
 struct Product {
@@ -73,11 +74,7 @@ __device__ __forceinline__ uint4 first_bytes(const uint4 &v, int n) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// The product in tiles of 256 x 256 (not into f32), of 128 x 128 with two stages in the LDS or four, or of 64 x 64, p.splits parts of
-// the contraction (icq_matmul_tiles.hip).
-enum icq_tiles { ICQ_TILES_WIDE, ICQ_TILES_SMALL, ICQ_TILES_DEEP, ICQ_TILES_LITTLE };
+// The product in tiles, p.splits parts of the contraction (icq_matmul_tiles.hip).
 int icq_launch_product_tiles(const Product &p, icq_tiles tiles, int a_format, int b_format, bool rows, bool pow2, int out_type, hipStream_t s);
 // The product of few rows of a (icq_matmul_few.hip).
-bool icq_product_few_usable(int64_t M, int64_t N, int num_cu);
-int icq_product_few_splits(int64_t N, int64_t K, int num_cu);
 int icq_launch_product_few(const Product &p, int num_cu, int a_format, int b_format, bool rows, int out_type, hipStream_t s);

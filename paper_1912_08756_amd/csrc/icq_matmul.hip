@@ -38,52 +38,6 @@ __global__ __launch_bounds__(256) void product_join_kernel(Product p) {
     store4<TYPE>(p, m, n, s);
 }
 
-// How a product is computed: `few` rows; else in tiles, the contraction in `splits` parts.
-struct Plan {
-    bool few;
-    icq_tiles tiles;
-    int splits;
-};
-
-// Tiles: the plan of the least time by a model of it, in us, from times of every form and number of parts on 33 to 8192 rows: 4.5 for a
-// launch with its first loads and last stores, and for a step (one scale block)
-//     256 x 256: 1.8 for a round of the chip, 1.2 and more for a part of one;
-//     128 x 128: 1.2 for two that share a compute unit, 0.5 to 0.6 for one by itself, the more of them the longer;
-//     64 x 64:   0.45 for two that share a compute unit, 0.3 for one by itself;
-// with the widened codes of a 32-bit result 1.9, 0.6 to 1.2, 0.66 and 0.45.  A split writes and reads its sums at 4.4 TB/s and costs a
-// launch.  (1024 x 1024 x 4096 into bf16: 128 x 128 in 1, 2, 4, 8 parts 23.1, 19.4, 19.1, 29.0; 64 x 64 in 1, 2, 4 parts 14.1, 18.6, 20.0.)
-Plan plan_of(int64_t M, int64_t N, int64_t K, bool exact, int num_cu) {
-    Plan best = {icq_product_few_usable(M, N, num_cu), ICQ_TILES_SMALL, 1};
-    if (best.few) {
-        best.splits = icq_product_few_splits(N, K, num_cu);
-        return best;
-    }
-    const int64_t kb = (K + 127) / 128;
-    double least = -1.0;
-    for (int64_t T = exact ? 128 : 256; T >= 64; T /= 2) {
-        const int64_t tiles = ((M + T - 1) / T) * ((N + T - 1) / T);
-        for (int splits = 1; splits <= 16 && (splits == 1 || kb >= 4 * splits); splits *= 2) {
-            const int64_t blocks = tiles * splits, steps = (kb + splits - 1) / splits, rounds = blocks / (2 * num_cu), left = blocks % (2 * num_cu);
-            const bool alone = blocks <= num_cu;
-            // what a step of the last round adds: a pair's, a single tile's, nothing
-            const auto last = [&](double pair, double one) { return left > num_cu ? pair : left > 0 ? one : 0.0; };
-            const double share = (double)left / num_cu;
-            double us;
-            if (T == 256) us = 1.8 * (blocks / num_cu) + (blocks % num_cu > 0 ? 1.2 + 0.6 * (blocks % num_cu) / num_cu : 0.0);
-            else if (T == 128) us = exact ? 1.9 * rounds + last(1.9, 0.6 + 0.6 * share) : 1.2 * rounds + last(1.2, 0.5 + 0.1 * share);
-            else us = exact ? 0.66 * rounds + last(0.66, 0.45) : 0.45 * rounds + last(0.45, 0.3);
-            us *= steps;
-            if (splits > 1) us += 2.5 + (double)splits * M * N * 8 / 4.4e6;
-            if (least < 0.0 || us < least) {
-                least = us;
-                best.tiles = T == 256 ? ICQ_TILES_WIDE : T == 64 ? ICQ_TILES_LITTLE : alone ? ICQ_TILES_DEEP : ICQ_TILES_SMALL;
-                best.splits = splits;
-            }
-        }
-    }
-    return best;
-}
-
 bool extents_ok(int64_t M, int64_t N, int64_t K) {
     return M >= 0 && N >= 0 && K >= 0 && M <= ICQ_MAX_EXTENT && N <= ICQ_MAX_EXTENT && K <= ICQ_MAX_EXTENT &&
            ((M + 63) / 64) * ((N + 63) / 64) <= 0x7fffffff;
@@ -95,7 +49,7 @@ ICQ_EXPORT int icq_block_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K,
     if (!out || !extents_ok(M, N, K)) return ICQ_ERR_ARG;
     const int cu = icq_num_cu();
     if (cu <= 0) return ICQ_ERR_HIP;
-    const int fast = plan_of(M, N, K, false, cu).splits, exact = plan_of(M, N, K, true, cu).splits, splits = fast > exact ? fast : exact;
+    const int fast = icq_plan_product(M, N, K, false, cu).splits, exact = icq_plan_product(M, N, K, true, cu).splits, splits = fast > exact ? fast : exact;
     *out = splits > 1 ? icq_align_up((size_t)splits * M * N * sizeof(float), ICQ_ALIGN) : 0;
     return ICQ_OK;
 }
@@ -119,7 +73,7 @@ ICQ_EXPORT int icq_block_matmul(const uint8_t *a, int a_format, int64_t lda, con
     p.M = M; p.N = N; p.K = K;
     p.kb = (int)((K + 127) / 128);
     p.out = out; p.ldo = ldo;
-    const Plan plan = plan_of(M, N, K, out_type == ICQ_F32, cu);
+    const icq_product_plan plan = icq_plan_product(M, N, K, out_type == ICQ_F32, cu);
     p.splits = plan.splits;
     p.per = (p.kb + p.splits - 1) / p.splits;
     p.part = static_cast<float *>(workspace);

@@ -10,7 +10,7 @@
 
 namespace {
 
-constexpr int WAVES = 8;
+constexpr int WAVES = ICQ_PRODUCT_FEW_WAVES;
 
 template <int FA, int FB, bool EXACT>
 __device__ __forceinline__ icq_f32x4 dot128(const icq_i32x8 &n, const icq_i32x8 &m) {
@@ -132,7 +132,7 @@ int launch(const Product &p, int num_cu, int out_type, hipStream_t s) {
             hipLaunchKernelGGL(kernel, dim3(std::min(blocks - i, ICQ_PRODUCT_BLOCKS), (uint32_t)p.splits), dim3(64 * WAVES), 0, s, p, out_type, i);
     };
     if (p.M > 16) go(product_few_kernel<FA, FB, ROWS, EXACT, 2, 1>, 1);
-    else if (p.N >= 64 * (int64_t)num_cu) go(product_few_kernel<FA, FB, ROWS, EXACT, 1, 4>, 4);     // (a's rows read a quarter as often)
+    else if (icq_product_few_wide(p.M, p.N, num_cu)) go(product_few_kernel<FA, FB, ROWS, EXACT, 1, 4>, 4);
     else go(product_few_kernel<FA, FB, ROWS, EXACT, 1, 1>, 1);
     return icq_check_launch();
 }
@@ -144,17 +144,6 @@ int launch_formats(const Product &p, int num_cu, int fa, int fb, int out_type, h
 }
 
 }  // namespace
-
-// Up to 16 rows; up to 32 where b has 16 rows for a compute unit or fewer (32 x 4096 x 4096: 10.5 us, in tiles 13; 32 x 16384 x 4096: 24,
-// in tiles 14; 16 x 16384 x 4096: 14.4 here).
-bool icq_product_few_usable(int64_t M, int64_t N, int num_cu) { return M <= 16 || (M <= 32 && N <= 16 * (int64_t)num_cu); }
-
-// Parts of the contraction: where the rows of b leave more than half of the chip idle, as long as a wavefront keeps four steps.
-int icq_product_few_splits(int64_t N, int64_t K, int num_cu) {
-    const int64_t blocks = (N + 15) / 16, idle = num_cu / (blocks > 0 ? blocks : 1), most = (K + 127) / 128 / (4 * WAVES);
-    const int64_t n = idle < most ? idle : most;
-    return (int)(n < 1 ? 1 : n);
-}
 
 int icq_launch_product_few(const Product &p, int num_cu, int fa, int fb, bool rows, int out_type, hipStream_t s) {
     if (out_type == ICQ_F32)
