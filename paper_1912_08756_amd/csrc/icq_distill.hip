@@ -16,6 +16,7 @@
 // partial results the gradient's launch joins.  The order of every sum is fixed, so a call gives the same bits each time.
 // Bound by memory where rows are many (4096 x 131072 bf16, loss and gradient 425 us, 5.05 TB/s of one reading and one writing; a copy
 // runs at 5.17), by the chain of loads and reductions of a launch where they are few (7 us; 8 x 10^6 f32: 24 us for two).
+#include "icq_distill_plan.h"
 #include "icq_overlap.h"
 #include "icq_types.h"
 
@@ -672,16 +673,6 @@ __global__ __launch_bounds__(N, 4) void distill_row_kernel(Distill a) {
         if (here[u] != ICQ_PAD_ID) out[here[u]] = E::put(mine[u]);
 }
 
-// Slices per row: one where there is a row for every compute unit, else enough blocks for the chip, none shorter than 8192 elements.
-// Loss and gradient together in one kernel (row_bytes: a row's, else 0): one slice from half as many rows on (200 rows of 131072 bf16:
-// 46 us in slices, 34 whole; 64 rows: 21 and 33), and for rows of up to 64 KB.
-int splits_of(int64_t R, int64_t V, int num_cu, int64_t row_bytes) {
-    if (R >= num_cu || (row_bytes > 0 && (2 * R >= num_cu || row_bytes <= 65536))) return 1;
-    const int64_t want = (4ll * num_cu + R - 1) / (R > 0 ? R : 1), most = V / 8192;
-    const int64_t n = want < most ? want : most;
-    return (int)(n < 1 ? 1 : n > 1024 ? 1024 : n);
-}
-
 size_t part_bytes(int64_t R, int splits) { return icq_align_up((size_t)R * splits * sizeof(Part), ICQ_ALIGN); }
 
 bool shape_ok(const void *logits, int type, int64_t R, int64_t V, int64_t ld, float scale, const uint32_t *ids, const float *values,
@@ -724,21 +715,18 @@ template <int TYPE, bool REST, int CAP>
 void launch_distill(const Distill &a, hipStream_t s) {
     constexpr int SIZE = sizeof(typename IcqElem<TYPE>::raw);
     if (a.grad && a.splits == 1 && same_phase(a, SIZE)) {
-        // threads and held groups by the row's length: up to 16, 32, 64 KB, and longer (4096 rows of 24000 bf16: 86 us by 256
-        // threads, 100 by 512; of 131072: 473 and 431); a row by itself on a compute unit by 1024
         auto go = [&](auto kernel, int n) { hipLaunchKernelGGL(kernel, dim3((uint32_t)a.R), dim3(n), 0, s, a); };
-        const int64_t bytes = a.V * SIZE;
-        if (a.R <= a.num_cu && bytes > 256 * 4 * 16 && bytes <= 1024 * 4 * 16) go(distill_row_kernel<TYPE, REST, CAP, 1024, 4, false>, 1024);
-        else if (bytes <= 256 * 4 * 16) go(distill_row_kernel<TYPE, REST, CAP, 256, 4, false>, 256);
-        else if (bytes <= 256 * 8 * 16) go(distill_row_kernel<TYPE, REST, CAP, 256, 8, false>, 256);
-        else if (bytes <= 256 * 16 * 16) go(distill_row_kernel<TYPE, REST, CAP, 256, 16, false>, 256);
-        else go(distill_row_kernel<TYPE, REST, CAP, 512, 16, true>, 512);
+        switch (icq_distill_row_form(a.R, a.V * SIZE, a.num_cu)) {
+            case ICQ_ROW_1024_4: go(distill_row_kernel<TYPE, REST, CAP, 1024, 4, false>, 1024); break;
+            case ICQ_ROW_256_4: go(distill_row_kernel<TYPE, REST, CAP, 256, 4, false>, 256); break;
+            case ICQ_ROW_256_8: go(distill_row_kernel<TYPE, REST, CAP, 256, 8, false>, 256); break;
+            case ICQ_ROW_256_16: go(distill_row_kernel<TYPE, REST, CAP, 256, 16, false>, 256); break;
+            case ICQ_ROW_LONG: go(distill_row_kernel<TYPE, REST, CAP, 512, 16, true>, 512); break;
+        }
         return;
     }
     const auto forward = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3((uint32_t)(a.R * a.splits)), dim3(threads), 0, s, a); };
-    // Whole rows of 256 KB and more by 512 threads (300 x 300000 f32: 74 us against 99 by 256, 1024 x 131072 bf16 53 and 55; shorter ones
-    // lose by it: 777 x 50021 f16 26.5 and 25.2, 8192 x 4096 f32 61 and 39).
-    if (a.splits == 1 && a.V * icq_type_bytes(TYPE) >= 262144) forward(distill_forward_kernel<TYPE, REST, CAP, 512>, 512);
+    if (icq_distill_forward_threads(a.splits, a.V * SIZE) == 512) forward(distill_forward_kernel<TYPE, REST, CAP, 512>, 512);
     else forward(distill_forward_kernel<TYPE, REST, CAP, T>, T);
     if (a.grad) launch_backward<TYPE, CAP>(a, a.splits > 1, s);
     else if (a.splits > 1) hipLaunchKernelGGL(HIP_KERNEL_NAME(distill_join_kernel<TYPE, CAP>), dim3((uint32_t)a.R), dim3(T), 0, s, a);
@@ -758,7 +746,7 @@ ICQ_EXPORT int icq_distill_workspace_bytes(int64_t R, int64_t V, size_t *out) {
     if (!out || R < 0 || R > ICQ_MAX_Q || V < 1 || V > ICQ_MAX_EXTENT) return ICQ_ERR_ARG;
     const int cu = icq_num_cu();
     if (cu <= 0) return ICQ_ERR_HIP;
-    *out = part_bytes(R, splits_of(R, V, cu, 0)) + part_bytes(R, 1);
+    *out = part_bytes(R, icq_distill_splits(R, V, cu, 0)) + part_bytes(R, 1);
     return ICQ_OK;
 }
 
@@ -771,14 +759,14 @@ ICQ_EXPORT int icq_distill(const void *logits, int type, int64_t R, int64_t V, i
     const int cu = icq_num_cu();
     if (cu <= 0) return ICQ_ERR_HIP;
     Distill a = params(logits, type, R, V, ld, scale, ids, values, topk, teacher_scale, teacher_lse);
-    const size_t parts = part_bytes(R, splits_of(R, V, cu, 0));
+    const size_t parts = part_bytes(R, icq_distill_splits(R, V, cu, 0));
     if (!workspace || (uintptr_t)workspace % ICQ_ALIGN != 0 || workspace_bytes < parts + part_bytes(R, 1)) return ICQ_ERR_WORKSPACE;
     a.part = static_cast<Part *>(workspace);
     a.loss = loss;
     a.stats = stats ? reinterpret_cast<float4 *>(stats) : reinterpret_cast<float4 *>(static_cast<char *>(workspace) + parts);
     a.grad_loss = grad_loss; a.grad = grad; a.ld_grad = ld_grad;
     a.num_cu = cu;
-    a.splits = splits_of(R, V, cu, grad && same_phase(a, icq_type_bytes(type)) ? V * icq_type_bytes(type) : 0);
+    a.splits = icq_distill_splits(R, V, cu, grad && same_phase(a, icq_type_bytes(type)) ? V * icq_type_bytes(type) : 0);
     hipStream_t s = static_cast<hipStream_t>(stream);
     const bool few = topk <= SHORT;
     ICQ_FOR_TYPE(type,
@@ -796,7 +784,7 @@ ICQ_EXPORT int icq_distill_backward(const void *logits, int type, int64_t R, int
     const int cu = icq_num_cu();
     if (cu <= 0) return ICQ_ERR_HIP;
     Distill a = params(logits, type, R, V, ld, scale, ids, values, topk, teacher_scale, teacher_lse);
-    a.splits = splits_of(R, V, cu, 0);
+    a.splits = icq_distill_splits(R, V, cu, 0);
     a.stats = reinterpret_cast<float4 *>(const_cast<float *>(stats));
     a.grad_loss = grad_loss; a.grad = grad; a.ld_grad = ld_grad;
     hipStream_t s = static_cast<hipStream_t>(stream);
