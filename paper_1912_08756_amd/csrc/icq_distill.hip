@@ -284,10 +284,20 @@ __device__ __forceinline__ void block_max2(float &a, float &b, float *red) {
 }
 
 // Block-wide, in a fixed order: the join of all threads' runs; REST: these are of what is off the list, and those listed items that `in`
-// takes join from the list.
+// takes join from the list.  listed: this thread's share of what the loss needs of the latter, sum of p (x - m) and sum of p.
 template <bool REST, int CAP, int N, typename In>
-__device__ __forceinline__ Sums block_run(const Run &a, const Distill &d, List<CAP> &l, In in) {
+__device__ __forceinline__ Sums block_run(const Run &a, const Distill &d, List<CAP> &l, In in, float (&listed)[2]) {
+    constexpr int PLACES = (CAP + N - 1) / N;
     Sums b = {a.m, 0.0f, a.m, 0.0f};
+    float x[PLACES], p[PLACES];                        // (p = -1: no item)
+#pragma unroll
+    for (int u = 0; u < PLACES; ++u) {
+        const int j = u * N + (int)threadIdx.x;
+        const bool here = j < d.topk && l.id[j] != ICQ_PAD_ID && in(l.id[j]);
+        x[u] = here ? l.x[j] : -INFINITY;
+        p[u] = here ? l.p[j] : -1.0f;
+        if (REST) b.m = fmaxf(b.m, x[u]);
+    }
     if constexpr (!REST) {
         float none = 0.0f;
         block_max_and_sum<N>(b.m, none, l.red);
@@ -296,38 +306,32 @@ __device__ __forceinline__ Sums block_run(const Run &a, const Distill &d, List<C
         b.s = v[0];
         b.mr = b.m;
     } else {
-        for (int j = threadIdx.x; j < d.topk; j += N)
-            if (l.id[j] != ICQ_PAD_ID && in(l.id[j])) b.m = fmaxf(b.m, l.x[j]);
         block_max2<N>(b.m, b.mr, l.red);
         float v[2] = {a.s * ex2((a.m - b.mr) * d.a2), 0.0f};
-        for (int j = threadIdx.x; j < d.topk; j += N)
-            if (l.id[j] != ICQ_PAD_ID && in(l.id[j])) v[1] += ex2((l.x[j] - b.m) * d.a2);
+#pragma unroll
+        for (int u = 0; u < PLACES; ++u) v[1] += ex2((x[u] - b.m) * d.a2);
         block_sums<N>(v, l.red);
         b.r = v[0];
         b.s = v[0] * ex2((b.mr - b.m) * d.a2) + v[1];
     }
+    listed[0] = listed[1] = 0.0f;
+#pragma unroll
+    for (int u = 0; u < PLACES; ++u)
+        if (!(p[u] == 0.0f) && !(p[u] == -1.0f)) {
+            listed[0] += p[u] * (x[u] - b.m);
+            listed[1] += p[u];
+        }
     return b;
 }
 
-// This thread's share of what the loss needs of those listed items that `in` takes, relative to the maximum m: sum of p (x - m), of p.
-template <int CAP, int N, typename In>
-__device__ __forceinline__ void listed_sum(const Distill &a, const List<CAP> &l, float m, float (&v)[2], In in) {
-    v[0] = v[1] = 0.0f;
-    for (int j = threadIdx.x; j < a.topk; j += N) {
-        const float p = l.p[j];
-        if (l.id[j] != ICQ_PAD_ID && !(p == 0.0f) && in(l.id[j])) {
-            v[0] += p * (l.x[j] - m);
-            v[1] += p;
-        }
-    }
-}
-
 // Loss and statistics of a row from its sums; listed: this thread's share of the sum of p (x - m).  All threads get the statistics.
+// may_rest: false where the kernel is one without the mass off the list; counts: whether the row has a loss.
 template <int CAP, int N>
-__device__ float4 finish_row(const Distill &a, int64_t row, List<CAP> &l, int entries, float sum_p, const Sums &run, float listed, bool write) {
+__device__ __forceinline__ float4 finish_row(const Distill &a, int64_t row, List<CAP> &l, int entries, float sum_p, const Sums &run, float listed, bool write,
+                                             bool may_rest, bool &counts) {
     const float log_s = logf(run.s);
-    const bool counts = entries > 0 && !(run.s == 0.0f);
-    const bool rest = a.teacher_lse && (int64_t)entries < a.V;
+    counts = entries > 0 && !(run.s == 0.0f);
+    const bool with_rest = may_rest && a.teacher_lse, rest = with_rest && (int64_t)entries < a.V;
     const float p_r = rest ? (sum_p > 1.0f ? 0.0f : 1.0f - sum_p) : 0.0f;
     // the sum off the list, zero where all of it is masked: it takes no gradient then (as it is, if that is NaN)
     const float r = run.mr > a.lowest ? run.r : 0.0f * run.r;
@@ -341,7 +345,7 @@ __device__ float4 finish_row(const Distill &a, int64_t row, List<CAP> &l, int en
     }
     // off the list q_v - p_r q_v / q_r = exp(scale (x_v - base)) factor
     float base = run.m, factor = 1.0f / run.s;
-    if (a.teacher_lse) {
+    if (with_rest) {
         base = run.mr;
         factor = r == 0.0f ? 0.0f : ex2((run.mr - run.m) * a.a2) / run.s - p_r / r;
     }
@@ -424,16 +428,20 @@ __device__ __forceinline__ void run_over(Run &run, const Distill &a, const List<
         const uint4 *at = body + b0;
         for (int i = done + (int)threadIdx.x; i < n; i += U * N) {
             uint4 w[U];
+            uint32_t on[U];                            // (from the LDS while the groups are on their way)
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                if (i + u * N < n) w[u] = at[i + u * N];
+                if (i + u * N < n) {
+                    const int e = (i + u * N) * PER;
+                    w[u] = at[i + u * N];
+                    on[u] = REST ? bits[e >> 5] >> (e & 31) : 0u;
+                }
 #pragma unroll
             for (int u = 0; u < U; ++u)
                 if (i + u * N < n) {
                     float y[PER];
                     E::unpack(w[u], y);
-                    const int e = (i + u * N) * PER;
-                    run_add<PER, REST>(run, y, REST ? bits[e >> 5] >> (e & 31) : 0u, a.a2);
+                    run_add<PER, REST>(run, y, on[u], a.a2);
                 }
         }
     }
@@ -451,8 +459,9 @@ __device__ __forceinline__ uint4 gradient_of(const uint4 &w, float m, float a2, 
 }
 
 // Sums of a row (splits == 1: and its loss) or of a slice of it.  REST: also those off the list.
+// (80 scalar registers: with two more, seven wavefronts share a SIMD instead of eight; 1024 x 131072 bf16 with a logsumexp 58 us against 51.)
 template <int TYPE, bool REST, int CAP, int N>
-__global__ __launch_bounds__(N) void distill_forward_kernel(Distill a) {
+__global__ __launch_bounds__(N) __attribute__((amdgpu_num_sgpr(80))) void distill_forward_kernel(Distill a) {
     typedef IcqElem<TYPE> E;
     constexpr int U = 8;
     __shared__ List<CAP> l;
@@ -463,7 +472,7 @@ __global__ __launch_bounds__(N) void distill_forward_kernel(Distill a) {
     float sum_p = 0.0f;
     const Span s = span_of<TYPE>(x, a.V);
     const Slice c = slice_of(s, k, a.splits);
-    const auto in = [&](uint32_t id) { return in_slice(s, c, id, E::PER); };
+    const auto in = [&](uint32_t id) { return a.splits == 1 || in_slice(s, c, id, E::PER); };
     const uint4 *body = reinterpret_cast<const uint4 *>(x + s.head);
     uint4 w[U];                                        // on their way while the list is worked on
 #pragma unroll
@@ -480,11 +489,11 @@ __global__ __launch_bounds__(N) void distill_forward_kernel(Distill a) {
     if (REST) mark<CAP, N>(a, l, s_bits, s.head + c.b0 * E::PER, c.b1 - c.b0 < CHUNK / E::PER ? (c.b1 - c.b0) * E::PER : CHUNK);
     run_held<TYPE, REST, N, U>(run, w, held, s_bits, a.a2);
     run_over<TYPE, REST, CAP, N>(run, a, l, s_bits, body, s.head, c.b0, held, c.b1);
-    const Sums sums = block_run<REST, CAP, N>(run, a, l, in);
     float v[2];
-    listed_sum<CAP, N>(a, l, sums.m, v, in);
+    const Sums sums = block_run<REST, CAP, N>(run, a, l, in, v);
     if (a.splits == 1) {
-        finish_row<CAP, N>(a, row, l, entries, sum_p, sums, v[0], true);
+        bool counts;
+        finish_row<CAP, N>(a, row, l, entries, sum_p, sums, v[0], true, REST, counts);
     } else {
         block_sums<N>(v, l.red);
         if (tid == 0) {
@@ -525,7 +534,8 @@ __global__ __launch_bounds__(T) void distill_join_kernel(Distill a) {
     float sum_p, listed;
     const int entries = load_list<TYPE, CAP, T>(a, row, nullptr, l, sum_p, [](uint32_t) { return false; });
     const Sums run = join_row<CAP, T>(a, row, l, listed);
-    finish_row<CAP, T>(a, row, l, entries, sum_p, run, listed, true);
+    bool counts;
+    finish_row<CAP, T>(a, row, l, entries, sum_p, run, listed, true, true, counts);
 }
 
 // The gradient of a slice of a row.  VEC: logits and gradient rows start at the same place within 16 bytes.
@@ -555,13 +565,15 @@ __global__ __launch_bounds__(T) void distill_backward_kernel(Distill a) {
     const auto in = [&](uint32_t id) { return in_slice(s, c, id, PER); };
     const int entries = load_list<TYPE, CAP, T>(a, row, x, l, sum_p, in);
     float4 st;
+    bool counts;
     if (JOIN) {
         const Sums run = join_row<CAP, T>(a, row, l, listed);
-        st = finish_row<CAP, T>(a, row, l, entries, sum_p, run, listed, k == 0);
+        st = finish_row<CAP, T>(a, row, l, entries, sum_p, run, listed, k == 0, true, counts);
     } else {
         st = a.stats[row];
+        counts = st.y != 0.0f;
     }
-    if (st.y == 0.0f) {                                // a row that does not count
+    if (!counts) {
         for (int64_t i = c.e0 + tid; i < c.e1; i += T) out[i < s.head ? i : i + s.body * PER] = E::put(0.0f);
         for (int64_t b = c.b0 + tid; b < c.b1; b += T) body_out[b] = make_uint4(0, 0, 0, 0);
         return;
@@ -638,12 +650,11 @@ __global__ __launch_bounds__(N, 4) void distill_row_kernel(Distill a) {
     if (REST) mark<CAP, N>(a, l, s_bits, s.head, s.body < CHUNK / PER ? s.body * PER : CHUNK);
     run_held<TYPE, REST, N, NV>(run, w, held, s_bits, a.a2);
     run_over<TYPE, REST, CAP, N>(run, a, l, s_bits, body, s.head, 0, held, s.body);
-    const Sums sums = block_run<REST, CAP, N>(run, a, l, [](uint32_t) { return true; });
     float v[2];
-    listed_sum<CAP, N>(a, l, sums.m, v, [](uint32_t) { return true; });
-    const float4 st = finish_row<CAP, N>(a, row, l, entries, sum_p, sums, v[0], true);
-    const bool counts = st.y != 0.0f;
-    const float g = g0 * a.scale, q0 = 1.0f / st.y, f = st.w * g;
+    const Sums sums = block_run<REST, CAP, N>(run, a, l, [](uint32_t) { return true; }, v);
+    bool counts;
+    const float4 st = finish_row<CAP, N>(a, row, l, entries, sum_p, sums, v[0], true, REST, counts);
+    const float g = g0 * a.scale, q0 = 1.0f / st.y, base = REST ? st.z : st.x, f = (REST ? st.w : q0) * g;      // (the same without the mass off the list)
     float mine[PLACES];
     uint32_t here[PLACES];
 #pragma unroll
@@ -654,10 +665,10 @@ __global__ __launch_bounds__(N, 4) void distill_row_kernel(Distill a) {
     }
     __syncthreads();
     const uint4 zero = make_uint4(0, 0, 0, 0);
-    if (single) out[v1] = E::put(counts ? ex2((y1[0] - st.z) * a.a2) * f : 0.0f);
+    if (single) out[v1] = E::put(counts ? ex2((y1[0] - base) * a.a2) * f : 0.0f);
 #pragma unroll
     for (int u = 0; u < NV; ++u)
-        if (u * N + tid < held) put_group<LONG>(body_out + u * N + tid, counts ? gradient_of<TYPE>(w[u], st.z, a.a2, f) : zero);
+        if (u * N + tid < held) put_group<LONG>(body_out + u * N + tid, counts ? gradient_of<TYPE>(w[u], base, a.a2, f) : zero);
     for (int64_t b = s.body - 1 - tid; b >= held; b -= U * N) {        // from the end: what was read last is nearest
         uint4 r[U];
 #pragma unroll
@@ -665,7 +676,7 @@ __global__ __launch_bounds__(N, 4) void distill_row_kernel(Distill a) {
             if (b - u * N >= held) r[u] = body[b - u * N];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (b - u * N >= held) put_group<LONG>(body_out + b - u * N, counts ? gradient_of<TYPE>(r[u], st.z, a.a2, f) : zero);
+            if (b - u * N >= held) put_group<LONG>(body_out + b - u * N, counts ? gradient_of<TYPE>(r[u], base, a.a2, f) : zero);
     }
     __syncthreads();
 #pragma unroll
