@@ -426,11 +426,15 @@ int icq_block_quantize(const void *x, int x_type, int64_t rows, int64_t cols, in
  *   out[m][n] = sum_kb sa[m][kb] sb[n][kb] sum_{k in block kb} a[m][k] b[n][k],
  * a [M][K] in blocks of 1 x 128, b [N][K] in blocks of b_block_rows x 128 (1 or
  * 128; with 128 the scale is sb[n / 128][kb]), scales and code rows laid out as
- * icq_block_quantize writes them (what the padding bytes hold does not matter).
+ * icq_block_quantize writes them (the bytes from a row's end to the next multiple
+ * of 16 are read; what they hold does not matter).
  * out [M][N] of out_type is rounded once from sums held in 32 bits; within
  * each eight neighbouring products of a 16-bit out, terms smaller than about
  * 2^-13 of the largest are lost (1.4e-5 of the result in the 2-norm for normal
- * values, below the result's rounding), a 32-bit out takes them all.  scaling =
+ * values, below the result's rounding; where large products cancel, what is
+ * lost can be more than the rounding of what is left), a 32-bit out takes them
+ * all.  A product sa sb of scales is formed in 32 bits by itself: it should lie
+ * between 2^-126 and 2^128, also where the codes are zero.  scaling =
  * ICQ_SCALES_POW2 promises that every scale is a power of two (as
  * icq_block_quantize makes them): the matrix instructions of a 16-bit out then
  * apply them, and of other scales only the exponent would count.
