@@ -501,6 +501,98 @@ int icq_distill_backward(const void *logits, int type, int64_t R, int64_t V, int
                          const float *stats, const float *grad_loss, void *grad, int64_t ld_grad, void *stream);
 
 /*
+ * Microscaled 4-bit floating point: blocks of 32 values that share a scale, a
+ * power of two.  A value's code is its sign, two bits of exponent and one of
+ * mantissa (0, 1/2, 1, 3/2, 2, 3, 4, 6: magnitudes' codes 0 to 7, sign 8); codes
+ * lie two to a byte, the first in the low half; a scale is a byte e that stands
+ * for 2^(e - 127), 255 for NaN.  A matrix [rows][cols] is held as codes [rows]
+ * [ceil(cols/2)] and scales [rows][ceil(cols/32)].  Code rows start on 16 bytes,
+ * scale rows on 4 (pointers and ld, in bytes, multiples of these, ICQ_ERR_ARG
+ * otherwise); a row's bytes up to the next multiple of 16 (4) belong to it: they
+ * are zeroed where the row is written, and may be read, whatever they hold, where
+ * it is read.
+ */
+#define ICQ_E2M1 3 /* a_type of icq_mx_matmul: codes */
+#define ICQ_MX_BLOCK 32
+/* scale from the largest magnitude a of a block: 2^(floor(log2 a) - 2), above 6 times which values saturate (up to 8 become 6), or the least power of two s
+   with a <= 6 s (2^125 at most) */
+#define ICQ_MX_FLOOR 0
+#define ICQ_MX_FIT 1
+
+/*
+ * Values x [rows][cols] to codes and scales.  With a the largest magnitude in a
+ * block, at least 2^-100, and s its scale by the rule `scaling`,
+ *     code = the value nearest to x / s, ties to the even code, 6 where it is
+ *     beyond; a zero keeps its sign.
+ * A block that holds an infinity or a NaN has scale NaN and codes 0.
+ * Either output or both (the other's pointers NULL), from one reading of x:
+ *   codes, scales: of x; block_rows = 1: a block is 32 values of a row;
+ *     block_rows = 32: the squares of 32 x 32 have one scale, repeated for their
+ *     rows, so that a matrix and its transpose hold the same values;
+ *   codes_t [cols][ceil(rows/2)], scales_t [cols][ceil(rows/32)]: of x's transpose.
+ */
+int icq_mx_quantize(const void *x, int x_type, int64_t rows, int64_t cols, int64_t ldx, int scaling, int block_rows, uint8_t *codes,
+                    int64_t ld_codes, uint8_t *scales, int64_t ld_scales, uint8_t *codes_t, int64_t ld_codes_t, uint8_t *scales_t,
+                    int64_t ld_scales_t, void *stream);
+
+/* out [rows][cols] of out_type: the values that codes and scales stand for, rounded once (exact in 32 bits and in bf16 where they are finite there) */
+int icq_mx_dequantize(const uint8_t *codes, int64_t ld_codes, const uint8_t *scales, int64_t ld_scales, int64_t rows, int64_t cols, void *out,
+                      int out_type, int64_t ldo, void *stream);
+
+/*
+ * Product of two such matrices along their rows, of whatever block_rows:
+ *   out[m][n] = sum_kb sa[m][kb] sb[n][kb] sum_{k in block kb} a[m][k] b[n][k],
+ * out [M][N] of out_type rounded once from sums held in 32 bits.  b [N][K] is
+ * held; a [M][K] is held (a_type ICQ_E2M1, lda in bytes), or given as values
+ * (a_type ICQ_F32, ICQ_F16 or ICQ_BF16, lda in elements, a_scales NULL) that are
+ * taken as icq_mx_quantize with `scaling` and block_rows = 1 would hold them; for few
+ * rows that costs no launch of its own.  With an odd K, what a row's last byte
+ * holds besides its last code does not matter.
+ * Rows with a NaN scale give NaN.  K = 0 gives zeros.
+ * workspace: icq_mx_matmul_workspace_bytes(M, N, K, a_type) bytes (may be 0:
+ * NULL), 256-byte aligned.
+ * With W held in squares of 32 x 32 as codes and codes_t, and G the gradient of
+ * the outputs: X W^T = (X, W), G W = (G, W's codes_t), G^T X = (G's codes_t, X's
+ * codes_t).
+ */
+int icq_mx_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K, int a_type, size_t *out /*host*/);
+int icq_mx_matmul(const void *a, int a_type, int64_t lda, const uint8_t *a_scales, int64_t ld_a_scales, int scaling, const uint8_t *b, int64_t ldb,
+                  const uint8_t *b_scales, int64_t ld_b_scales, int64_t M, int64_t N, int64_t K, void *out, int out_type, int64_t ldo, void *workspace,
+                  size_t workspace_bytes, void *stream);
+
+/*
+ * The global norm of many gradients, and clipping by it.  A list holds `count`
+ * matrices: addresses, types, rows, cols and ld (elements between rows; a
+ * tensor without gaps is one row), and where their clipped values go: outs NULL:
+ * in their place; else addresses of their own with out_types and ld_outs (all
+ * three given), of the same shape in any of the three types.  It keeps the
+ * addresses, not the memory, and stays good as long as the memory does.  What is written may share
+ * no memory with another matrix of the list, read or written; a matrix's own
+ * place, type and ld are allowed (ICQ_ERR_ARG otherwise).  The arrays are host
+ * memory.  Creation allocates and waits for a copy: not inside a captured graph.  A list
+ * works on the device that was current at its creation (ICQ_ERR_ARG elsewhere).
+ *
+ *   norm = scale * sqrt(sum of all squares), squares and sums in 64 bits, rounded once
+ *   factor = scale where norm <= max_norm, else scale * (max_norm / norm)  (NaN where norm is NaN)
+ *   out = g * factor, in 32 bits, rounded once more to out's type
+ * scale (finite, >= 0) undoes a loss scale; max_norm >= 0, may be +inf.
+ * With factor 1 and outputs in place nothing is read or written.
+ *
+ * icq_grad_norm writes norm [1]; icq_grad_clip reads it (what ranks have made of
+ * their norms, say); icq_grad_norm_clip does both.  Sums are in a fixed order: the
+ * same gradients give the same bits.  workspace: icq_grad_workspace_bytes(list)
+ * bytes, 256-byte aligned.
+ */
+typedef struct icq_grad_list icq_grad_list;
+int icq_grad_list_create(icq_grad_list **out /*host*/, const void *const *grads, const int *types, const int64_t *rows, const int64_t *cols,
+                         const int64_t *ld, void *const *outs, const int *out_types, const int64_t *ld_outs, int count, void *stream);
+void icq_grad_list_destroy(icq_grad_list *list);
+int icq_grad_workspace_bytes(const icq_grad_list *list, size_t *out /*host*/);
+int icq_grad_norm(const icq_grad_list *list, float scale, float *norm, void *workspace, size_t workspace_bytes, void *stream);
+int icq_grad_clip(const icq_grad_list *list, float scale, float max_norm, const float *norm, void *stream);
+int icq_grad_norm_clip(const icq_grad_list *list, float scale, float max_norm, float *norm, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Machine-limit probe, a measurement aid (nothing on the search path uses it): runs one of a few
  * plain kernels `reps` times on `stream`, WAITS for them, and reports the mean launch time in
  * milliseconds (*ms_out, host) and the work one launch did (*units_out, host): bytes read

@@ -55,6 +55,16 @@ SIGNATURES = {
     "icq_distill_workspace_bytes": (_i, [_i64, _i64, ctypes.POINTER(_sz)]),
     "icq_distill": (_i, [_vp, _i, _i64, _i64, _i64, _f, _vp, _vp, _i, _f, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _sz, _vp]),
     "icq_distill_backward": (_i, [_vp, _i, _i64, _i64, _i64, _f, _vp, _vp, _i, _f, _vp, _vp, _vp, _vp, _i64, _vp]),
+    "icq_mx_quantize": (_i, [_vp, _i, _i64, _i64, _i64, _i, _i, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp]),
+    "icq_mx_dequantize": (_i, [_vp, _i64, _vp, _i64, _i64, _i64, _vp, _i, _i64, _vp]),
+    "icq_mx_matmul_workspace_bytes": (_i, [_i64, _i64, _i64, _i, ctypes.POINTER(_sz)]),
+    "icq_mx_matmul": (_i, [_vp, _i, _i64, _vp, _i64, _i, _vp, _i64, _vp, _i64, _i64, _i64, _i64, _vp, _i, _i64, _vp, _sz, _vp]),
+    "icq_grad_list_create": (_i, [ctypes.POINTER(_vp)] + [_vp] * 8 + [_i, _vp]),
+    "icq_grad_list_destroy": (None, [_vp]),
+    "icq_grad_workspace_bytes": (_i, [_vp, ctypes.POINTER(_sz)]),
+    "icq_grad_norm": (_i, [_vp, _f, _vp, _vp, _sz, _vp]),
+    "icq_grad_clip": (_i, [_vp, _f, _f, _vp, _vp]),
+    "icq_grad_norm_clip": (_i, [_vp, _f, _f, _vp, _vp, _sz, _vp]),
     "icq_machine_probe": (_i, [_i, _vp, _sz, _i, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double), _vp]),
 }
 _lib = None
@@ -473,6 +483,202 @@ def icq_distill_backward(logits, ids, values, scale, teacher_scale, teacher_lse,
     if rc:
         _check(rc, "icq_distill_backward")
     return grad
+
+
+ICQ_E2M1, ICQ_MX_BLOCK = 3, 32
+ICQ_MX_FLOOR, ICQ_MX_FIT = 0, 1
+_MX_CODES = {torch.uint8: ICQ_E2M1, torch.float4_e2m1fn_x2: ICQ_E2M1}
+_MX_SCALES = {torch.uint8: 0, torch.float8_e8m0fnu: 0}
+
+
+def _here(t, name):
+    """A matrix of the current device: the work is enqueued on that device's stream."""
+    if t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError("%s is on another device than the current one" % name)
+
+
+def _mx_rows(t, dtypes, shape, step, name, written):
+    """(address, bytes between rows) of held codes or scales, whose rows take up whole `step` bytes of their own storage."""
+    ptr, _, ld = _rows(t, dtypes, shape, name)
+    _here(t, name)
+    rows, cols = t.shape
+    if rows == 1:
+        ld = -(-ld // step) * step                             # (the distance to a row that is not there)
+    if rows and cols and t.storage_offset() + (rows - 1) * ld + -(-cols // step) * step > t.untyped_storage().nbytes():
+        raise ValueError("%s ends before its last row's next multiple of %d bytes (see icq_mx_codes, icq_mx_scales)" % (name, step))
+    return ptr, ld
+
+
+def icq_mx_codes(rows, cols, device="cuda"):
+    """An uninitialised matrix for [rows][cols] values in 4 bits: uint8 [rows][ceil(cols/2)], rows start on 16 bytes."""
+    return torch.empty((rows, -(-cols // 32) * 16), dtype=torch.uint8, device=device)[:, :-(-cols // 2)]
+
+
+def icq_mx_scales(rows, cols, device="cuda"):
+    """An uninitialised matrix for their scales: uint8 [rows][ceil(cols/32)], rows start on 4 bytes."""
+    return torch.empty((rows, -(-cols // 128) * 4), dtype=torch.uint8, device=device)[:, :-(-cols // 32)]
+
+
+def icq_mx_quantize(x, codes, scales, codes_t=None, scales_t=None, block_rows=1, fit=False):
+    """x [rows][cols] f32 / f16 / bf16 -> codes [rows][ceil(cols/2)] and scales [rows][ceil(cols/32)] and / or those of its transpose (uint8,
+    float4_e2m1fn_x2, float8_e8m0fnu, see icq_mx_codes and icq_mx_scales; either pair may be None)."""
+    xp, x_type, ldx = _rows(x, _TYPES, None, "x")
+    _here(x, "x")
+    rows, cols = x.shape
+    cp = sp = tp = stp = None
+    ld = ld_s = ld_t = ld_st = 0
+    if codes is not None:
+        cp, ld = _mx_rows(codes, _MX_CODES, (rows, -(-cols // 2)), 16, "codes", True)
+        sp, ld_s = _mx_rows(scales, _MX_SCALES, (rows, -(-cols // ICQ_MX_BLOCK)), 4, "scales", True)
+    if codes_t is not None:
+        tp, ld_t = _mx_rows(codes_t, _MX_CODES, (cols, -(-rows // 2)), 16, "codes_t", True)
+        stp, ld_st = _mx_rows(scales_t, _MX_SCALES, (cols, -(-rows // ICQ_MX_BLOCK)), 4, "scales_t", True)
+    rc = (_lib or load()).icq_mx_quantize(xp, x_type, rows, cols, ldx, ICQ_MX_FIT if fit else ICQ_MX_FLOOR, block_rows, cp, ld, sp, ld_s, tp, ld_t, stp, ld_st,
+                                          _raw_stream())
+    if rc:
+        _check(rc, "icq_mx_quantize")
+
+
+def icq_mx_dequantize(codes, scales, out):
+    """out [rows][cols] f32 / f16 / bf16: the values of codes [rows][ceil(cols/2)] with scales [rows][ceil(cols/32)]."""
+    op, out_type, ldo = _rows(out, _TYPES, None, "out")
+    _here(out, "out")
+    rows, cols = out.shape
+    cp, ld = _mx_rows(codes, _MX_CODES, (rows, -(-cols // 2)), 16, "codes", False)
+    sp, ld_s = _mx_rows(scales, _MX_SCALES, (rows, -(-cols // ICQ_MX_BLOCK)), 4, "scales", False)
+    rc = (_lib or load()).icq_mx_dequantize(cp, ld, sp, ld_s, rows, cols, op, out_type, ldo, _raw_stream())
+    if rc:
+        _check(rc, "icq_mx_dequantize")
+    return out
+
+
+def icq_mx_matmul_workspace_bytes(M, N, K, a_dtype=None):
+    """a_dtype: the type of a's values, None where a is held."""
+    out = ctypes.c_size_t(0)
+    _check(load().icq_mx_matmul_workspace_bytes(M, N, K, ICQ_E2M1 if a_dtype is None else _TYPES[a_dtype], ctypes.byref(out)), "icq_mx_matmul_workspace_bytes")
+    return int(out.value)
+
+
+def icq_mx_matmul(a, a_scales, b, b_scales, out, workspace=None, K=None, fit=False):
+    """out [M][N] f32 / f16 / bf16 = a [M][K] times b [N][K] transposed; b is held (codes and scales), a is held too or, with a_scales None, given
+    as values (f32 / f16 / bf16) that are quantised on the way by the rule `fit`.  K: the row length, where it cannot be read off
+    a (values) and is not twice the bytes of a row of b."""
+    if K is None:
+        K = a.shape[1] if a_scales is None else 2 * b.shape[1]
+    bytes_, blocks = -(-K // 2), -(-K // ICQ_MX_BLOCK)
+    op, out_type, ldo = _rows(out, _TYPES, None, "out")
+    _here(out, "out")
+    M, N = out.shape
+    if a_scales is None:
+        ap, a_type, lda = _rows(a, _TYPES, (M, K), "a")
+        _here(a, "a")
+        sp, ld_s = None, 0
+    else:
+        a_type = ICQ_E2M1
+        ap, lda = _mx_rows(a, _MX_CODES, (M, bytes_), 16, "a", False)
+        sp, ld_s = _mx_rows(a_scales, _MX_SCALES, (M, blocks), 4, "a_scales", False)
+    bp, ldb = _mx_rows(b, _MX_CODES, (N, bytes_), 16, "b", False)
+    ep, ld_e = _mx_rows(b_scales, _MX_SCALES, (N, blocks), 4, "b_scales", False)
+    rc = (_lib or load()).icq_mx_matmul(ap, a_type, lda, sp, ld_s, ICQ_MX_FIT if fit else ICQ_MX_FLOOR, bp, ldb, ep, ld_e, M, N, K, op, out_type, ldo,
+                                        _ptr(workspace, torch.uint8, None, "workspace"), workspace.numel() if workspace is not None else 0, _raw_stream())
+    if rc:
+        _check(rc, "icq_mx_matmul")
+    return out
+
+
+class GradList:
+    """Owner of an icq_grad_list handle (destroyed with the object) and of references to its tensors."""
+
+    def __init__(self, handle, tensors):
+        self.handle, self.tensors = handle, tensors
+
+    def __del__(self):
+        h, self.handle = getattr(self, "handle", None), None
+        if h and _lib is not None:
+            _lib.icq_grad_list_destroy(h)
+
+
+def _without_gaps(t):
+    """Whether a tensor's values fill a stretch of memory, in whatever order of its axes."""
+    n = 1
+    for stride, size in sorted((st, sz) for st, sz in zip(t.stride(), t.shape) if sz > 1):
+        if stride != n:
+            return False
+        n *= size
+    return True
+
+
+def _same_order(t, u):
+    return all(a == b for a, b, n in zip(t.stride(), u.stride(), t.shape) if n > 1)
+
+
+def icq_grad_list_create(grads, outs=None):
+    """GradList of gradients (f32 / f16 / bf16 tensors without gaps, or matrices with contiguous rows); outs: where their clipped values go,
+    tensors of the same shapes and orders of axes, of any of the three types; None: in their place."""
+    grads, outs = list(grads), None if outs is None else list(outs)
+    if outs is not None and len(outs) != len(grads):
+        raise ValueError("%d outs for %d gradients" % (len(outs), len(grads)))
+    rows = []                                                  # address, type, rows, cols, ld; address, type, ld of the out
+    for k, g in enumerate(grads):
+        out = g if outs is None else outs[k]
+        for t, name in ((g, "grads[%d]" % k), (out, "outs[%d]" % k)):
+            if t.dtype not in _TYPES or not t.is_cuda:
+                raise TypeError("%s must be a CUDA tensor of %s" % (name, ", ".join(str(d) for d in _TYPES)))
+            _here(t, name)
+        if out.shape != g.shape:
+            raise ValueError("outs[%d] has shape %s, expected %s" % (k, tuple(out.shape), tuple(g.shape)))
+        n = g.numel()
+        if n == 0 or (_without_gaps(g) and _without_gaps(out) and _same_order(g, out)):
+            rows.append((g.data_ptr(), _TYPES[g.dtype], 1, n, n, out.data_ptr(), _TYPES[out.dtype], n))
+        elif g.dim() == 2:
+            gp, gt, ld = _rows(g, _TYPES, None, "grads[%d]" % k)
+            op, ot, ldo = _rows(out, _TYPES, None, "outs[%d]" % k)
+            rows.append((gp, gt, g.shape[0], g.shape[1], ld, op, ot, ldo))
+        else:
+            raise ValueError("grads[%d] must have no gaps, and outs[%d] the same order of axes" % (k, k))
+    column = lambda i, kind: (kind * len(rows))(*(r[i] for r in rows))  # noqa: E731
+    h = ctypes.c_void_p(0)
+    rc = load().icq_grad_list_create(ctypes.byref(h), column(0, _vp), column(1, _i), column(2, _i64), column(3, _i64), column(4, _i64),
+                                     None if outs is None else column(5, _vp), column(6, _i), column(7, _i64), len(rows), _raw_stream())
+    _check(rc, "icq_grad_list_create")
+    return GradList(h, (grads, outs))
+
+
+def icq_grad_list_destroy(list):
+    h, list.handle = list.handle, None
+    if h:
+        load().icq_grad_list_destroy(h)
+
+
+def icq_grad_workspace_bytes(list):
+    out = ctypes.c_size_t(0)
+    _check(load().icq_grad_workspace_bytes(list.handle, ctypes.byref(out)), "icq_grad_workspace_bytes")
+    return int(out.value)
+
+
+def icq_grad_norm(list, norm, workspace, scale=1.0):
+    """norm [1] f32 = scale times the global norm of the list's gradients."""
+    rc = (_lib or load()).icq_grad_norm(list.handle, scale, _ptr(norm, torch.float32, (1,), "norm"), _ptr(workspace, torch.uint8, None, "workspace"), workspace.numel(),
+                                        _raw_stream())
+    if rc:
+        _check(rc, "icq_grad_norm")
+    return norm
+
+
+def icq_grad_clip(list, norm, max_norm, scale=1.0):
+    """The gradients times scale, and times max_norm / norm where norm [1] f32 is over max_norm."""
+    rc = (_lib or load()).icq_grad_clip(list.handle, scale, max_norm, _ptr(norm, torch.float32, (1,), "norm"), _raw_stream())
+    if rc:
+        _check(rc, "icq_grad_clip")
+
+
+def icq_grad_norm_clip(list, norm, max_norm, workspace, scale=1.0):
+    """icq_grad_norm, then icq_grad_clip."""
+    rc = (_lib or load()).icq_grad_norm_clip(list.handle, scale, max_norm, _ptr(norm, torch.float32, (1,), "norm"), _ptr(workspace, torch.uint8, None, "workspace"),
+                                             workspace.numel(), _raw_stream())
+    if rc:
+        _check(rc, "icq_grad_norm_clip")
+    return norm
 
 
 ICQ_PROBE_READ, ICQ_PROBE_READ_NT, ICQ_PROBE_LDS_B32, ICQ_PROBE_LDS_B64, ICQ_PROBE_LDS_B128, ICQ_PROBE_VALU, \

@@ -78,3 +78,6 @@ __device__ __forceinline__ uint4 first_bytes(const uint4 &v, int n) {
 int icq_launch_product_tiles(const Product &p, icq_tiles tiles, int a_format, int b_format, bool rows, bool pow2, int out_type, hipStream_t s);
 // The product of few rows of a (icq_matmul_few.hip).
 int icq_launch_product_few(const Product &p, int num_cu, int a_format, int b_format, bool rows, int out_type, hipStream_t s);
+// The splits' partial sums into the result; of no splits, zeros (icq_matmul.hip).
+int icq_launch_product_join(const Product &p, int out_type, hipStream_t s);
+bool icq_product_extents_ok(int64_t M, int64_t N, int64_t K);

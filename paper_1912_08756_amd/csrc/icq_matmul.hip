@@ -13,6 +13,8 @@
 // the 16-bit ones, which hold 32, over codes widened to bf16 (exact for both formats).
 #include "icq_matmul.h"
 
+#include <algorithm>
+
 namespace {
 
 // The splits' partial sums added in order; four columns a thread.
@@ -38,15 +40,33 @@ __global__ __launch_bounds__(256) void product_join_kernel(Product p) {
     store4<TYPE>(p, m, n, s);
 }
 
-bool extents_ok(int64_t M, int64_t N, int64_t K) {
+}  // namespace
+
+bool icq_product_extents_ok(int64_t M, int64_t N, int64_t K) {
     return M >= 0 && N >= 0 && K >= 0 && M <= ICQ_MAX_EXTENT && N <= ICQ_MAX_EXTENT && K <= ICQ_MAX_EXTENT &&
            ((M + 63) / 64) * ((N + 63) / 64) <= 0x7fffffff;
 }
 
-}  // namespace
+int icq_launch_product_join(const Product &p, int out_type, hipStream_t s) {
+    const auto go = [&](const Product &q) {
+        const dim3 by_four((uint32_t)((q.N + 1023) / 1024), (uint32_t)(q.M < 32768 ? q.M : 32768), (uint32_t)((q.M + 32767) / 32768));
+        ICQ_FOR_TYPE(out_type, hipLaunchKernelGGL(HIP_KERNEL_NAME(product_join_kernel<TYPE>), by_four, dim3(256), 0, s, q))
+    };
+    if (p.splits > 0) go(p);                                                  // (few tiles, then: far from a launch's 2^32 threads)
+    else {
+        const int64_t step = std::max<int64_t>(1, ICQ_PRODUCT_BLOCKS / ((p.N + 1023) / 1024));
+        for (int64_t m = 0; m < p.M; m += step) {
+            Product q = p;
+            q.M = std::min(step, p.M - m);
+            q.out = static_cast<char *>(p.out) + m * p.ldo * icq_type_bytes(out_type);
+            go(q);
+        }
+    }
+    return icq_check_launch();
+}
 
 ICQ_EXPORT int icq_block_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K, size_t *out) {
-    if (!out || !extents_ok(M, N, K)) return ICQ_ERR_ARG;
+    if (!out || !icq_product_extents_ok(M, N, K)) return ICQ_ERR_ARG;
     const int cu = icq_num_cu();
     if (cu <= 0) return ICQ_ERR_HIP;
     const int fast = icq_plan_product(M, N, K, false, cu).splits, exact = icq_plan_product(M, N, K, true, cu).splits, splits = fast > exact ? fast : exact;
@@ -59,7 +79,7 @@ ICQ_EXPORT int icq_block_matmul(const uint8_t *a, int a_format, int64_t lda, con
                                 void *out, int out_type, int64_t ldo, void *workspace, size_t workspace_bytes, void *stream) {
     const int size = icq_type_bytes(out_type);
     if (size == 0 || (a_format != ICQ_E4M3 && a_format != ICQ_E5M2) || (b_format != ICQ_E4M3 && b_format != ICQ_E5M2) ||
-        (scaling != ICQ_SCALES_F32 && scaling != ICQ_SCALES_POW2) || (b_block_rows != 1 && b_block_rows != ICQ_BLOCK) || !extents_ok(M, N, K))
+        (scaling != ICQ_SCALES_F32 && scaling != ICQ_SCALES_POW2) || (b_block_rows != 1 && b_block_rows != ICQ_BLOCK) || !icq_product_extents_ok(M, N, K))
         return ICQ_ERR_ARG;
     if (M == 0 || N == 0) return ICQ_OK;
     if (!out || (uintptr_t)out % size != 0 || ldo < N) return ICQ_ERR_ARG;
@@ -78,11 +98,9 @@ ICQ_EXPORT int icq_block_matmul(const uint8_t *a, int a_format, int64_t lda, con
     p.per = (p.kb + p.splits - 1) / p.splits;
     p.part = static_cast<float *>(workspace);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const dim3 by_four((uint32_t)((N + 1023) / 1024), (uint32_t)(M < 32768 ? M : 32768), (uint32_t)((M + 32767) / 32768));
     if (K == 0) {
         p.splits = 0;                                                         // (a sum of nothing)
-        ICQ_FOR_TYPE(out_type, hipLaunchKernelGGL(HIP_KERNEL_NAME(product_join_kernel<TYPE>), by_four, dim3(256), 0, s, p))
-        return icq_check_launch();
+        return icq_launch_product_join(p, out_type, s);
     }
     if (p.splits > 1 && (!workspace || (uintptr_t)workspace % ICQ_ALIGN != 0 || workspace_bytes < (size_t)p.splits * M * N * sizeof(float)))
         return ICQ_ERR_WORKSPACE;
@@ -90,6 +108,5 @@ ICQ_EXPORT int icq_block_matmul(const uint8_t *a, int a_format, int64_t lda, con
     const int rc = plan.few ? icq_launch_product_few(p, cu, a_format, b_format, rows, out_type, s)
                             : icq_launch_product_tiles(p, plan.tiles, a_format, b_format, rows, scaling == ICQ_SCALES_POW2, out_type, s);
     if (rc != ICQ_OK || p.splits == 1) return rc;
-    ICQ_FOR_TYPE(out_type, hipLaunchKernelGGL(HIP_KERNEL_NAME(product_join_kernel<TYPE>), by_four, dim3(256), 0, s, p))
-    return icq_check_launch();
+    return icq_launch_product_join(p, out_type, s);
 }

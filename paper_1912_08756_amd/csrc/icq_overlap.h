@@ -20,3 +20,35 @@ static inline bool icq_rows_overlap(uintptr_t a, int64_t lda, uintptr_t b, int64
         if (meets(i)) return true;
     return false;
 }
+
+// Rows of `len` bytes every `ld` from an address on.
+struct icq_extent {
+    uintptr_t from;
+    int64_t rows, ld, len;
+};
+
+static inline bool icq_extents_overlap(const icq_extent &a, const icq_extent &b) {
+    if (a.rows <= 0 || b.rows <= 0 || a.len <= 0 || b.len <= 0) return false;
+    const __int128 end_a = (__int128)a.from + (__int128)(a.rows - 1) * a.ld + a.len, end_b = (__int128)b.from + (__int128)(b.rows - 1) * b.ld + b.len;
+    if (end_a <= (__int128)b.from || end_b <= (__int128)a.from) return false;
+    if (a.rows > 1 && b.rows > 1 && a.ld == b.ld) {
+        // parts of the same long rows, which meet in some row unless their places within a row are apart
+        const icq_extent &x = a.from <= b.from ? a : b, &y = a.from <= b.from ? b : a;
+        const int64_t d = (int64_t)((__int128)(y.from - x.from) % x.ld);
+        return d < x.len || d + y.len > x.ld;
+    }
+    // each row of the one with fewer rows against the other's rows around its start and up to its end
+    const icq_extent &x = a.rows <= b.rows ? b : a, &y = a.rows <= b.rows ? a : b;
+    for (int64_t i = 0; i < y.rows; ++i) {
+        const __int128 from = (__int128)y.from + (__int128)i * y.ld, off = from - (__int128)x.from;
+        if (x.rows == 1) {
+            if (off < x.len && off + y.len > 0) return true;
+            continue;
+        }
+        __int128 k = off >= 0 ? off / x.ld : 0;                                // the last row of x that starts at or before it, or the first
+        if (k >= x.rows) k = x.rows - 1;
+        if (off < k * x.ld + x.len && off + y.len > k * x.ld) return true;
+        if (k + 1 < x.rows && off + y.len > (k + 1) * x.ld && off < (k + 1) * x.ld + x.len) return true;
+    }
+    return false;
+}

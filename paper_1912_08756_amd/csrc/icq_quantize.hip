@@ -11,7 +11,7 @@
 // lanes that hold a block agreeing on its largest value: 8192 x 8192 bf16 42 us, 4.8 TB/s; f32 57 us, 5.8 TB/s.  Columns need
 // a 128 x 128 tile in registers, whose codes turn round in the LDS so that either output is written in whole 128-byte pieces:
 // 8192 x 16000 bf16 both ways 117 us, 4.6 TB/s; 10007 x 4096 f32 in 128 x 128 blocks both ways 49.5 us, 5.0 TB/s.
-#include "icq_types.h"
+#include "icq_eight.h"
 
 namespace {
 
@@ -92,25 +92,6 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(Quantize a, int64_t 
     if ((threadIdx.x & 15u) == 0) a.scales[r * a.across + block] = s;
 }
 
-// Eight values of one row as they were loaded, and the bits of their magnitudes: pairs of halves, or words.
-template <int TYPE>
-struct Eight {
-    static constexpr int WORDS = TYPE == ICQ_F32 ? 8 : 4;
-    uint32_t w[WORDS];
-};
-
-typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-
-// The larger magnitudes, pair by pair or word by word.
-template <int TYPE>
-__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
-    if constexpr (TYPE == ICQ_F32) return max(a, b);
-    else return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
-}
-
-template <int TYPE>
-__device__ __forceinline__ uint32_t magnitude(uint32_t w) { return w & (TYPE == ICQ_F32 ? 0x7fffffffu : 0x7fff7fffu); }
-
 // Magnitudes' bits of infinities and NaN replaced by zero.
 template <int TYPE>
 __device__ __forceinline__ uint32_t finite_only(uint32_t m) {
@@ -121,14 +102,6 @@ __device__ __forceinline__ uint32_t finite_only(uint32_t m) {
     }
 }
 
-// A magnitude's bits as those of a float.
-template <int TYPE>
-__device__ __forceinline__ uint32_t float_bits(uint32_t half) {
-    if constexpr (TYPE == ICQ_F32) return half;
-    else if constexpr (TYPE == ICQ_F16) return __float_as_uint((float)__builtin_bit_cast(_Float16, (uint16_t)half));
-    else return half << 16;
-}
-
 // The largest of 16 neighbouring lanes, in all of them.
 template <int TYPE>
 __device__ __forceinline__ uint32_t largest_of_16(uint32_t m) {
@@ -136,31 +109,6 @@ __device__ __forceinline__ uint32_t largest_of_16(uint32_t m) {
     m = larger<TYPE>(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x124, 0xf, 0xf, true));
     m = larger<TYPE>(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x122, 0xf, 0xf, true));
     return larger<TYPE>(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x121, 0xf, 0xf, true));
-}
-
-template <int TYPE>
-__device__ __forceinline__ Eight<TYPE> read8(const Quantize &a, int64_t r, int64_t c) {
-    typedef typename IcqElem<TYPE>::raw raw;
-    Eight<TYPE> v;
-#pragma unroll
-    for (int i = 0; i < Eight<TYPE>::WORDS; ++i) v.w[i] = 0;
-    if (r >= a.rows) return v;
-    const raw *p = static_cast<const raw *>(a.x) + r * a.ldx + c;
-    if (c + 8 <= a.cols) __builtin_memcpy(v.w, p, sizeof v.w);
-    else
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (c + i < a.cols) {
-                if constexpr (TYPE == ICQ_F32) v.w[i] = __float_as_uint(p[i]);
-                else v.w[i >> 1] |= (uint32_t)__builtin_bit_cast(uint16_t, p[i]) << (16 * (i & 1));
-            }
-    return v;
-}
-
-template <int TYPE>
-__device__ __forceinline__ void values8(const Eight<TYPE> &v, float *x) {
-#pragma unroll
-    for (int h = 0; h < Eight<TYPE>::WORDS / 4; ++h) IcqElem<TYPE>::unpack(make_uint4(v.w[4 * h], v.w[4 * h + 1], v.w[4 * h + 2], v.w[4 * h + 3]), x + 4 * h);
 }
 
 // A 128 x 128 tile per block; thread (g, h) holds rows 4 h .. 4 h + 3 of columns 8 g .. 8 g + 7.
@@ -179,7 +127,7 @@ __global__ __launch_bounds__(512) void quantize_tile_kernel(Quantize a, uint32_t
     const int64_t r0 = (int64_t)br * 128 + 4 * h, c0 = (int64_t)bc * 128 + 8 * g;
     Eight<TYPE> v[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = read8<TYPE>(a, r0 + i, c0);
+    for (int i = 0; i < 4; ++i) v[i] = read8<TYPE>(a.x, a.rows, a.cols, a.ldx, r0 + i, c0);
     uint32_t col[WORDS], row[4];
     const auto largest = [&](auto bits) {
 #pragma unroll

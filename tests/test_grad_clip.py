@@ -1,0 +1,328 @@
+"""The global norm of many gradients and clipping by it, against plain 64-bit forms."""
+import ctypes
+
+import numpy as np
+import pytest
+
+import mx_reference as ref
+from test_host_rules import _run as _compiled
+
+gpu = pytest.mark.gpu
+
+
+def _torch():
+    import torch
+    from paper_1912_08756_amd import binding
+    binding.load()
+    return torch, binding
+
+
+def _types(torch):
+    return {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+
+
+def _np(t):
+    return t.double().cpu().numpy()
+
+
+def _space(torch, b, lst):
+    return torch.empty(b.icq_grad_workspace_bytes(lst), dtype=torch.uint8, device="cuda")
+
+
+def _bits(torch, t):
+    return t.contiguous().view({4: torch.int32, 2: torch.int16}[t.element_size()])
+
+
+def _check(torch, grads, before, outs, norm, max_norm, scale):
+    """Norm: squares and sums in 64 bits (2^-50 at most for these numbers of terms), one rounding.  Values: the factor's two roundings (quotient, product),
+    the product's, and the result's."""
+    want = ref.norm(before, scale)
+    got = float(norm)
+    if not np.isfinite(want) or want > np.finfo(np.float32).max:
+        assert got == want or (np.isnan(got) and np.isnan(want)) or np.isinf(got)
+    else:
+        assert abs(got - want) <= (2.0 ** -24 + 2.0 ** -49) * want + 2.0 ** -149
+    if outs is None:
+        return
+    f = ref.factor(got, max_norm, scale)
+    for g, o in zip(before, outs):
+        info = torch.finfo(o.dtype)
+        half, least = info.eps / 2, info.smallest_normal * info.eps
+        with np.errstate(all="ignore"):
+            exact = g.astype(np.float64) * f
+        have = _np(o)
+        fine = np.abs(exact) < float(info.max)
+        assert np.array_equal(np.isnan(have), np.isnan(exact))
+        fine &= ~np.isnan(exact)
+        off = np.abs(have[fine] - exact[fine])
+        # (a factor or product below the normal numbers of 32 bits is rounded to a multiple of 2^-149)
+        assert (off <= (3 * 2.0 ** -24 + half) * (1 + 2.0 ** -20) * np.abs(exact[fine]) + least + 2.0 ** -149 * (1 + np.abs(g[fine]))).all()
+
+
+SETS = {"one value": [(1,)], "short": [(3,), (7,), (8,), (9,), (1, 1), (2, 3, 4)], "a chunk and around": [(16384,), (16383,), (16385,), (32769,)],
+        "many": [(k % 37 + 1, k % 11 + 1) for k in range(700)], "long": [(3_000_001,), (257, 4099)], "empty among others": [(0,), (5,), (0, 3), (4, 0), (11,)]}
+
+
+@gpu
+@pytest.mark.parametrize("shapes", SETS.values(), ids=SETS.keys())
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("out", ["in place", "f32", "f16", "bf16"])
+@pytest.mark.parametrize("above", [False, True])
+def test_norm_and_clipped_values(shapes, kind, out, above):
+    torch, b = _torch()
+    g = torch.Generator().manual_seed(len(shapes))
+    grads = [(torch.randn(s, generator=g) * float(torch.exp2(4 * torch.rand((), generator=g)))).to(_types(torch)[kind]).cuda() for s in shapes]
+    before = [_np(x) for x in grads]
+    outs = None if out == "in place" else [torch.full(s, -7.0, dtype=_types(torch)[out], device="cuda") for s in shapes]
+    lst = b.icq_grad_list_create(grads, outs)
+    scale = 0.25
+    max_norm = float(np.float32(ref.norm(before, scale) * (0.3 if above else 1.5)))
+    norm, space = torch.full((1,), -1.0, device="cuda"), _space(torch, b, lst)
+    b.icq_grad_norm(lst, norm, space, scale=scale)
+    _check(torch, grads, before, None, norm, max_norm, scale)
+    assert all(np.array_equal(_np(x), y) for x, y in zip(grads, before))
+    first = norm.clone()
+    norm.fill_(-1.0)
+    b.icq_grad_norm_clip(lst, norm, max_norm, space, scale=scale)
+    assert torch.equal(_bits(torch, norm), _bits(torch, first))
+    _check(torch, grads, before, outs or grads, norm, max_norm, scale)
+    # the same in two calls, bit for bit
+    again = [torch.from_numpy(y).to(x.dtype).cuda() for x, y in zip(grads, before)]
+    to = None if outs is None else [torch.full_like(o, -9.0) for o in outs]
+    other = b.icq_grad_list_create(again, to)
+    b.icq_grad_norm(other, norm, _space(torch, b, other), scale=scale)
+    b.icq_grad_clip(other, norm, max_norm, scale=scale)
+    for x, y in zip(to or again, outs or grads):
+        assert torch.equal(_bits(torch, x), _bits(torch, y))
+
+
+@gpu
+def test_a_factor_of_one_leaves_gradients_as_they_are_and_copies_them():
+    torch, b = _torch()
+    x = [torch.randn((1000,), device="cuda").bfloat16(), torch.randn((77, 3), device="cuda")]
+    x[1][5, 1] = 3e-41                                         # below the normal numbers
+    keep = [t.clone() for t in x]
+    norm = torch.empty((1,), device="cuda")
+    lst = b.icq_grad_list_create(x)
+    b.icq_grad_norm_clip(lst, norm, float("inf"), _space(torch, b, lst))
+    assert all(torch.equal(_bits(torch, t), _bits(torch, u)) for t, u in zip(x, keep))
+    b.icq_grad_clip(lst, norm, float(norm))                    # at the bound: not over it
+    assert all(torch.equal(_bits(torch, t), _bits(torch, u)) for t, u in zip(x, keep))
+    outs = [torch.empty((1000,), device="cuda"), torch.empty((77, 3), device="cuda")]
+    lst = b.icq_grad_list_create(x, outs)
+    b.icq_grad_norm_clip(lst, norm, 1e30, _space(torch, b, lst))
+    assert torch.equal(outs[0], keep[0].float()) and torch.equal(_bits(torch, outs[1]), _bits(torch, keep[1]))
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_magnitudes_whose_squares_leave_32_bits(kind):
+    torch, b = _torch()
+    dtype = _types(torch)[kind]
+    for size in (1e-38, 1e-30, 1e25, 1e35):
+        x = [(torch.randn((5000,), generator=torch.Generator().manual_seed(1)) * size).to(dtype).cuda(), torch.zeros((9,), dtype=dtype, device="cuda")]
+        before = [_np(t) for t in x]
+        norm, lst = torch.empty((1,), device="cuda"), b.icq_grad_list_create(x)
+        b.icq_grad_norm_clip(lst, norm, 1.0, _space(torch, b, lst))
+        _check(torch, x, before, x, norm, 1.0, 1.0)
+
+
+@gpu
+def test_infinities_nan_and_zeros():
+    torch, b = _torch()
+    norm = torch.empty((1,), device="cuda")
+    for bad, want in ((float("nan"), float("nan")), (float("inf"), float("inf"))):
+        x = [torch.ones((300,), device="cuda"), torch.ones((50,), device="cuda").half()]
+        x[1][7] = bad
+        lst = b.icq_grad_list_create(x)
+        b.icq_grad_norm_clip(lst, norm, 1.0, _space(torch, b, lst))
+        if np.isnan(want):
+            assert np.isnan(float(norm)) and all(bool(torch.isnan(t).all()) for t in x)
+        else:
+            assert float(norm) == want and not x[0].any() and bool(torch.isnan(x[1][7])) and not x[1][:7].any()
+    x = [torch.zeros((300,), device="cuda")]
+    lst = b.icq_grad_list_create(x)
+    b.icq_grad_norm_clip(lst, norm, 0.0, _space(torch, b, lst))
+    assert float(norm) == 0.0 and not x[0].any()
+    x[0].fill_(2.0)
+    b.icq_grad_norm_clip(lst, norm, 0.0, _space(torch, b, lst))
+    assert float(norm) > 0 and not x[0].any()                  # a bound of zero
+    x[0].fill_(2.0)
+    b.icq_grad_norm_clip(lst, norm, 1.0, _space(torch, b, lst), scale=0.0)
+    assert float(norm) == 0.0 and not x[0].any()
+    none = b.icq_grad_list_create([])
+    b.icq_grad_norm_clip(none, norm.fill_(-1), 1.0, _space(torch, b, none))
+    assert float(norm) == 0.0
+    b.icq_grad_clip(none, norm, 1.0)
+
+
+@gpu
+def test_a_norm_from_elsewhere():
+    """What ranks have made of their norms."""
+    torch, b = _torch()
+    x = [torch.full((100,), 3.0, device="cuda")]
+    lst = b.icq_grad_list_create(x)
+    b.icq_grad_clip(lst, torch.full((1,), 12.0, device="cuda"), 4.0, scale=0.5)
+    assert torch.equal(x[0], torch.full((100,), 3.0 * np.float32(0.5) * (np.float32(4) / np.float32(12)), device="cuda"))
+
+
+@gpu
+@pytest.mark.parametrize("out", [False, True])
+def test_rows_of_wider_buffers_values_in_other_orders_and_odd_addresses(out):
+    torch, b = _torch()
+    g = torch.Generator(device="cuda").manual_seed(3)
+    wide = torch.randn((300, 130), device="cuda", generator=g).bfloat16()
+    flat = torch.randn((50_003,), device="cuda", generator=g)
+    kernel = torch.randn((4, 6, 5, 3), device="cuda", generator=g).to(memory_format=torch.channels_last)
+    tall = torch.randn((9000, 5), device="cuda", generator=g).half()
+    long = torch.randn((3, 40_000), device="cuda", generator=g)
+    grads = [wide[:, 1:60], wide[::2, 64:127], flat[1:20_000], flat[20_000:], kernel, tall[:, 1:4], long[:, 3:39_990], torch.randn((70, 90), device="cuda", generator=g).t()]
+    if out:
+        buffer = torch.full((300, 200), -7.0, device="cuda")
+        outs = [buffer[:, 3:62], buffer[1:151, 100:163], torch.empty((20_001,), device="cuda")[1:20_000], torch.empty((30_004,), device="cuda", dtype=torch.half)[1:],
+                torch.empty_like(kernel), torch.empty((9000, 3), device="cuda"), torch.empty((3, 39_987), device="cuda").bfloat16(), torch.empty((70, 90), device="cuda").t()]
+    before, keep = [_np(t) for t in grads], wide.clone()
+    lst = b.icq_grad_list_create(grads, outs if out else None)
+    norm = torch.empty((1,), device="cuda")
+    b.icq_grad_norm_clip(lst, norm, 5.0, _space(torch, b, lst))
+    _check(torch, grads, before, outs if out else grads, norm, 5.0, 1.0)
+    assert torch.equal(wide[:, 0], keep[:, 0]) and torch.equal(wide[:, 60:64], keep[:, 60:64]) and torch.equal(wide[1::2, 64:], keep[1::2, 64:]) and torch.equal(wide[:, 127:], keep[:, 127:])
+    if out:
+        assert (buffer[:, :3] == -7).all() and (buffer[:, 62:100] == -7).all() and (buffer[:, 163:] == -7).all() and (buffer[0, 100:163] == -7).all()
+        assert all(np.array_equal(_np(t), y) for t, y in zip(grads, before))
+
+
+@gpu
+def test_captured_and_replayed_with_eager_work_between():
+    torch, b = _torch()
+    x = [torch.randn((40_000,), device="cuda"), torch.randn((31, 17), device="cuda").bfloat16()]
+    lst, norm = b.icq_grad_list_create(x), torch.empty((1,), device="cuda")
+    space = _space(torch, b, lst)
+    b.icq_grad_norm_clip(lst, norm, 1.0, space)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.icq_grad_norm_clip(lst, norm, 1.0, space)
+    for seed in range(4):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        fresh = [torch.randn(t.shape, device="cuda", generator=g).to(t.dtype) for t in x]
+        for t, u in zip(x, fresh):
+            t.copy_(u)
+        before = [_np(t) for t in x]
+        graph.replay()
+        torch.cuda.synchronize()
+        _check(torch, x, before, x, norm, 1.0, 1.0)
+        got = [t.clone() for t in x]
+        for t, u in zip(x, fresh):
+            t.copy_(u)
+        b.icq_grad_norm_clip(lst, norm, 1.0, space)
+        assert all(torch.equal(t, u) for t, u in zip(x, got))
+
+
+@gpu
+def test_on_a_stream_of_its_own():
+    torch, b = _torch()
+    x = [torch.randn((1 << 20,), device="cuda")]
+    before = [_np(x[0])]
+    lst, norm = b.icq_grad_list_create(x), torch.empty((1,), device="cuda")
+    space, s = _space(torch, b, lst), torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        b.icq_grad_norm_clip(lst, norm, 1.0, space)
+    torch.cuda.current_stream().wait_stream(s)
+    _check(torch, x, before, x, norm, 1.0, 1.0)
+
+
+@gpu
+def test_overlaps_are_refused_at_creation():
+    torch, b = _torch()
+    x = torch.zeros((100, 40), device="cuda")
+    y = torch.zeros((100, 40), device="cuda")
+    for grads, outs in (([x, x], None), ([x, x[3]], None), ([x[:, :20], x[:, 19:]], None), ([x], [x.view(torch.bfloat16)[:, :40]]),
+                        ([x[:99], y[:99]], [y[1:], x[1:]]), ([x, y], [y, x]), ([x, x], [y, y]), ([x[:50], y[:50]], [x[50:], x[49:99]])):
+        with pytest.raises(b.IcqError) as e:
+            b.icq_grad_list_create(grads, outs)
+        assert e.value.code == b.ICQ_ERR_ARG
+    b.icq_grad_list_create([x[:, :20], x[:, 20:]])
+    b.icq_grad_list_create([x[:50], x[50:]], [y[:50], y[50:]])
+    b.icq_grad_list_create([x, x], [y, torch.zeros_like(y)])    # read twice, written apart
+    b.icq_grad_list_create([x, y], [x, torch.zeros_like(y)])
+
+
+@gpu
+def test_the_binding_refuses_what_does_not_fit():
+    torch, b = _torch()
+    x = torch.zeros((4, 6, 8), device="cuda")
+    for grads, outs in (([x[:, :, 1:]], None), ([x], [x[0]]), ([x], []), ([x.permute(2, 0, 1)], [torch.zeros((8, 4, 6), device="cuda")]), ([x[0, :1, :1].expand(6, 8)], None)):
+        with pytest.raises(ValueError):
+            b.icq_grad_list_create(grads, outs)
+    with pytest.raises(TypeError):
+        b.icq_grad_list_create([x.double()])
+    with pytest.raises(TypeError):
+        b.icq_grad_list_create([x.cpu()])
+    lst, norm = b.icq_grad_list_create([x]), torch.zeros((1,), device="cuda")
+    space = _space(torch, b, lst)
+    for bad in (float("nan"), -1.0):
+        with pytest.raises(b.IcqError):
+            b.icq_grad_norm_clip(lst, norm, bad, space)
+        with pytest.raises(b.IcqError):
+            b.icq_grad_norm(lst, norm, space, scale=bad)
+    with pytest.raises(b.IcqError):
+        b.icq_grad_clip(lst, norm, 1.0, scale=float("inf"))
+    with pytest.raises(b.IcqError) as e:
+        b.icq_grad_norm(lst, norm, space[:0])
+    assert e.value.code == b.ICQ_ERR_WORKSPACE
+    b.icq_grad_list_destroy(lst)
+    with pytest.raises(b.IcqError):
+        b.icq_grad_norm(lst, norm, space)
+
+
+# ---- on the CPU
+
+def test_bad_arguments_are_refused_before_any_device_work():
+    from paper_1912_08756_amd import binding as b
+    lib, E = b.load(), b.ICQ_ERR_ARG
+    h = ctypes.c_void_p(0)
+
+    def make(g=4096, t=0, r=2, c=8, ld=8, o=None, ot=0, ldo=8, n=1):
+        one = lambda v, kind: None if v is None else (kind * 1)(v)  # noqa: E731
+        return lib.icq_grad_list_create(ctypes.byref(h), one(g, ctypes.c_void_p), one(t, ctypes.c_int), one(r, ctypes.c_int64), one(c, ctypes.c_int64), one(ld, ctypes.c_int64),
+                                        one(o, ctypes.c_void_p), one(ot, ctypes.c_int), one(ldo, ctypes.c_int64), n, None)
+
+    for bad in (dict(g=None), dict(t=None), dict(t=3), dict(t=-1), dict(r=-1), dict(c=-1), dict(r=None), dict(ld=7), dict(g=4097), dict(g=0), dict(o=8192, ot=None), dict(o=8192, ldo=None),
+                dict(o=8192, ldo=7), dict(o=8193), dict(o=4100), dict(o=4096, ot=1), dict(o=4096, ldo=9), dict(n=-1), dict(r=2 ** 40, c=2 ** 40, ld=2 ** 40), dict(r=2 ** 30, ld=2 ** 62)):
+        assert make(**bad) == E and h.value is None, bad
+    size = ctypes.c_size_t(0)
+    p = ctypes.c_void_p(4096)
+    assert lib.icq_grad_list_create(None, None, None, None, None, None, None, None, None, 0, None) == E
+    assert lib.icq_grad_workspace_bytes(None, ctypes.byref(size)) == E
+    assert lib.icq_grad_norm(None, 1.0, p, p, 1 << 20, None) == E
+    assert lib.icq_grad_clip(None, 1.0, 1.0, p, None) == E
+    assert lib.icq_grad_norm_clip(None, 1.0, 1.0, p, p, 1 << 20, None) == E
+    lib.icq_grad_list_destroy(None)
+
+
+def test_extents_that_share_memory_against_counting_bytes(tmp_path):
+    rng = np.random.default_rng(4)
+    cases, want = [], []
+    for _ in range(3000):
+        m = []
+        ld = int(rng.integers(1, 12))
+        for k in range(2):
+            rows, ld = int(rng.integers(0, 6)), ld if rng.random() < 0.6 else int(rng.integers(1, 12))
+            length = int(rng.integers(0, ld + 1)) if rows != 1 else int(rng.integers(0, 30))
+            m.append((int(rng.integers(100, 150)), rows, ld, length))
+        cells = [{f + i * d + j for i in range(r) for j in range(n)} for f, r, d, n in m]
+        cases.append(m)
+        want.append(bool(cells[0] & cells[1]))
+    assert 0.2 < np.mean(want) < 0.8
+    out = _compiled(tmp_path, """
+#include "icq_overlap.h"
+#include <stdio.h>
+int main() {
+    const icq_extent e[][2] = {%s};
+    for (const auto &p : e) printf("%%d%%d\\n", icq_extents_overlap(p[0], p[1]), icq_extents_overlap(p[1], p[0]));
+    return 0;
+}
+""" % ",".join("{{%d,%d,%d,%d},{%d,%d,%d,%d}}" % (*x, *y) for x, y in cases))
+    assert [o == "11" for o in out] == want and all(o in ("00", "11") for o in out)

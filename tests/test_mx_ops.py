@@ -1,0 +1,365 @@
+"""Microscaled 4-bit floating point against plain 64-bit forms: codes, scales and values equal to the bit; products within what 32-bit sums of
+their terms can be off."""
+import ctypes
+
+import numpy as np
+import pytest
+
+import mx_reference as ref
+
+gpu = pytest.mark.gpu
+
+
+def _torch():
+    import torch
+    from paper_1912_08756_amd import binding
+    binding.load()
+    return torch, binding
+
+
+def _types(torch):
+    return {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+
+
+def _np(t):
+    return t.double().cpu().numpy()
+
+
+def _values(torch, rows, cols, kind, seed):
+    """Rows of very different magnitude, some zero; in f16 subnormal numbers among them."""
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn((rows, cols), generator=g)
+    far = 20 if kind != "f16" else 14
+    x = x * torch.exp2(torch.randint(-far, far if kind != "f16" else 8, (rows, 1), generator=g).float()) * (torch.rand((rows, 1), generator=g) > 0.1)
+    return x.to(_types(torch)[kind]).cuda()
+
+
+def _held(torch, b, x, block_rows=1, fit=False):
+    """(codes, scales) of x from the plain form, on the device, with padding that would be wrong if it were used."""
+    codes, scales = ref.quantize(_np(x), block_rows, fit)
+    c, s = b.icq_mx_codes(*x.shape), b.icq_mx_scales(*x.shape)
+    for t, v in ((c, ref.pack(codes)), (s, scales)):
+        t.untyped_storage().fill_(0xFF)
+        t.copy_(torch.from_numpy(v))
+    return c, s
+
+
+# ---- the plain form against itself (CPU)
+
+def test_reference_codes_of_all_values_and_their_middles():
+    assert np.array_equal(ref.VALUES[ref.nearest(ref.VALUES)], ref.VALUES) and np.array_equal(ref.nearest(ref.VALUES), np.arange(16))
+    assert np.array_equal(ref.nearest(ref.MIDDLES), [0, 2, 2, 4, 4, 6, 6])
+    assert np.array_equal(ref.nearest(ref.MIDDLES * (1 + 1e-9)), np.arange(1, 8)) and np.array_equal(ref.nearest(ref.MIDDLES * (1 - 1e-9)), np.arange(7))
+    assert np.array_equal(ref.nearest(np.array([7.9, -7.9, 1e9, -0.0])), [7, 15, 7, 8])
+
+
+def test_reference_scales():
+    for a in (2.0 ** -120, 2.0 ** -100, 1e-20, 0.99, 1.0, 5.9, 6.0, 6.1, 7.9, 8.0, 1e30, 3.4e38):
+        used = max(a, 2.0 ** -100)
+        floor, fit = (2.0 ** ref.scale_exponent(a, f) for f in (False, True))
+        assert 4 * floor <= used < 8 * floor
+        assert used <= 6 * fit or fit == 2.0 ** 125
+        assert 3 * fit < used or fit == 2.0 ** 125
+
+
+def test_reference_packing():
+    c = np.random.default_rng(1).integers(0, 16, (5, 7)).astype(np.uint8)
+    assert np.array_equal(ref.unpack(ref.pack(c), 7), c) and ref.pack(c)[0, 0] == c[0, 0] + 16 * c[0, 1]
+
+
+# ---- quantisation
+
+SIZES = [(1, 1), (1, 31), (3, 32), (5, 33), (33, 95), (130, 17), (257, 960), (129, 1000), (16, 4099)]
+
+
+@gpu
+@pytest.mark.parametrize("rows,cols", SIZES)
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("fit", [False, True])
+@pytest.mark.parametrize("block", [1, 32])
+def test_codes_and_scales_are_the_formula_s(rows, cols, kind, fit, block):
+    torch, b = _torch()
+    x = _values(torch, rows, cols, kind, rows * 7 + cols)
+    if kind == "f32" and rows > 100:
+        x[100:] *= 1e-33                                       # blocks below 2^-100
+    for which in ("rows", "columns", "both"):
+        got = [b.icq_mx_codes(rows, cols), b.icq_mx_scales(rows, cols), b.icq_mx_codes(cols, rows), b.icq_mx_scales(cols, rows)]
+        for t in got:
+            t.untyped_storage().fill_(0x55)
+        use = [t if which != ("columns" if k < 2 else "rows") else None for k, t in enumerate(got)]
+        b.icq_mx_quantize(x, *use, block_rows=block, fit=fit)
+        for codes, scales, v in ((use[0], use[1], _np(x)), (use[2], use[3], _np(x).T)):
+            if codes is None:
+                continue
+            n = v.shape[1]
+            want, s = ref.quantize(v, block, fit)
+            assert np.array_equal(ref.unpack(codes.cpu().numpy(), n), want)
+            assert np.array_equal(scales.cpu().numpy(), s)
+            for t, step in ((codes, 16), (scales, 4)):          # what belongs to a row behind its end is zero
+                wide = torch.as_strided(t, (t.shape[0], -(-t.shape[1] // step) * step), (t.stride(0), 1))
+                assert not wide[:, t.shape[1]:].any()
+            if n % 2:
+                assert not (codes[:, -1] >> 4).any()
+        for k, t in enumerate(got):
+            if use[k] is None:
+                assert (torch.as_strided(t, (t.untyped_storage().nbytes(),), (1,)) == 0x55).all()
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("fit", [False, True])
+def test_every_value_of_a_block_and_every_tie(kind, fit):
+    """Grids around each code and each middle, as far as the type holds them, under several scales."""
+    torch, b = _torch()
+    dtype = _types(torch)[kind]
+    base = np.concatenate([np.abs(ref.VALUES[:8]), ref.MIDDLES])
+    near = np.concatenate([base, base * (1 + 2.0 ** -7), base * (1 - 2.0 ** -7), base * (1 + 2.0 ** -10), base * (1 - 2.0 ** -10), [5.0, 7.0, 7.96875]])
+    rows = []
+    for top in (4.0, 5.0, 6.0, 6.03125, 7.0, 7.96875):
+        v = near[near <= top]
+        v = np.concatenate([v, -v])
+        v = np.concatenate([v, np.zeros(-len(v) % 31)]).reshape(-1, 31)
+        rows.append(np.concatenate([np.full((len(v), 1), top), v], axis=1))
+    x = np.concatenate(rows)
+    exps = [-14, -3, 0, 9] if kind == "f16" else [-90, -3, 0, 60, 120]
+    x = torch.from_numpy(np.concatenate([x * 2.0 ** e for e in exps])).to(dtype)
+    codes, scales = b.icq_mx_codes(*x.shape), b.icq_mx_scales(*x.shape)
+    b.icq_mx_quantize(x.cuda(), codes, scales, fit=fit)
+    want, s = ref.quantize(x.double().numpy(), 1, fit)
+    assert np.array_equal(scales.cpu().numpy(), s) and np.array_equal(ref.unpack(codes.cpu().numpy(), 32), want)
+    codes_t, scales_t = b.icq_mx_codes(*x.shape), b.icq_mx_scales(*x.shape)
+    b.icq_mx_quantize(x.t().contiguous().cuda(), None, None, codes_t, scales_t, fit=fit)
+    assert torch.equal(codes_t, codes) and torch.equal(scales_t, scales)
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("block", [1, 32])
+def test_infinities_nan_the_largest_and_the_smallest(kind, block):
+    torch, b = _torch()
+    dtype = _types(torch)[kind]
+    x = torch.randn((140, 300), generator=torch.Generator().manual_seed(9)).to(dtype)
+    x[3, 5], x[3, 200], x[4, 7], x[77, 131], x[139, 299] = float("inf"), float("-inf"), float("nan"), float("nan"), float("inf")
+    x[96:, :32] = 0.0
+    x[128:, 32:64] = torch.finfo(dtype).max
+    x[64:96, 64:96] = torch.finfo(dtype).tiny
+    x[64:96, 96:128] = torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps * 3
+    for fit in (False, True):
+        got = [b.icq_mx_codes(140, 300), b.icq_mx_scales(140, 300), b.icq_mx_codes(300, 140), b.icq_mx_scales(300, 140)]
+        b.icq_mx_quantize(x.cuda(), *got, block_rows=block, fit=fit)
+        for codes, scales, v in ((got[0], got[1], x.double().numpy()), (got[2], got[3], x.double().numpy().T)):
+            want, s = ref.quantize(v, block, fit)
+            assert np.array_equal(scales.cpu().numpy(), s) and np.array_equal(ref.unpack(codes.cpu().numpy(), v.shape[1]), want)
+            for out in _types(torch).values():
+                y = torch.full(v.shape, -7.0, dtype=out, device="cuda")
+                b.icq_mx_dequantize(codes, scales, y)
+                exact = torch.from_numpy(ref.values(want, s))
+                assert np.array_equal(_np(y), _np(exact.to(out)), equal_nan=True)
+
+
+@gpu
+def test_rows_of_wider_buffers_and_rows_that_start_anywhere():
+    torch, b = _torch()
+    big = _values(torch, 67, 700, "bf16", 1)
+    for x in (big[:, 3:403], big[5:, :300], big[::2, 8:520], big[1:2, 1:130], big.float()[:, 1:]):
+        rows, cols = x.shape
+        got = [b.icq_mx_codes(rows, cols), b.icq_mx_scales(rows, cols), b.icq_mx_codes(cols, rows), b.icq_mx_scales(cols, rows)]
+        b.icq_mx_quantize(x, *got)
+        want, s = ref.quantize(_np(x))
+        assert np.array_equal(ref.unpack(got[0].cpu().numpy(), cols), want) and np.array_equal(got[1].cpu().numpy(), s)
+        alone = [b.icq_mx_codes(rows, cols), b.icq_mx_scales(rows, cols)]
+        b.icq_mx_quantize(x, *alone)
+        assert torch.equal(alone[0], got[0]) and torch.equal(alone[1], got[1])
+        wide = torch.full((rows, cols + 5), -3.0, device="cuda")
+        b.icq_mx_dequantize(*alone, wide[:, 2:cols + 2])
+        assert np.array_equal(_np(wide[:, 2:cols + 2]), ref.values(want, s)) and (wide[:, :2] == -3).all() and (wide[:, cols + 2:] == -3).all()
+
+
+@gpu
+@pytest.mark.parametrize("out", ["f32", "f16", "bf16"])
+def test_every_code_under_every_scale(out):
+    torch, b = _torch()
+    codes, scales = b.icq_mx_codes(256, 32), b.icq_mx_scales(256, 32)
+    codes.copy_(torch.arange(0, 256, 17, dtype=torch.uint8).repeat(256, 1))
+    scales.copy_(torch.arange(256, dtype=torch.int32).to(torch.uint8)[:, None])
+    y = torch.empty((256, 32), dtype=_types(torch)[out], device="cuda")
+    b.icq_mx_dequantize(codes, scales, y)
+    want = torch.from_numpy(ref.values(ref.unpack(codes.cpu().numpy(), 32), scales.cpu().numpy())).to(_types(torch)[out])
+    assert np.array_equal(_np(y), _np(want), equal_nan=True)
+
+
+# ---- products
+
+def _check_product(got, out, x, w):
+    """Sums of n terms in 32 bits, in any order, are off by at most (n + 8) / 2 units of 2^-23 of the sum of magnitudes; the result's rounding adds
+    half a step."""
+    want, size = x @ w.T, np.abs(x) @ np.abs(w).T
+    half = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}[out]
+    least = {"f32": 2.0 ** -149, "f16": 2.0 ** -25, "bf16": 2.0 ** -133}[out]
+    off = np.abs(got - want)
+    allowed = (x.shape[1] + 8) * 2.0 ** -24 * size + half * np.abs(want) + least
+    assert (off <= allowed).all(), (np.argwhere(~(off <= allowed))[:3], off.max())
+
+
+@gpu
+@pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 17, 31), (2, 33, 64), (5, 100, 129), (16, 48, 255), (17, 130, 257), (40, 61, 960), (33, 200, 1023), (130, 260, 640),
+                                   (300, 270, 77), (1, 700, 4100), (20, 300, 2049)])
+@pytest.mark.parametrize("out", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("a", ["held", "f32", "f16", "bf16"])
+def test_products(M, N, K, out, a):
+    torch, b = _torch()
+    fit = (M + N + K) % 2 == 0
+    g = torch.Generator().manual_seed(M * N + K)
+    x = (torch.randn((M, K), generator=g) * torch.exp2(torch.randint(-3, 4, (M, K), generator=g).float())).to(_types(torch)["f32" if a == "held" else a]).cuda()
+    w = (torch.randn((N, K), generator=g) * 0.05).cuda()
+    wc, ws = _held(torch, b, w, 32)
+    xv = ref.values(*ref.quantize(_np(x), 1, fit))
+    wv = ref.values(*ref.quantize(_np(w), 32))
+    y = torch.full((M, N + 3), -7.0, dtype=_types(torch)[out], device="cuda")
+    need = b.icq_mx_matmul_workspace_bytes(M, N, K, None if a == "held" else x.dtype)
+    space = torch.empty(max(1, need), dtype=torch.uint8, device="cuda") if need else None
+    if a == "held":
+        b.icq_mx_matmul(*_held(torch, b, x, 1, fit), wc, ws, y[:, :N], space, K=K)
+    else:
+        b.icq_mx_matmul(x, None, wc, ws, y[:, :N], space, fit=fit, K=K)
+    assert (y[:, N:] == -7).all()
+    _check_product(_np(y[:, :N]), out, xv, wv)
+
+
+@gpu
+@pytest.mark.parametrize("a", ["held", "bf16"])
+@pytest.mark.parametrize("M,K", [(1, 40), (5, 200), (37, 300), (300, 700)])
+def test_rows_with_a_nan_give_nan_and_no_others(M, K, a):
+    torch, b = _torch()
+    g = torch.Generator().manual_seed(M)
+    x, w = torch.randn((M, K), generator=g).bfloat16(), torch.randn((90, K), generator=g)
+    x[M // 2, K - 1] = float("nan")
+    w[7, 0], w[80, 33] = float("inf"), float("nan")
+    x, w = x.cuda(), w.cuda()
+    wc, ws = _held(torch, b, w)
+    y = torch.empty((M, 90), device="cuda")
+    space = torch.empty(max(1, b.icq_mx_matmul_workspace_bytes(M, 90, K, x.dtype)), dtype=torch.uint8, device="cuda")
+    b.icq_mx_matmul(*(_held(torch, b, x) if a == "held" else (x, None)), wc, ws, y, space, K=K)
+    want = torch.zeros((M, 90), dtype=torch.bool)
+    want[M // 2], want[:, 7], want[:, 80] = True, True, True
+    assert torch.equal(torch.isnan(y).cpu(), want)
+
+
+@gpu
+def test_no_contraction_and_empty_results():
+    torch, b = _torch()
+    wc, ws = b.icq_mx_codes(5, 0), b.icq_mx_scales(5, 0)
+    y = torch.full((3, 5), -1.0, device="cuda")
+    b.icq_mx_matmul(torch.empty((3, 0), device="cuda"), None, wc, ws, y)
+    assert not y.any()
+    b.icq_mx_matmul(b.icq_mx_codes(3, 0), b.icq_mx_scales(3, 0), wc, ws, y.fill_(2.0), K=0)
+    assert not y.any()
+    w2, s2 = b.icq_mx_codes(5, 64), b.icq_mx_scales(5, 64)
+    b.icq_mx_matmul(torch.empty((0, 64), device="cuda"), None, w2, s2, torch.empty((0, 5), device="cuda"))
+    b.icq_mx_quantize(torch.empty((0, 64), device="cuda"), b.icq_mx_codes(0, 64), b.icq_mx_scales(0, 64))
+
+
+@gpu
+def test_forward_and_backward_of_a_layer():
+    """Y = X W^T, dX = G W, dW = G^T X from one quantisation of each, W in squares: both products see the same W."""
+    torch, b = _torch()
+    g = torch.Generator().manual_seed(5)
+    T, N, K = 200, 333, 150
+    x, w, gr = (torch.randn(s, generator=g).cuda() for s in ((T, K), (N, K), (T, N)))
+    q = {}
+    for name, t, block in (("x", x, 1), ("w", w, 32), ("g", gr, 1)):
+        q[name] = [b.icq_mx_codes(*t.shape), b.icq_mx_scales(*t.shape), b.icq_mx_codes(*t.t().shape), b.icq_mx_scales(*t.t().shape)]
+        b.icq_mx_quantize(t, *q[name], block_rows=block, fit=True)
+    v = lambda t, block: ref.values(*ref.quantize(_np(t), block, True))  # noqa: E731
+    wv = v(w, 32)
+    assert np.array_equal(v(w.t(), 32), wv.T)
+    for a, c, n, k, xv, yv in ((q["x"][:2], q["w"][:2], N, K, v(x, 1), wv), (q["g"][:2], q["w"][2:], K, N, v(gr, 1), wv.T),
+                               (q["g"][2:], q["x"][2:], K, T, v(gr.t(), 1), v(x.t(), 1))):
+        out = torch.empty((xv.shape[0], n), device="cuda")
+        need = b.icq_mx_matmul_workspace_bytes(*out.shape, k)
+        b.icq_mx_matmul(*a, *c, out, torch.empty(need, dtype=torch.uint8, device="cuda") if need else None, K=k)
+        _check_product(_np(out), "f32", xv, yv)
+
+
+@gpu
+def test_other_dtypes_of_codes_and_scales_and_odd_rows():
+    torch, b = _torch()
+    x = torch.randn((6, 64), device="cuda")
+    codes, scales = b.icq_mx_codes(6, 64), b.icq_mx_scales(6, 64)
+    b.icq_mx_quantize(x, codes.view(torch.float4_e2m1fn_x2), scales.view(torch.float8_e8m0fnu))
+    assert np.array_equal(ref.unpack(codes.cpu().numpy(), 64), ref.quantize(_np(x))[0])
+    y, z = torch.empty((6, 64), device="cuda"), torch.empty((6, 6), device="cuda")
+    b.icq_mx_dequantize(codes.view(torch.float4_e2m1fn_x2), scales.view(torch.float8_e8m0fnu), y)
+    assert torch.equal(y.cpu(), torch.from_numpy(ref.values(*ref.quantize(_np(x)))).float())
+    b.icq_mx_matmul(codes.view(torch.float4_e2m1fn_x2), scales.view(torch.float8_e8m0fnu), codes, scales, z)       # K = 64: twice the bytes
+    assert torch.allclose(z, y @ y.t(), rtol=1e-5, atol=1e-5)
+
+
+# ---- refusals
+
+def test_bad_arguments_are_refused_before_any_device_work():
+    from paper_1912_08756_amd import binding as b
+    lib, E, W = b.load(), b.ICQ_ERR_ARG, b.ICQ_ERR_WORKSPACE
+    p, n = ctypes.c_void_p(4096), None
+    quant = lambda x=p, t=0, r=4, c=64, ldx=64, rule=0, block=1, codes=p, ld=32, s=p, lds=4, ct=n, ldt=0, st=n, ldst=0: lib.icq_mx_quantize(  # noqa: E731
+        x, t, r, c, ldx, rule, block, codes, ld, s, lds, ct, ldt, st, ldst, None)
+    assert quant(r=0) == 0 and quant(c=0) == 0
+    odd = ctypes.c_void_p(4097)
+    for bad in (dict(t=3), dict(t=-1), dict(r=-1), dict(c=-1), dict(c=2 ** 31), dict(ldx=63), dict(rule=2), dict(block=2), dict(block=128), dict(codes=n), dict(s=n), dict(x=n),
+                dict(ld=16), dict(ld=40), dict(lds=1), dict(lds=2), dict(lds=6), dict(codes=ctypes.c_void_p(4104)), dict(s=ctypes.c_void_p(4098)), dict(x=odd), dict(ct=p),
+                dict(ct=p, st=p, ldt=16, ldst=0), dict(ct=p, st=p, ldt=0, ldst=4), dict(ct=odd, st=p, ldt=16, ldst=4)):
+        assert quant(**bad) == E, bad
+    back = lambda codes=p, ld=32, s=p, lds=4, r=4, c=64, out=p, t=0, ldo=64: lib.icq_mx_dequantize(codes, ld, s, lds, r, c, out, t, ldo, None)  # noqa: E731
+    assert back(r=0) == 0
+    for bad in (dict(codes=n), dict(s=n), dict(out=n), dict(out=odd), dict(t=3), dict(ldo=63), dict(ld=16), dict(lds=1), dict(r=-1), dict(c=2 ** 31)):
+        assert back(**bad) == E, bad
+    mul = lambda a=p, t=3, lda=32, sa=p, ldsa=4, rule=0, w=p, ldb=32, sb=p, ldsb=4, M=4, N=4, K=64, out=p, ot=0, ldo=4, ws=p, wsb=1 << 20: lib.icq_mx_matmul(  # noqa: E731
+        a, t, lda, sa, ldsa, rule, w, ldb, sb, ldsb, M, N, K, out, ot, ldo, ws, wsb, None)
+    assert mul(M=0) == 0 and mul(N=0) == 0
+    for bad in (dict(a=n), dict(t=4), dict(t=-1), dict(lda=16), dict(lda=40), dict(sa=n), dict(ldsa=1), dict(ldsa=5), dict(rule=2), dict(w=n), dict(ldb=16), dict(ldb=2 ** 24), dict(sb=n),
+                dict(ldsb=0), dict(M=-1), dict(N=-1), dict(K=-1), dict(M=2 ** 31), dict(out=n), dict(out=odd), dict(ot=3), dict(ldo=3), dict(t=0, lda=64), dict(t=0, lda=63, sa=n),
+                dict(t=0, a=odd, lda=64, sa=n), dict(t=2, a=n, lda=64, sa=n)):
+        assert mul(**bad) == E, bad
+    size = ctypes.c_size_t(0)
+    assert lib.icq_mx_matmul_workspace_bytes(4, 4, 64, 5, ctypes.byref(size)) == E and lib.icq_mx_matmul_workspace_bytes(4, 4, -1, 3, ctypes.byref(size)) == E
+    assert lib.icq_mx_matmul_workspace_bytes(4, 4, 64, 3, None) == E
+
+
+@gpu
+def test_a_missing_or_short_workspace_is_refused():
+    torch, b = _torch()
+    x = torch.randn((400, 256), device="cuda")
+    codes, scales = b.icq_mx_codes(400, 256), b.icq_mx_scales(400, 256)
+    b.icq_mx_quantize(x, codes, scales)
+    y = torch.full((400, 400), -7.0, device="cuda")
+    need = b.icq_mx_matmul_workspace_bytes(400, 400, 256, torch.float32)
+    assert need > 0
+    for space in (None, torch.empty(need - 256, dtype=torch.uint8, device="cuda"), torch.empty(need + 256, dtype=torch.uint8, device="cuda")[1:]):
+        with pytest.raises(b.IcqError) as e:
+            b.icq_mx_matmul(x, None, codes, scales, y, space)
+        assert e.value.code == b.ICQ_ERR_WORKSPACE
+    assert (y == -7).all()
+
+
+@gpu
+def test_the_binding_refuses_what_does_not_fit():
+    torch, b = _torch()
+    x = torch.randn((4, 64), device="cuda")
+    codes, scales = b.icq_mx_codes(4, 64), b.icq_mx_scales(4, 64)
+    tight = torch.empty((4, 10), dtype=torch.uint8, device="cuda")
+    with pytest.raises(ValueError):
+        b.icq_mx_quantize(x, b.icq_mx_codes(4, 62), scales)
+    with pytest.raises(ValueError):
+        b.icq_mx_quantize(x, codes, b.icq_mx_scales(4, 128))
+    with pytest.raises(ValueError):                            # the last row's bytes up to the next multiple of 16 are not there
+        b.icq_mx_quantize(x[:, :20], tight, b.icq_mx_scales(4, 20))
+    with pytest.raises(TypeError):
+        b.icq_mx_quantize(x.double(), codes, scales)
+    with pytest.raises(TypeError):
+        b.icq_mx_quantize(x, codes.int(), scales)
+    with pytest.raises(ValueError):
+        b.icq_mx_matmul(x, None, codes, scales, torch.empty((4, 5), device="cuda"))
+    with pytest.raises(ValueError):
+        b.icq_mx_matmul(x, None, codes, scales, torch.empty((4, 4), device="cuda"), K=62)
+    with pytest.raises(b.IcqError):
+        b.icq_mx_quantize(x, None, None)
