@@ -1,6 +1,7 @@
 // Shared by the kernels of microscaled 4-bit floating point.
 #pragma once
 #include "icq_matmul.h"
+#include "icq_mx_plan.h"
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
@@ -66,3 +67,5 @@ struct MxQuantize {
 
 // Rows of blocks of 32 (icq_mx.hip): what icq_mx_quantize does for `codes` alone with block_rows = 1.
 int icq_launch_mx_rows(const MxQuantize &a, int x_type, hipStream_t s);
+// The product in tiles, p.splits parts of the contraction; a step along K is 256 values (icq_mx_tiles.hip).
+int icq_launch_mx_tiles(const MxProduct &q, icq_tiles tiles, int out_type, hipStream_t s);

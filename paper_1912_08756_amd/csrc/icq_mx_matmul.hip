@@ -45,13 +45,16 @@ __global__ __launch_bounds__(64 * WAVES) void mx_product_kernel(MxProduct q, int
 
 bool values(int a_type) { return icq_type_bytes(a_type) > 0; }
 
-// Where a's codes and scales lie in the workspace if it comes as values.
-struct Held { int64_t ld, ld_s; size_t scales, bytes; };
-Held held(int64_t M, int64_t K) {
-    Held h;
+// The workspace: the parts' sums, then a's codes and scales if it comes as values.
+struct Held { int64_t ld, ld_s; size_t codes, scales, bytes; };
+Held held(int64_t M, int64_t N, int64_t K, bool values, const icq_mx_plan &plan) {
+    Held h = {};
+    h.codes = plan.splits > 1 ? icq_align_up((size_t)plan.splits * M * N * sizeof(float), ICQ_ALIGN) : 0;
+    h.bytes = h.codes;
+    if (!values) return h;
     h.ld = (K + 31) / 32 * 16;
     h.ld_s = (K + 127) / 128 * 4;
-    h.scales = icq_align_up((size_t)M * h.ld, ICQ_ALIGN);
+    h.scales = h.codes + icq_align_up((size_t)M * h.ld, ICQ_ALIGN);
     h.bytes = h.scales + icq_align_up((size_t)M * h.ld_s, ICQ_ALIGN);
     return h;
 }
@@ -60,7 +63,9 @@ Held held(int64_t M, int64_t K) {
 
 ICQ_EXPORT int icq_mx_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K, int a_type, size_t *out) {
     if (!out || !icq_product_extents_ok(M, N, K) || (a_type != ICQ_E2M1 && !values(a_type))) return ICQ_ERR_ARG;
-    *out = values(a_type) && M > 0 && N > 0 && K > 0 ? held(M, K).bytes : 0;
+    const int cu = icq_num_cu();
+    if (cu <= 0) return ICQ_ERR_HIP;
+    *out = M > 0 && N > 0 && K > 0 ? held(M, N, K, values(a_type), icq_plan_mx(M, N, K, cu)).bytes : 0;
     return ICQ_OK;
 }
 
@@ -93,17 +98,27 @@ ICQ_EXPORT int icq_mx_matmul(const void *a, int a_type, int64_t lda, const uint8
         p.splits = 0;                                                         // (a sum of nothing)
         return icq_launch_product_join(p, out_type, s);
     }
+    const int cu = icq_num_cu();
+    if (cu <= 0) return ICQ_ERR_HIP;
+    const icq_mx_plan plan = icq_plan_mx(M, N, K, cu);
+    const Held h = held(M, N, K, values(a_type), plan);
+    if (h.bytes > 0 && (!workspace || (uintptr_t)workspace % ICQ_ALIGN != 0 || workspace_bytes < h.bytes)) return ICQ_ERR_WORKSPACE;
     if (values(a_type)) {
-        const Held h = held(M, K);
-        if (!workspace || (uintptr_t)workspace % ICQ_ALIGN != 0 || workspace_bytes < h.bytes) return ICQ_ERR_WORKSPACE;
         MxQuantize z = {};
         z.x = a; z.rows = M; z.cols = K; z.ldx = lda;
-        z.codes = static_cast<uint8_t *>(workspace); z.scales = z.codes + h.scales; z.ld = h.ld; z.ld_s = h.ld_s;
+        z.codes = static_cast<uint8_t *>(workspace) + h.codes; z.scales = static_cast<uint8_t *>(workspace) + h.scales; z.ld = h.ld; z.ld_s = h.ld_s;
         z.across = (int)((K + 127) / 128);
         z.fit = scaling == ICQ_MX_FIT;
         const int rc = icq_launch_mx_rows(z, a_type, s);
         if (rc != ICQ_OK) return rc;
         p.a = z.codes; p.lda = h.ld; q.ea = z.scales; q.ld_ea = h.ld_s;
+    }
+    if (!plan.few) {
+        p.kb = (int)((K + 255) / 256);
+        p.splits = plan.splits; p.per = plan.per;
+        p.part = static_cast<float *>(workspace);
+        const int rc = icq_launch_mx_tiles(q, plan.tiles, out_type, s);
+        return rc != ICQ_OK || p.splits == 1 ? rc : icq_launch_product_join(p, out_type, s);
     }
     const int64_t tiles_n = (N + 15) / 16, tiles = (M + 15) / 16 * tiles_n, step = (int64_t)ICQ_PRODUCT_BLOCKS * WAVES;
     for (int64_t t = 0; t < tiles; t += step) {

@@ -1,0 +1,40 @@
+// How icq_mx_matmul computes a product, by its sizes.  Host code, no HIP.
+#pragma once
+#include "icq_matmul_plan.h"
+
+// Tiles of 256 x 256, of 128 x 128 with two stages in the LDS or four, or of 64 x 64; a stage is 256 values along K.
+struct icq_mx_plan {
+    bool few;
+    icq_tiles tiles;
+    int splits, per;           // parts of the contraction, stages in each
+};
+
+static inline icq_mx_plan icq_plan_mx(int64_t M, int64_t N, int64_t K, int num_cu) {
+    const int64_t stages = (K + 255) / 256;
+    icq_mx_plan best = {M <= 16, ICQ_TILES_SMALL, 1, (int)stages};
+    if (best.few) return best;
+    double least = -1.0;
+    for (int64_t T = 256; T >= 64; T /= 2) {
+        const int64_t tiles = ((M + T - 1) / T) * ((N + T - 1) / T);
+        for (int splits = 1; splits <= 16 && (splits == 1 || stages >= 2 * splits); splits *= 2) {
+            const int64_t per = (stages + splits - 1) / splits, parts = (stages + per - 1) / per, blocks = tiles * parts;
+            const int64_t rounds = blocks / (2 * num_cu), left = blocks % (2 * num_cu);
+            const bool alone = blocks <= num_cu;
+            const auto last = [&](double pair, double one) { return left > num_cu ? pair : left > 0 ? one : 0.0; };
+            const double share = (double)left / num_cu;
+            double us;
+            if (T == 256) us = 1.5 * (blocks / num_cu) + (blocks % num_cu > 0 ? 1.1 + 0.4 * (blocks % num_cu) / num_cu : 0.0);
+            else if (T == 128) us = 1.0 * rounds + last(1.0, 0.5 + 0.1 * share);
+            else us = 0.45 * rounds + last(0.45, 0.3);
+            us *= per;
+            if (parts > 1) us += 2.5 + (double)parts * M * N * 8 / 4.4e6;
+            if (least < 0.0 || us < least) {
+                least = us;
+                best.tiles = T == 256 ? ICQ_TILES_WIDE : T == 64 ? ICQ_TILES_LITTLE : alone ? ICQ_TILES_DEEP : ICQ_TILES_SMALL;
+                best.splits = (int)parts;
+                best.per = (int)per;
+            }
+        }
+    }
+    return best;
+}

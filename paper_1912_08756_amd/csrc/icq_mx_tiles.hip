@@ -1,0 +1,272 @@
+// Products of matrices in microscaled 4-bit floating point, in tiles of 256 x 256 (four wavefronts of 128 x 128), 128 x 128 (four of 64 x 64)
+// or 64 x 64 (four of 32 x 32).
+//
+// A stage is 256 values of each row: 128 bytes of codes and eight scales, which go from memory straight into the LDS. A row's eight 16-byte
+// pieces are permuted by its number, by the choice of each lane's address, so that 16 rows' pieces fall on all 64 banks. One piece is a
+// lane's operand of a 32x32x64 instruction; its scale is a byte of a word that holds the lane's four of the stage.
+// A stage has four steps of 64 values. A step's fragments are read beside the matrix instructions of the step before. The one barrier of a
+// stage stands before its last step's: by then the next stage has arrived and this one's last fragments are in registers, so its place
+// in the LDS takes the stage after the next.
+#include "icq_mx.h"
+#include "icq_tiles.h"
+
+#include <algorithm>
+
+namespace {
+
+// Rows and columns of a wavefront's part in units of 32, wavefronts along m and n, stages in the LDS, blocks that share a compute unit.
+template <int NI_, int NJ_, int WM_, int WN_, int DEPTH_, int SHARE_>
+struct Shape {
+    static constexpr int NI = NI_, NJ = NJ_, WM = WM_, WN = WN_, DEPTH = DEPTH_, SHARE = SHARE_, WAVES = WM * WN, THREADS = 64 * WAVES, T = 32 * NI * WM;
+    static constexpr int PARTS = T / (8 * WAVES), WORDS = 2 * T / 32 / WAVES, LOADS = 2 * PARTS + WORDS;   // of a wavefront for a stage: codes, scales
+    static constexpr int FIRST = LOADS / 2;                                   // requested in the step of the barrier, the others in the next
+    static constexpr int STAGE = 2 * T * 128, SCALES = 2 * T * 8;             // bytes of a stage's codes, scales
+    static constexpr int LDS_BYTES = DEPTH * (STAGE + SCALES);
+    static_assert(32 * NJ * WN == T && T % 64 == 0 && WORDS >= 1 && (2 * T / 32) % WAVES == 0 && (DEPTH - 1) * LOADS < 64 && DEPTH * STAGE / WAVES >= 32 * (32 * NJ + 4) * 4,
+                  "square tiles; whole loads; countable ones; results fit the stages");
+    static_assert(SHARE * LDS_BYTES <= 160 * 1024, "fits the LDS");
+};
+typedef Shape<4, 4, 2, 2, 2, 1> Wide;
+typedef Shape<4, 2, 2, 4, 2, 1> Wide8;
+typedef Shape<2, 2, 2, 2, 2, 2> Small;
+typedef Shape<2, 2, 2, 2, 4, 1> Deep;
+typedef Shape<1, 1, 2, 2, 4, 2> Little;
+
+// Rows of 32 NJ words in the LDS, 4 words between them, into the result.
+template <int TYPE, int NJ>
+__device__ __forceinline__ void rows_from(const float *turn, void *out, int64_t ldo, int64_t M, int64_t N, int64_t m0, int64_t n0, int lane) {
+    typedef IcqElem<TYPE> E;
+    typedef typename E::raw raw;
+    constexpr int WIDTH = 32 * NJ, STRIDE = WIDTH + 4, PER = E::PER, LANES = WIDTH / PER, AT_ONCE = 64 / LANES;
+    const int c = lane % LANES * PER, rows = (int)min((int64_t)32, M - m0), left = (int)min((int64_t)PER, N - n0 - c);
+    raw *to = static_cast<raw *>(out) + (m0 + lane / LANES) * ldo + n0 + c;
+#pragma unroll 4
+    for (int r0 = 0; r0 < 32; r0 += AT_ONCE, to += AT_ONCE * ldo) {
+        const int r = r0 + lane / LANES;
+        if (r >= rows) break;
+        float x[PER];
+#pragma unroll
+        for (int k = 0; k < PER; k += 4) *reinterpret_cast<icq_f32x4 *>(x + k) = *reinterpret_cast<const icq_f32x4 *>(turn + r * STRIDE + c + k);
+        if (left == PER) {
+            const uint4 v = E::pack(x);
+            __builtin_memcpy(to, &v, 16);                                     // (to any address)
+        } else {
+            for (int e = 0; e < left; ++e) to[e] = E::put(x[e]);
+        }
+    }
+}
+
+// store_rows with the type known at run time: the accumulators go into the LDS as they are (a branch for each type around them would have the
+// compiler move and spill them), `turn`: 32 rows of 32 NJ + 4 words.
+template <int NJ>
+__device__ __forceinline__ void store_rows_as(uint8_t *turn, const f32x16 (&acc)[NJ], void *out, int type, int64_t ldo, int64_t M, int64_t N, int64_t m0, int64_t n0,
+                                              int lane) {
+    constexpr int WIDTH = 32 * NJ, STRIDE = WIDTH + 4;
+    const int at = lane & 31, half = lane >> 5;
+    float *mine = reinterpret_cast<float *>(turn);
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const icq_f32x4 v = {acc[j][4 * g], acc[j][4 * g + 1], acc[j][4 * g + 2], acc[j][4 * g + 3]};
+            *reinterpret_cast<icq_f32x4 *>(mine + at * STRIDE + j * 32 + 8 * g + 4 * half) = v;
+        }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    ICQ_FOR_TYPE(type, rows_from<TYPE, NJ>(mine, out, ldo, M, N, m0, n0, lane))
+}
+
+// RAGGED: the last stage is not whole.
+template <typename S, bool RAGGED>
+__global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_kernel(MxProduct q, int tiles_m, int tiles_n, int out_type, uint32_t first_block) {
+    constexpr int T = S::T, NI = S::NI, NJ = S::NJ, DEPTH = S::DEPTH, WAVES = S::WAVES, PARTS = S::PARTS, WORDS = S::WORDS, LOADS = S::LOADS, FIRST = S::FIRST;
+    constexpr int N = NI * NJ, F = NI + NJ;                                   // matrix instructions, fragments of a step
+    extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];          // stages' codes, then stages' scales
+    const Product &p = q.p;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    // XCD blockIdx % 8 takes a contiguous share of the tiles, eight tiles of m at a time (first_block: a multiple of 8)
+    const uint32_t block_id = first_block + blockIdx.x;
+    const int total = tiles_m * tiles_n, q8 = total / 8, r8 = total % 8, xcd = block_id % 8, at8 = block_id / 8;
+    const int tile = xcd * q8 + (xcd < r8 ? xcd : r8) + at8;
+    const int group = tile / (8 * tiles_n), in = tile % (8 * tiles_n), high = min(8, tiles_m - group * 8);
+    const int64_t m0 = (int64_t)(group * 8 + in % high) * T, n0 = (int64_t)(in / high) * T;
+    const int k0 = blockIdx.y * p.per, last = min(p.kb, k0 + p.per) - 1;      // stages k0 .. last, one at least
+    const int wm = (wave % S::WM) * 32 * NI, wn = (wave / S::WM) * 32 * NJ, at = lane & 31, half = lane >> 5;
+    const int whole = (int)(p.K / 256), ragged = (int)(p.K % 256);            // stages along K, and values in one more
+
+    // this lane's place in the loads: instruction u of a wavefront brings rows 8 (WAVES u + wave) .. + 7 of a, then of b; row r's piece c sits at
+    // place c ^ (r / 2 % 8)
+    uint32_t off_a[PARTS], off_b[PARTS], off_s[WORDS];
+    const int piece = (lane & 7) ^ ((4 * wave + (lane >> 4)) & 7);
+#pragma unroll
+    for (int u = 0; u < PARTS; ++u) {
+        const int r = 8 * (WAVES * u + wave) + (lane >> 3);
+        off_a[u] = (uint32_t)(min((int64_t)r, p.M - 1 - m0) * p.lda) + piece * 16;
+        off_b[u] = (uint32_t)(min((int64_t)r, p.N - 1 - n0) * p.ldb) + piece * 16;
+    }
+    // scales: 64 rows' words of four a load; the stage's first words of all rows (a's, then b's), then its second ones
+    i32x4 rsrc_s[WORDS];
+    int second[WORDS];
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) {
+        const int x = w * WAVES + wave, chunk = x % (2 * T / 64), r = chunk * 64 % T + lane;
+        second[w] = x / (2 * T / 64);
+        const bool of_a = chunk * 64 < T;
+        rsrc_s[w] = bytes_from(of_a ? q.ea + m0 * q.ld_ea : q.eb + n0 * q.ld_eb);
+        off_s[w] = (uint32_t)(of_a ? min((int64_t)r, p.M - 1 - m0) * q.ld_ea : min((int64_t)r, p.N - 1 - n0) * q.ld_eb);
+    }
+    const i32x4 rsrc_a = bytes_from(p.a + m0 * p.lda), rsrc_b = bytes_from(p.b + n0 * p.ldb);
+    const int last_word = (q.blocks - 1) >> 2;
+    const uint32_t beyond = piece * 32 >= ragged ? piece * 16 : 0;
+    // what takes a piece of stage kb beyond the row's end back into it
+    auto back_of = [&](int kb) { return RAGGED && kb == whole ? beyond : 0u; };
+    // request v of stage kb into place buf
+    auto request = [&](int v, int kb, int buf, uint32_t back) {
+        if (v < 2 * PARTS) {
+            const int u = v >> 1;
+            const uint32_t to = buf * S::STAGE + (v & 1) * T * 128 + (WAVES * u + wave) * 1024;
+            load_to_lds((v & 1) ? rsrc_b : rsrc_a, ((v & 1) ? off_b[u] : off_a[u]) - back, kb * 128, to);
+        } else {
+            const int w = v - 2 * PARTS;
+            load_word_to_lds(rsrc_s[w], off_s[w], min(2 * kb + second[w], last_word) * 4, DEPTH * S::STAGE + buf * S::SCALES + (w * WAVES + wave) * 256);
+        }
+    };
+
+    f32x16 acc[NI][NJ];
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+
+    i32x4 f[2][F];                                                            // fragments of two steps: a's, then b's
+    uint32_t sc[F], lo[F], hi[F];                                             // scales of the stage; of the next one as they are read
+    const uint32_t pick = half ? 0x07050301u : 0x06040200u;
+    // a lane's codes and scales of the last stage that count: all others become zero in a, and their scales some number
+    uint32_t tail[4][4], keep = 0;
+    if constexpr (RAGGED) {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const uint4 t = first_codes(make_uint4(~0u, ~0u, ~0u, ~0u), min(max(ragged - 64 * s - 32 * half, 0), 32));
+            tail[s][0] = t.x; tail[s][1] = t.y; tail[s][2] = t.z; tail[s][3] = t.w;
+            if (2 * s + half < q.blocks - 8 * whole) keep |= 0xffu << (8 * s);
+        }
+    }
+    const uint8_t *row_a = smem + (wm + at) * 128, *row_b = smem + (T + wn + at) * 128;
+    // fragment v of step s of the stage in place buf
+    auto read = [&](int v, int s, int buf) {
+        const uint8_t *row = (v < NI ? row_a + v * 4096 : row_b + (v - NI) * 4096) + buf * S::STAGE;
+        return *reinterpret_cast<const i32x4 *>(row + (((2 * s + half) ^ (at >> 1 & 7)) << 4));
+    };
+    auto read_scales = [&](int v, int buf) {
+        const int row = v < NI ? wm + v * 32 + at : T + wn + (v - NI) * 32 + at;
+        const uint32_t *w = reinterpret_cast<const uint32_t *>(smem + DEPTH * S::STAGE + buf * S::SCALES) + row;
+        lo[v] = w[0];
+        hi[v] = w[2 * T];
+    };
+    // all: ~0 for a whole stage, else 0
+    auto take_scales = [&](uint32_t all) {
+#pragma unroll
+        for (int v = 0; v < F; ++v) {
+            sc[v] = __builtin_amdgcn_perm(hi[v], lo[v], pick);
+            if constexpr (RAGGED) sc[v] = (sc[v] & (keep | all)) | (0x7f7f7f7fu & ~(keep | all));
+        }
+    };
+    auto multiply = [&](int i, int j, int s, uint32_t all) {
+        i32x4 x = f[s & 1][NI + j], y = f[s & 1][i];
+        if constexpr (RAGGED)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                if (j == 0) f[s & 1][i][w] &= (int)(tail[s][w] | all);
+                y[w] = f[s & 1][i][w];
+            }
+        const icq_i32x8 n = {x[0], x[1], x[2], x[3], 0, 0, 0, 0}, m = {y[0], y[1], y[2], y[3], 0, 0, 0, 0};
+        const int en = (int)sc[NI + j], em = (int)sc[i];
+        if (s == 0) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(n, m, acc[i][j], 4, 4, 0, en, 0, em);
+        else if (s == 1) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(n, m, acc[i][j], 4, 4, 1, en, 1, em);
+        else if (s == 2) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(n, m, acc[i][j], 4, 4, 2, en, 2, em);
+        else acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(n, m, acc[i][j], 4, 4, 3, en, 3, em);
+    };
+    auto all_of = [&](int kb) { return RAGGED && kb == whole ? 0u : ~0u; };
+
+    // beyond the last stage it is requested again: no branch in the loop
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) {
+        const int kb = min(k0 + d, last);
+        const uint32_t back = back_of(kb);
+#pragma unroll
+        for (int v = 0; v < LOADS; ++v)
+            if (d < DEPTH - 1 || v < FIRST) request(v, kb, d, back);
+    }
+    __builtin_amdgcn_s_waitcnt(loads_left((DEPTH - 2) * LOADS + FIRST));
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < F; ++v) {
+        f[0][v] = read(v, 0, 0);
+        read_scales(v, 0);
+    }
+    take_scales(all_of(k0));
+    int buf = 0, kb = k0;
+    do {
+        const int next_buf = (buf + 1) & (DEPTH - 1), last_buf = (buf + DEPTH - 1) & (DEPTH - 1);
+        const int late = min(kb + DEPTH - 1, last), later = min(kb + DEPTH, last);
+        const uint32_t back_late = back_of(late), back_later = back_of(later), all = all_of(kb);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            if (s == 3) {
+                __builtin_amdgcn_s_waitcnt(loads_left((DEPTH - 2) * LOADS));              // the next stage is here, later ones may not be
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup", "local");
+                __builtin_amdgcn_s_barrier();
+            }
+#pragma unroll
+            for (int t = 0; t < N; ++t) {
+                // requests and reads, spread over the step's matrix instructions
+#pragma unroll
+                for (int v = 0; v < LOADS; ++v) {
+                    if (s == 0 && v >= FIRST && (v - FIRST) * N / (LOADS - FIRST) == t) request(v, late, last_buf, back_late);
+                    if (s == 3 && v < FIRST && v * N / FIRST == t) request(v, later, buf, back_later);
+                }
+                multiply(t / NJ, t % NJ, s, all);
+#pragma unroll
+                for (int v = 0; v < F; ++v)
+                    if (v * N / F == t) {
+                        if (s == 3) read_scales(v, next_buf);
+                        f[(s + 1) & 1][v] = s < 3 ? read(v, s + 1, buf) : read(v, 0, next_buf);
+                    }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        take_scales(all_of(kb + 1));
+        buf = next_buf;
+    } while (++kb <= last);
+    __builtin_amdgcn_s_waitcnt(loads_left(0));
+    __syncthreads();                                                          // (a wavefront's part of the stages takes its results)
+    uint8_t *turn = smem + wave * (DEPTH * S::STAGE / WAVES);
+    void *out = p.splits > 1 ? static_cast<void *>(p.part + (int64_t)blockIdx.y * p.M * p.N) : p.out;
+    const int64_t ldo = p.splits > 1 ? p.N : p.ldo;
+    if (p.splits > 1) out_type = ICQ_F32;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) store_rows_as<NJ>(turn, acc[i], out, out_type, ldo, p.M, p.N, m0 + wm + i * 32, n0 + wn, lane);
+}
+
+template <typename S>
+int launch(const MxProduct &q, int out_type, hipStream_t s) {
+    const int tm = (int)((q.p.M + S::T - 1) / S::T), tn = (int)((q.p.N + S::T - 1) / S::T);
+    const uint32_t blocks = (uint32_t)((int64_t)tm * tn);
+    const auto go = [&](auto kernel) {
+        if (icq_allow_lds(reinterpret_cast<const void *>(kernel), S::LDS_BYTES, true) != hipSuccess) return ICQ_ERR_HIP;
+        for (uint32_t i = 0; i < blocks; i += ICQ_PRODUCT_BLOCKS)
+            hipLaunchKernelGGL(kernel, dim3(std::min(blocks - i, ICQ_PRODUCT_BLOCKS), (uint32_t)q.p.splits), dim3(S::THREADS), S::LDS_BYTES, s, q, tm, tn, out_type, i);
+        return icq_check_launch();
+    };
+    return q.p.K % 256 ? go(mx_tiles_kernel<S, true>) : go(mx_tiles_kernel<S, false>);
+}
+
+}  // namespace
+
+int icq_launch_mx_tiles(const MxProduct &q, icq_tiles tiles, int out_type, hipStream_t s) {
+    return tiles == ICQ_TILES_WIDE ? launch<Wide>(q, out_type, s) : tiles == ICQ_TILES_LITTLE ? launch<Little>(q, out_type, s)
+           : tiles == ICQ_TILES_DEEP ? launch<Deep>(q, out_type, s) : launch<Small>(q, out_type, s);
+}
