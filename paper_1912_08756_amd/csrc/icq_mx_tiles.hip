@@ -18,11 +18,12 @@ namespace {
 template <int NI_, int NJ_, int WM_, int WN_, int DEPTH_, int SHARE_>
 struct Shape {
     static constexpr int NI = NI_, NJ = NJ_, WM = WM_, WN = WN_, DEPTH = DEPTH_, SHARE = SHARE_, WAVES = WM * WN, THREADS = 64 * WAVES, T = 32 * NI * WM;
-    static constexpr int PARTS = T / (8 * WAVES), WORDS = 2 * T / 32 / WAVES, LOADS = 2 * PARTS + WORDS;   // of a wavefront for a stage: codes, scales
+    static constexpr int PARTS = T / (8 * WAVES), LOADS = 2 * PARTS;          // of a wavefront for a stage's codes: eight rows each
     static constexpr int FIRST = LOADS / 2;                                   // requested in the step of the barrier, the others in the next
-    static constexpr int STAGE = 2 * T * 128, SCALES = 2 * T * 8;             // bytes of a stage's codes, scales
-    static constexpr int LDS_BYTES = DEPTH * (STAGE + SCALES);
-    static_assert(32 * NJ * WN == T && T % 64 == 0 && WORDS >= 1 && (2 * T / 32) % WAVES == 0 && (DEPTH - 1) * LOADS < 64 && DEPTH * STAGE / WAVES >= 32 * (32 * NJ + 4) * 4,
+    static constexpr int WORDS = 2 * T / 32 / WAVES;                          // of a wavefront for four stages' scales: 32 rows each
+    static constexpr int STAGE = 2 * T * 128, SCALES = 2 * T * 32;            // bytes of a stage's codes, of four stages' scales
+    static constexpr int LDS_BYTES = DEPTH * STAGE + 2 * SCALES;
+    static_assert(32 * NJ * WN == T && WORDS >= 1 && (2 * T / 32) % WAVES == 0 && (DEPTH - 1) * LOADS < 64 && DEPTH * STAGE / WAVES >= 32 * (32 * NJ + 4) * 4,
                   "square tiles; whole loads; countable ones; results fit the stages");
     static_assert(SHARE * LDS_BYTES <= 160 * 1024, "fits the LDS");
 };
@@ -97,7 +98,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_
 
     // this lane's place in the loads: instruction u of a wavefront brings rows 8 (WAVES u + wave) .. + 7 of a, then of b; row r's piece c sits at
     // place c ^ (r / 2 % 8)
-    uint32_t off_a[PARTS], off_b[PARTS], off_s[WORDS];
+    uint32_t off_a[PARTS], off_b[PARTS];
     const int piece = (lane & 7) ^ ((4 * wave + (lane >> 4)) & 7);
 #pragma unroll
     for (int u = 0; u < PARTS; ++u) {
@@ -105,32 +106,31 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_
         off_a[u] = (uint32_t)(min((int64_t)r, p.M - 1 - m0) * p.lda) + piece * 16;
         off_b[u] = (uint32_t)(min((int64_t)r, p.N - 1 - n0) * p.ldb) + piece * 16;
     }
-    // scales: 64 rows' words of four a load; the stage's first words of all rows (a's, then b's), then its second ones
+    // four stages' scales are 32 bytes of a row, in two pieces: instruction w brings both of 32 rows
+    uint32_t off_s[WORDS];
     i32x4 rsrc_s[WORDS];
-    int second[WORDS];
 #pragma unroll
     for (int w = 0; w < WORDS; ++w) {
-        const int x = w * WAVES + wave, chunk = x % (2 * T / 64), r = chunk * 64 % T + lane;
-        second[w] = x / (2 * T / 64);
-        const bool of_a = chunk * 64 < T;
+        const int r = (w * WAVES + wave) * 32;
+        const bool of_a = r < T;
         rsrc_s[w] = bytes_from(of_a ? q.ea + m0 * q.ld_ea : q.eb + n0 * q.ld_eb);
-        off_s[w] = (uint32_t)(of_a ? min((int64_t)r, p.M - 1 - m0) * q.ld_ea : min((int64_t)r, p.N - 1 - n0) * q.ld_eb);
+        off_s[w] = (uint32_t)(of_a ? min((int64_t)(r + (lane >> 1)), p.M - 1 - m0) * q.ld_ea : min((int64_t)(r - T + (lane >> 1)), p.N - 1 - n0) * q.ld_eb);
     }
     const i32x4 rsrc_a = bytes_from(p.a + m0 * p.lda), rsrc_b = bytes_from(p.b + n0 * p.ldb);
-    const int last_word = (q.blocks - 1) >> 2;
+    const int words = (q.blocks + 3) >> 2;                                    // of four scales in a row
     const uint32_t beyond = piece * 32 >= ragged ? piece * 16 : 0;
     // what takes a piece of stage kb beyond the row's end back into it
     auto back_of = [&](int kb) { return RAGGED && kb == whole ? beyond : 0u; };
     // request v of stage kb into place buf
     auto request = [&](int v, int kb, int buf, uint32_t back) {
-        if (v < 2 * PARTS) {
-            const int u = v >> 1;
-            const uint32_t to = buf * S::STAGE + (v & 1) * T * 128 + (WAVES * u + wave) * 1024;
-            load_to_lds((v & 1) ? rsrc_b : rsrc_a, ((v & 1) ? off_b[u] : off_a[u]) - back, kb * 128, to);
-        } else {
-            const int w = v - 2 * PARTS;
-            load_word_to_lds(rsrc_s[w], off_s[w], min(2 * kb + second[w], last_word) * 4, DEPTH * S::STAGE + buf * S::SCALES + (w * WAVES + wave) * 256);
-        }
+        const int u = v >> 1;
+        load_to_lds((v & 1) ? rsrc_b : rsrc_a, ((v & 1) ? off_b[u] : off_a[u]) - back, kb * 128, buf * S::STAGE + (v & 1) * T * 128 + (WAVES * u + wave) * 1024);
+    };
+    // A piece of 16 bytes that would reach beyond its row starts earlier: its words sit by so many further in their place.
+    auto request_scales = [&](int kb, int place) {
+        const uint32_t from = (uint32_t)min(2 * kb + 4 * (lane & 1), words - 4) * 4u;
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) load_to_lds(rsrc_s[w], off_s[w] + from, 0, DEPTH * S::STAGE + place * S::SCALES + (w * WAVES + wave) * 1024);
     };
 
     f32x16 acc[NI][NJ];
@@ -160,11 +160,14 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_
         const uint8_t *row = (v < NI ? row_a + v * 4096 : row_b + (v - NI) * 4096) + buf * S::STAGE;
         return *reinterpret_cast<const i32x4 *>(row + (((2 * s + half) ^ (at >> 1 & 7)) << 4));
     };
-    auto read_scales = [&](int v, int buf) {
+    // the scales of stage kb: two words of a piece, the second only if there is one
+    auto scales_of = [&](int kb) { return DEPTH * S::STAGE + (((kb - k0) >> 2) & 1) * S::SCALES + (((kb - k0) >> 1) & 1) * 16; };
+    auto read_scales = [&](int v, int kb) {
         const int row = v < NI ? wm + v * 32 + at : T + wn + (v - NI) * 32 + at;
-        const uint32_t *w = reinterpret_cast<const uint32_t *>(smem + DEPTH * S::STAGE + buf * S::SCALES) + row;
-        lo[v] = w[0];
-        hi[v] = w[2 * T];
+        const int first = ((kb - k0) >> 1) * 4 + 2 * k0, at_word = 2 * kb - max(0, min(first, words - 4));
+        const uint8_t *w = smem + scales_of(kb) + row * 32;
+        lo[v] = *reinterpret_cast<const uint32_t *>(w + min(at_word, 3) * 4);
+        hi[v] = *reinterpret_cast<const uint32_t *>(w + min(at_word + 1, 3) * 4);
     };
     // all: ~0 for a whole stage, else 0
     auto take_scales = [&](uint32_t all) {
@@ -191,6 +194,12 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_
     };
     auto all_of = [&](int kb) { return RAGGED && kb == whole ? 0u : ~0u; };
 
+    if (words >= 4) request_scales(k0, 0);
+    else                                                                      // rows of fewer than 16 bytes: one by one, all there are
+        for (int r = tid; r < 2 * T; r += S::THREADS) {
+            const uint8_t *from = r < T ? q.ea + min(m0 + r, p.M - 1) * q.ld_ea : q.eb + min(n0 + r - T, p.N - 1) * q.ld_eb;
+            for (int w = 0; w < words; ++w) *reinterpret_cast<uint32_t *>(smem + DEPTH * S::STAGE + r * 32 + w * 4) = *reinterpret_cast<const uint32_t *>(from + w * 4);
+        }
     // beyond the last stage it is requested again: no branch in the loop
 #pragma unroll
     for (int d = 0; d < DEPTH; ++d) {
@@ -205,42 +214,47 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_
 #pragma unroll
     for (int v = 0; v < F; ++v) {
         f[0][v] = read(v, 0, 0);
-        read_scales(v, 0);
+        read_scales(v, k0);
     }
     take_scales(all_of(k0));
     int buf = 0, kb = k0;
-    do {
-        const int next_buf = (buf + 1) & (DEPTH - 1), last_buf = (buf + DEPTH - 1) & (DEPTH - 1);
-        const int late = min(kb + DEPTH - 1, last), later = min(kb + DEPTH, last);
-        const uint32_t back_late = back_of(late), back_later = back_of(later), all = all_of(kb);
+    do {                                                                      // four stages: their scales are in the LDS
+        if (kb + 4 <= last) request_scales(kb + 4, ((kb - k0) >> 2 & 1) ^ 1); // (nobody reads that place any more: three barriers since)
+        const int end = min(kb + 3, last);
+        do {
+            const int next_buf = (buf + 1) & (DEPTH - 1), last_buf = (buf + DEPTH - 1) & (DEPTH - 1);
+            const int late = min(kb + DEPTH - 1, last), later = min(kb + DEPTH, last), next = min(kb + 1, last);
+            const uint32_t back_late = back_of(late), back_later = back_of(later), all = all_of(kb);
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            if (s == 3) {
-                __builtin_amdgcn_s_waitcnt(loads_left((DEPTH - 2) * LOADS));              // the next stage is here, later ones may not be
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup", "local");
-                __builtin_amdgcn_s_barrier();
-            }
-#pragma unroll
-            for (int t = 0; t < N; ++t) {
-                // requests and reads, spread over the step's matrix instructions
-#pragma unroll
-                for (int v = 0; v < LOADS; ++v) {
-                    if (s == 0 && v >= FIRST && (v - FIRST) * N / (LOADS - FIRST) == t) request(v, late, last_buf, back_late);
-                    if (s == 3 && v < FIRST && v * N / FIRST == t) request(v, later, buf, back_later);
+            for (int s = 0; s < 4; ++s) {
+                if (s == 3) {
+                    // the next stage is here, and the next four's scales after the last; later stages may not be
+                    __builtin_amdgcn_s_waitcnt(loads_left((DEPTH - 2) * LOADS));
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup", "local");
+                    __builtin_amdgcn_s_barrier();
                 }
-                multiply(t / NJ, t % NJ, s, all);
 #pragma unroll
-                for (int v = 0; v < F; ++v)
-                    if (v * N / F == t) {
-                        if (s == 3) read_scales(v, next_buf);
-                        f[(s + 1) & 1][v] = s < 3 ? read(v, s + 1, buf) : read(v, 0, next_buf);
+                for (int t = 0; t < N; ++t) {
+                    // requests and reads, spread over the step's matrix instructions
+#pragma unroll
+                    for (int v = 0; v < LOADS; ++v) {
+                        if (s == 0 && v >= FIRST && (v - FIRST) * N / (LOADS - FIRST) == t) request(v, late, last_buf, back_late);
+                        if (s == 3 && v < FIRST && v * N / FIRST == t) request(v, later, buf, back_later);
                     }
-                __builtin_amdgcn_sched_barrier(0);
+                    multiply(t / NJ, t % NJ, s, all);
+#pragma unroll
+                    for (int v = 0; v < F; ++v)
+                        if (v * N / F == t) {
+                            if (s == 3) read_scales(v, next);
+                            f[(s + 1) & 1][v] = s < 3 ? read(v, s + 1, buf) : read(v, 0, next_buf);
+                        }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
-        }
-        take_scales(all_of(kb + 1));
-        buf = next_buf;
-    } while (++kb <= last);
+            take_scales(all_of(next));
+            buf = next_buf;
+        } while (++kb <= end);
+    } while (kb <= last);
     __builtin_amdgcn_s_waitcnt(loads_left(0));
     __syncthreads();                                                          // (a wavefront's part of the stages takes its results)
     uint8_t *turn = smem + wave * (DEPTH * S::STAGE / WAVES);
