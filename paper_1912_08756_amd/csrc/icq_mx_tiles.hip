@@ -20,10 +20,10 @@ struct Shape {
     static constexpr int NI = NI_, NJ = NJ_, WM = WM_, WN = WN_, DEPTH = DEPTH_, SHARE = SHARE_, WAVES = WM * WN, THREADS = 64 * WAVES, T = 32 * NI * WM;
     static constexpr int PARTS = T / (8 * WAVES), LOADS = 2 * PARTS;          // of a wavefront for a stage's codes: eight rows each
     static constexpr int FIRST = LOADS / 2;                                   // requested in the step of the barrier, the others in the next
-    static constexpr int WORDS = 2 * T / 32 / WAVES;                          // of a wavefront for four stages' scales: 32 rows each
+    static constexpr int WORDS = 2 * T / 32 / WAVES;                          // of a wavefront for four stages' scales: half of 64 rows' each
     static constexpr int STAGE = 2 * T * 128, SCALES = 2 * T * 32;            // bytes of a stage's codes, of four stages' scales
     static constexpr int LDS_BYTES = DEPTH * STAGE + 2 * SCALES;
-    static_assert(32 * NJ * WN == T && WORDS >= 1 && (2 * T / 32) % WAVES == 0 && (DEPTH - 1) * LOADS < 64 && DEPTH * STAGE / WAVES >= 32 * (32 * NJ + 4) * 4,
+    static_assert(32 * NJ * WN == T && T % 64 == 0 && WORDS >= 1 && (2 * T / 32) % WAVES == 0 && (DEPTH - 1) * LOADS < 64 && DEPTH * STAGE / WAVES >= 32 * (32 * NJ + 4) * 4,
                   "square tiles; whole loads; countable ones; results fit the stages");
     static_assert(SHARE * LDS_BYTES <= 160 * 1024, "fits the LDS");
 };
@@ -106,15 +106,18 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_
         off_a[u] = (uint32_t)(min((int64_t)r, p.M - 1 - m0) * p.lda) + piece * 16;
         off_b[u] = (uint32_t)(min((int64_t)r, p.N - 1 - n0) * p.ldb) + piece * 16;
     }
-    // four stages' scales are 32 bytes of a row, in two pieces: instruction w brings both of 32 rows
+    // four stages' scales are two pieces of 16 bytes of a row: an instruction brings one of 64 rows (in rows of 32 bytes they would
+    // meet on the same banks when read)
     uint32_t off_s[WORDS];
     i32x4 rsrc_s[WORDS];
+    int second[WORDS];
 #pragma unroll
     for (int w = 0; w < WORDS; ++w) {
-        const int r = (w * WAVES + wave) * 32;
+        const int x = w * WAVES + wave, r = x % (2 * T / 64) * 64;
         const bool of_a = r < T;
+        second[w] = x / (2 * T / 64);
         rsrc_s[w] = bytes_from(of_a ? q.ea + m0 * q.ld_ea : q.eb + n0 * q.ld_eb);
-        off_s[w] = (uint32_t)(of_a ? min((int64_t)(r + (lane >> 1)), p.M - 1 - m0) * q.ld_ea : min((int64_t)(r - T + (lane >> 1)), p.N - 1 - n0) * q.ld_eb);
+        off_s[w] = (uint32_t)(of_a ? min((int64_t)(r + lane), p.M - 1 - m0) * q.ld_ea : min((int64_t)(r - T + lane), p.N - 1 - n0) * q.ld_eb);
     }
     const i32x4 rsrc_a = bytes_from(p.a + m0 * p.lda), rsrc_b = bytes_from(p.b + n0 * p.ldb);
     const int words = (q.blocks + 3) >> 2;                                    // of four scales in a row
@@ -128,9 +131,9 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_
     };
     // A piece of 16 bytes that would reach beyond its row starts earlier: its words sit by so many further in their place.
     auto request_scales = [&](int kb, int place) {
-        const uint32_t from = (uint32_t)min(2 * kb + 4 * (lane & 1), words - 4) * 4u;
 #pragma unroll
-        for (int w = 0; w < WORDS; ++w) load_to_lds(rsrc_s[w], off_s[w] + from, 0, DEPTH * S::STAGE + place * S::SCALES + (w * WAVES + wave) * 1024);
+        for (int w = 0; w < WORDS; ++w)
+            load_to_lds(rsrc_s[w], off_s[w], min(2 * kb + 4 * second[w], words - 4) * 4, DEPTH * S::STAGE + place * S::SCALES + (w * WAVES + wave) * 1024);
     };
 
     f32x16 acc[NI][NJ];
@@ -161,13 +164,19 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_
         return *reinterpret_cast<const i32x4 *>(row + (((2 * s + half) ^ (at >> 1 & 7)) << 4));
     };
     // the scales of stage kb: two words of a piece, the second only if there is one
-    auto scales_of = [&](int kb) { return DEPTH * S::STAGE + (((kb - k0) >> 2) & 1) * S::SCALES + (((kb - k0) >> 1) & 1) * 16; };
+    auto scales_of = [&](int kb) { return DEPTH * S::STAGE + (((kb - k0) >> 2) & 1) * S::SCALES + (((kb - k0) >> 1) & 1) * 2 * T * 16; };
     auto read_scales = [&](int v, int kb) {
         const int row = v < NI ? wm + v * 32 + at : T + wn + (v - NI) * 32 + at;
         const int first = ((kb - k0) >> 1) * 4 + 2 * k0, at_word = 2 * kb - max(0, min(first, words - 4));
-        const uint8_t *w = smem + scales_of(kb) + row * 32;
-        lo[v] = *reinterpret_cast<const uint32_t *>(w + min(at_word, 3) * 4);
-        hi[v] = *reinterpret_cast<const uint32_t *>(w + min(at_word + 1, 3) * 4);
+        const uint8_t *w = smem + scales_of(kb) + row * 16;
+        if constexpr (RAGGED) {
+            lo[v] = *reinterpret_cast<const uint32_t *>(w + min(at_word, 3) * 4);
+            hi[v] = *reinterpret_cast<const uint32_t *>(w + min(at_word + 1, 3) * 4);
+        } else {                                                              // (an even number of words in a row)
+            const uint2 both = *reinterpret_cast<const uint2 *>(w + at_word * 4);
+            lo[v] = both.x;
+            hi[v] = both.y;
+        }
     };
     // all: ~0 for a whole stage, else 0
     auto take_scales = [&](uint32_t all) {
@@ -182,7 +191,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_
         if constexpr (RAGGED)
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                if (j == 0) f[s & 1][i][w] &= (int)(tail[s][w] | all);
+                if (j == (i % 2 ? NJ - 1 : 0)) f[s & 1][i][w] &= (int)(tail[s][w] | all);
                 y[w] = f[s & 1][i][w];
             }
         const icq_i32x8 n = {x[0], x[1], x[2], x[3], 0, 0, 0, 0}, m = {y[0], y[1], y[2], y[3], 0, 0, 0, 0};
@@ -198,7 +207,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_
     else                                                                      // rows of fewer than 16 bytes: one by one, all there are
         for (int r = tid; r < 2 * T; r += S::THREADS) {
             const uint8_t *from = r < T ? q.ea + min(m0 + r, p.M - 1) * q.ld_ea : q.eb + min(n0 + r - T, p.N - 1) * q.ld_eb;
-            for (int w = 0; w < words; ++w) *reinterpret_cast<uint32_t *>(smem + DEPTH * S::STAGE + r * 32 + w * 4) = *reinterpret_cast<const uint32_t *>(from + w * 4);
+            for (int w = 0; w < words; ++w) *reinterpret_cast<uint32_t *>(smem + DEPTH * S::STAGE + r * 16 + w * 4) = *reinterpret_cast<const uint32_t *>(from + w * 4);
         }
     // beyond the last stage it is requested again: no branch in the loop
 #pragma unroll
@@ -241,7 +250,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_
                         if (s == 0 && v >= FIRST && (v - FIRST) * N / (LOADS - FIRST) == t) request(v, late, last_buf, back_late);
                         if (s == 3 && v < FIRST && v * N / FIRST == t) request(v, later, buf, back_later);
                     }
-                    multiply(t / NJ, t % NJ, s, all);
+                    multiply(t / NJ, t / NJ % 2 ? NJ - 1 - t % NJ : t % NJ, s, all);         // (neighbours share an operand)
 #pragma unroll
                     for (int v = 0; v < F; ++v)
                         if (v * N / F == t) {
