@@ -2,17 +2,34 @@
 #pragma once
 #include "icq_matmul_plan.h"
 
-// Tiles of 256 x 256, of 128 x 128 with two stages in the LDS or four, or of 64 x 64; a stage is 256 values along K.
+constexpr int ICQ_MX_FEW_WAVES = 8;                // of a block of the kernel for few rows
+
+// `few` rows of a: wavefronts of 64 rows of b or of 16, `along` of a block's share rows and take parts of the contraction.  Else tiles: of 256 x 256, of
+// 128 x 128 with two stages in the LDS or four, or of 64 x 64.
 struct icq_mx_plan {
-    bool few;
+    bool few, wide;
+    int along;
     icq_tiles tiles;
-    int splits, per;           // parts of the contraction, stages in each
+    int splits, per;           // parts of the contraction between blocks, steps of 256 values in each
 };
 
 static inline icq_mx_plan icq_plan_mx(int64_t M, int64_t N, int64_t K, int num_cu) {
     const int64_t stages = (K + 255) / 256;
-    icq_mx_plan best = {M <= 16, ICQ_TILES_SMALL, 1, (int)stages};
-    if (best.few) return best;
+    icq_mx_plan best = {M <= 16 || (M <= 32 && N <= 16 * (int64_t)num_cu), false, 1, ICQ_TILES_SMALL, 1, (int)stages};
+    if (best.few) {
+        best.wide = M <= 16 && N >= 64 * (int64_t)num_cu;
+        // as many wavefronts as have a step, until each compute unit has sixteen
+        const int64_t groups = (N + (best.wide ? 64 : 16) - 1) / (best.wide ? 64 : 16);
+        while (best.along < ICQ_MX_FEW_WAVES && 2 * best.along <= stages && groups * best.along < 16 * (int64_t)num_cu) best.along *= 2;
+        // and as many blocks, while a wavefront keeps four steps
+        const int64_t blocks = (groups * best.along + ICQ_MX_FEW_WAVES - 1) / ICQ_MX_FEW_WAVES, idle = num_cu / (blocks > 0 ? blocks : 1);
+        const int64_t most = stages / (4 * best.along), n = idle < most ? idle : most;
+        if (n > 1) {
+            best.per = (int)((stages + n - 1) / n);
+            best.splits = (int)((stages + best.per - 1) / best.per);
+        }
+        return best;
+    }
     double least = -1.0;
     for (int64_t T = 256; T >= 64; T /= 2) {
         const int64_t tiles = ((M + T - 1) / T) * ((N + T - 1) / T);
