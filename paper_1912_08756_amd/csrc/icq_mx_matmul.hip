@@ -16,7 +16,7 @@ Held held(int64_t M, int64_t N, int64_t K, bool values, const icq_mx_plan &plan)
     Held h = {};
     h.codes = plan.splits > 1 ? icq_align_up((size_t)plan.splits * M * N * sizeof(float), ICQ_ALIGN) : 0;
     h.bytes = h.codes;
-    if (!values || plan.few) return h;
+    if (!values || (plan.few && icq_mx_few_quantises(M, plan.per))) return h;      // (the kernel for few rows quantises them itself)
     h.ld = (K + 31) / 32 * 16;
     h.ld_s = (K + 127) / 128 * 4;
     h.scales = h.codes + icq_align_up((size_t)M * h.ld, ICQ_ALIGN);
@@ -71,18 +71,16 @@ ICQ_EXPORT int icq_mx_matmul(const void *a, int a_type, int64_t lda, const uint8
     p.splits = plan.splits; p.per = plan.per;
     p.part = static_cast<float *>(workspace);
     int rc = ICQ_OK;
-    if (plan.few) rc = icq_launch_mx_few(q, plan, a, a_type, lda, scaling == ICQ_MX_FIT, out_type, s);
-    else {
-        if (values(a_type)) {
-            MxQuantize z = {};
-            z.x = a; z.rows = M; z.cols = K; z.ldx = lda;
-            z.codes = static_cast<uint8_t *>(workspace) + h.codes; z.scales = static_cast<uint8_t *>(workspace) + h.scales; z.ld = h.ld; z.ld_s = h.ld_s;
-            z.across = (int)((K + 127) / 128);
-            z.fit = scaling == ICQ_MX_FIT;
-            if ((rc = icq_launch_mx_rows(z, a_type, s)) != ICQ_OK) return rc;
-            p.a = z.codes; p.lda = h.ld; q.ea = z.scales; q.ld_ea = h.ld_s;
-        }
-        rc = icq_launch_mx_tiles(q, plan.tiles, out_type, s);
+    if (h.scales > 0) {
+        MxQuantize z = {};
+        z.x = a; z.rows = M; z.cols = K; z.ldx = lda;
+        z.codes = static_cast<uint8_t *>(workspace) + h.codes; z.scales = static_cast<uint8_t *>(workspace) + h.scales; z.ld = h.ld; z.ld_s = h.ld_s;
+        z.across = (int)((K + 127) / 128);
+        z.fit = scaling == ICQ_MX_FIT;
+        if ((rc = icq_launch_mx_rows(z, a_type, s)) != ICQ_OK) return rc;
+        p.a = z.codes; p.lda = h.ld; q.ea = z.scales; q.ld_ea = h.ld_s;
+        a_type = ICQ_E2M1;
     }
+    rc = plan.few ? icq_launch_mx_few(q, plan, cu, a, a_type, lda, scaling == ICQ_MX_FIT, out_type, s) : icq_launch_mx_tiles(q, plan.tiles, out_type, s);
     return rc != ICQ_OK || p.splits == 1 ? rc : icq_launch_product_join(p, out_type, s);
 }

@@ -4,7 +4,12 @@
 
 constexpr int ICQ_MX_FEW_WAVES = 8;                // of a block of the kernel for few rows
 
-// `few` rows of a: wavefronts of 64 rows of b or of 16, `along` of a block's share rows and take parts of the contraction.  Else tiles: of 256 x 256, of
+// Whether that kernel quantises a's values itself, in every block, `per` steps of 256 values of M rows: 68 KB of the LDS at most, and while that costs
+// less than a launch of its own (values against held, 16384 x 4096, 16 steps: 1 row 8.8 - 8.6, 4 rows 10.3 - 9.2, 8 rows 12.4 - 9.8, 16 rows 16.9 - 10.8; a launch
+// about 2).
+static inline bool icq_mx_few_quantises(int64_t M, int64_t per) { return per <= 32 && M * per <= 64; }
+
+// `few` rows of a: wavefronts of 32 rows of b or of 16, `along` of a block's share rows and take parts of the contraction.  Else tiles: of 256 x 256, of
 // 128 x 128 with two stages in the LDS or four, or of 64 x 64.
 struct icq_mx_plan {
     bool few, wide;
@@ -15,12 +20,16 @@ struct icq_mx_plan {
 
 static inline icq_mx_plan icq_plan_mx(int64_t M, int64_t N, int64_t K, int num_cu) {
     const int64_t stages = (K + 255) / 256;
-    icq_mx_plan best = {M <= 16 || (M <= 32 && N <= 16 * (int64_t)num_cu), false, 1, ICQ_TILES_SMALL, 1, (int)stages};
+    // (N K large: the tiles' loads into the LDS read faster, 6.3 TB/s against 5.5: 1 x 65536 x 8192 45 against 50 us, 16 x 65536 x 8192 47 against 67;
+    // 16 x 16384 x 4096 8.3 against 10.8, 1 x 16384 x 4096 8.3 against 8.6)
+    const bool long_rows = K >= 4096 && N >= 64 * (int64_t)num_cu && (M >= 8 || N * K >= (int64_t)1 << 28);
+    icq_mx_plan best = {M <= 16 && !long_rows, false, 1, ICQ_TILES_SMALL, 1, (int)stages};
     if (best.few) {
-        best.wide = M <= 16 && N >= 64 * (int64_t)num_cu;
-        // as many wavefronts as have a step, until each compute unit has sixteen
-        const int64_t groups = (N + (best.wide ? 64 : 16) - 1) / (best.wide ? 64 : 16);
-        while (best.along < ICQ_MX_FEW_WAVES && 2 * best.along <= stages && groups * best.along < 16 * (int64_t)num_cu) best.along *= 2;
+        best.wide = N >= 64 * (int64_t)num_cu;
+        const int64_t groups = (N + (best.wide ? 32 : 16) - 1) / (best.wide ? 32 : 16);
+        // four wavefronts to a row as far as there are steps, eight where there are few rows
+        while (best.along < 4 && 2 * best.along <= stages) best.along *= 2;
+        if (8 <= stages && groups * best.along < 8 * (int64_t)num_cu) best.along = 8;
         // and as many blocks, while a wavefront keeps four steps
         const int64_t blocks = (groups * best.along + ICQ_MX_FEW_WAVES - 1) / ICQ_MX_FEW_WAVES, idle = num_cu / (blocks > 0 ? blocks : 1);
         const int64_t most = stages / (4 * best.along), n = idle < most ? idle : most;
