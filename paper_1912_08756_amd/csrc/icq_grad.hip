@@ -35,48 +35,69 @@ struct icq_grad_list {
 
 namespace {
 
-// Visits a chunk's values: each(pointer offset in g, offset in out, n) with n = 8 (neighbours) or fewer.
-template <typename F>
-__device__ __forceinline__ void visit(const Chunk &c, F each) {
+// Values that a thread takes at a time: 16 bytes of the narrower of its types, or 8 beside 16 of the wider, so that a wavefront's loads and stores are
+// whole stretches (eight 16-bit values beside eight of 32 bits, 32 bytes a lane in two stores: 3.2 TB/s).
+template <int FROM, int TO>
+constexpr int at_once() { return FROM == ICQ_F32 || TO == ICQ_F32 ? 4 : 8; }
+
+template <int TYPE, int N>
+struct Values { uint32_t w[N * (TYPE == ICQ_F32 ? 4 : 2) / 4]; };
+
+template <int TYPE, int N>
+__device__ __forceinline__ void unpack(const Values<TYPE, N> &v, float *x) {
+    if constexpr (TYPE == ICQ_F32) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = __uint_as_float(v.w[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) IcqElem<TYPE>::unpack2(v.w[i], x + 2 * i);
+    }
+}
+
+template <int TYPE, int N>
+__device__ __forceinline__ Values<TYPE, N> pack(const float *x) {
+    Values<TYPE, N> v;
+    if constexpr (TYPE == ICQ_F32) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v.w[i] = __float_as_uint(x[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) v.w[i] = IcqElem<TYPE>::pack2(x[2 * i], x[2 * i + 1]);
+    }
+    return v;
+}
+
+// Visits a chunk's values: take(place in g, its raw values) for N neighbours at a time, LOADS of them requested before the first is taken, and one(place in g,
+// place in out) for what is left.
+template <int TYPE, int N, int LOADS, typename F, typename G>
+__device__ __forceinline__ void visit(const Chunk &c, F take, G one) {
+    typedef typename IcqElem<TYPE>::raw raw;
+    const raw *g = static_cast<const raw *>(c.g);
     if (c.rows == 1) {
-        for (uint32_t i = threadIdx.x * 8u; i < c.cols; i += THREADS * 8u) each((int64_t)i, (int64_t)i, min(8u, c.cols - i));
-    } else {
-        const uint32_t pieces = (c.cols + 7u) / 8u;
-        for (uint32_t i = threadIdx.x; i < c.rows * pieces; i += THREADS) {
-            const uint32_t r = i / pieces, k = i % pieces * 8u;
-            each((int64_t)r * c.ld + k, (int64_t)r * c.ld_out + k, min(8u, c.cols - k));
+        constexpr uint32_t STEP = THREADS * N;
+        const uint32_t groups = c.cols / N;                                   // whole ones
+        uint32_t i = threadIdx.x;
+        for (; i + (LOADS - 1) * THREADS < groups; i += LOADS * THREADS) {
+            Values<TYPE, N> v[LOADS];
+#pragma unroll
+            for (int k = 0; k < LOADS; ++k) __builtin_memcpy(&v[k], g + (size_t)i * N + k * STEP, sizeof v[k]);        // (any address will do)
+#pragma unroll
+            for (int k = 0; k < LOADS; ++k) take((int64_t)i * N + k * STEP, v[k]);
         }
-    }
-}
-
-template <int TYPE>
-__device__ __forceinline__ void read(const void *g, int64_t at, uint32_t n, float *x) {
-    typedef IcqElem<TYPE> E;
-    const typename E::raw *p = static_cast<const typename E::raw *>(g) + at;
-    if (n == 8) {
-        uint4 v[8 / E::PER];
-        __builtin_memcpy(v, p, sizeof v);                                      // (the memory pipe takes 16 bytes from any address)
-#pragma unroll
-        for (int h = 0; h < 8 / E::PER; ++h) E::unpack(v[h], x + h * E::PER);
+        for (; i < groups; i += THREADS) {
+            Values<TYPE, N> v;
+            __builtin_memcpy(&v, g + (size_t)i * N, sizeof v);
+            take((int64_t)i * N, v);
+        }
+        const uint32_t rest = groups * N + threadIdx.x;
+        if (rest < c.cols) one(rest, rest);
     } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = i < (int)n ? E::get(p[i]) : 0.0f;
-    }
-}
-
-template <int TYPE>
-__device__ __forceinline__ void write(void *out, int64_t at, uint32_t n, const float *x) {
-    typedef IcqElem<TYPE> E;
-    typename E::raw *p = static_cast<typename E::raw *>(out) + at;
-    if (n == 8) {
-        uint4 v[8 / E::PER];
-#pragma unroll
-        for (int h = 0; h < 8 / E::PER; ++h) v[h] = E::pack(x + h * E::PER);
-        __builtin_memcpy(p, v, sizeof v);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < (int)n) p[i] = E::put(x[i]);
+        // rows apart: value by value (their lines are whole in the caches)
+        const uint32_t values = c.rows * c.cols;
+        for (uint32_t i = threadIdx.x; i < values; i += THREADS) {
+            const uint32_t r = i / c.cols, k = i % c.cols;
+            one((int64_t)r * c.ld + k, (int64_t)r * c.ld_out + k);
+        }
     }
 }
 
@@ -93,18 +114,24 @@ __device__ __forceinline__ double block_sum(double x, double *s) {
 }
 
 template <int TYPE>
-__device__ double squares(const Chunk &c) {
+__device__ __forceinline__ double squares(const Chunk &c) {
+    constexpr int N = TYPE == ICQ_F32 ? 4 : 8;
     double sum = 0.0;
-    visit(c, [&](int64_t at, int64_t, uint32_t n) {
-        float x[8];
-        read<TYPE>(c.g, at, n, x);
+    visit<TYPE, N, 4>(c,
+        [&](int64_t, const Values<TYPE, N> &v) {
+            float x[N];
+            unpack<TYPE, N>(v, x);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum = fma((double)x[i], (double)x[i], sum);
-    });
+            for (int i = 0; i < N; ++i) sum = fma((double)x[i], (double)x[i], sum);
+        },
+        [&](int64_t at, int64_t) {
+            const double x = (double)IcqElem<TYPE>::get(static_cast<const typename IcqElem<TYPE>::raw *>(c.g)[at]);
+            sum = fma(x, x, sum);
+        });
     return sum;
 }
 
-__global__ __launch_bounds__(THREADS) void grad_squares_kernel(const Chunk *chunks, int count, double *part) {
+__global__ __launch_bounds__(THREADS) void grad_squares_kernel(const Chunk *__restrict__ chunks, int count, double *part) {
     __shared__ double s[THREADS / 64];
     double sum = 0.0;
     for (int k = blockIdx.x; k < count; k += gridDim.x) {
@@ -128,19 +155,26 @@ __global__ __launch_bounds__(THREADS) void grad_norm_kernel(const double *part, 
     if (threadIdx.x == 0) *norm = x;
 }
 
-template <int TYPE, int OUT>
-__device__ void scale_chunk(const Chunk &c, float factor) {
-    visit(c, [&](int64_t at, int64_t to, uint32_t n) {
-        float x[8];
-        read<TYPE>(c.g, at, n, x);
+template <int FROM, int TO>
+__device__ __forceinline__ void scale_chunk(const Chunk &c, float factor) {
+    constexpr int N = at_once<FROM, TO>();
+    typedef typename IcqElem<TO>::raw raw;
+    raw *out = static_cast<raw *>(c.out);
+    visit<FROM, N, 4>(c,
+        [&](int64_t at, const Values<FROM, N> &v) {
+            float x[N];
+            unpack<FROM, N>(v, x);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] *= factor;
-        write<OUT>(c.out, to, n, x);
-    });
+            for (int i = 0; i < N; ++i) x[i] *= factor;
+            const Values<TO, N> w = pack<TO, N>(x);
+            __builtin_memcpy(out + at, &w, sizeof w);
+        },
+        [&](int64_t at, int64_t to) { out[to] = IcqElem<TO>::put(IcqElem<FROM>::get(static_cast<const typename IcqElem<FROM>::raw *>(c.g)[at]) * factor); });
 }
 
-// part: the blocks' sums of the squares, from which the norm comes (block 0 writes it); nullptr: it is there.
-__global__ __launch_bounds__(THREADS) void grad_clip_kernel(const Chunk *chunks, int count, const double *part, int parts, float scale, float max_norm, float *norm) {
+// part: the blocks' sums of the squares, from which the norm comes (block 0 writes it); nullptr: it is there.  The chunks in the reverse of the order in
+// which their squares were summed: the last ones are still in the caches.
+__global__ __launch_bounds__(THREADS) void grad_clip_kernel(const Chunk *__restrict__ chunks, int count, const double *part, int parts, float scale, float max_norm, float *norm) {
     __shared__ double s[THREADS / 64];
     float x;
     if (part) {
@@ -150,7 +184,7 @@ __global__ __launch_bounds__(THREADS) void grad_clip_kernel(const Chunk *chunks,
         x = *norm;
     }
     const float factor = x <= max_norm ? scale : scale * (max_norm / x);
-    for (int k = blockIdx.x; k < count; k += gridDim.x) {
+    for (int k = count - 1 - blockIdx.x; k >= 0; k -= gridDim.x) {
         const Chunk c = chunks[k];
         if (factor == 1.0f && c.g == c.out) continue;
         ICQ_FOR_TYPE(c.type, constexpr int FROM = TYPE; ICQ_FOR_TYPE(c.out_type, scale_chunk<FROM, TYPE>(c, factor)))

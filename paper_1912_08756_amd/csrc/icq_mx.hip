@@ -52,12 +52,14 @@ __global__ __launch_bounds__(256) void mx_rows_kernel(MxQuantize a, int64_t firs
 // block along a row is four neighbouring lanes' and one down a column four lanes' 16 apart.
 // SQUARE: one scale for each 32 x 32.
 template <int TYPE, bool SQUARE>
-__global__ __launch_bounds__(256) void mx_tile_kernel(MxQuantize a, uint32_t first_tile) {
+__global__ __launch_bounds__(256) void mx_tile_kernel(MxQuantize a, uint32_t first_tile, uint32_t tiles) {
     constexpr int WORDS = Eight<TYPE>::WORDS;
     __shared__ __attribute__((aligned(16))) uint8_t s_turn[128 * 80];          // columns' 64 bytes of codes, 16 bytes apart: column 8 g + j at place 16 j + g
     __shared__ uint8_t s_rows[128 * 4], s_cols[128 * 4];                       // scales: of the tile's rows, of its columns
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane & 15, h = lane >> 4;
-    const uint32_t tile = first_tile + blockIdx.x;
+    // XCD blockIdx % 8 takes a contiguous share of the launch's tiles: neighbours' halves of a line of codes, and their scales, meet in one cache
+    const uint32_t xcd = blockIdx.x % 8, q8 = tiles / 8, r8 = tiles % 8;
+    const uint32_t tile = first_tile + xcd * q8 + min(xcd, r8) + blockIdx.x / 8;
     const int bc = (int)(tile % (uint32_t)a.across), br = (int)(tile / (uint32_t)a.across);
     const int64_t r0 = (int64_t)br * 128 + 32 * wave + 8 * h, c0 = (int64_t)bc * 128 + 8 * g;
     const int64_t wide = (a.cols + 31) & ~(int64_t)31, tall = (a.rows + 31) & ~(int64_t)31;
@@ -188,8 +190,8 @@ int launch_tiles(const MxQuantize &a, bool square, hipStream_t s) {
     const int64_t tiles = (int64_t)a.across * a.down;
     for (int64_t t = 0; t < tiles; t += TILES) {
         const dim3 grid((uint32_t)(tiles - t < TILES ? tiles - t : TILES));
-        if (square) hipLaunchKernelGGL(HIP_KERNEL_NAME(mx_tile_kernel<TYPE, true>), grid, dim3(256), 0, s, a, (uint32_t)t);
-        else hipLaunchKernelGGL(HIP_KERNEL_NAME(mx_tile_kernel<TYPE, false>), grid, dim3(256), 0, s, a, (uint32_t)t);
+        if (square) hipLaunchKernelGGL(HIP_KERNEL_NAME(mx_tile_kernel<TYPE, true>), grid, dim3(256), 0, s, a, (uint32_t)t, grid.x);
+        else hipLaunchKernelGGL(HIP_KERNEL_NAME(mx_tile_kernel<TYPE, false>), grid, dim3(256), 0, s, a, (uint32_t)t, grid.x);
     }
     return icq_check_launch();
 }
