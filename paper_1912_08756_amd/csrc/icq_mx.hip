@@ -48,6 +48,10 @@ __global__ __launch_bounds__(256) void mx_rows_kernel(MxQuantize a, int64_t firs
     if (at == 0) *reinterpret_cast<uint32_t *>(a.scales + r * a.ld_s + group * 4) = scales;
 }
 
+// Tiles are taken four rows of them at a time, so that lines of the transposed codes, which two tiles one above the other share, are written whole too
+// (16384 x 16384 bf16 both ways, 1, 2, 4, 8 rows: 223, 197, 186, 214 us).
+constexpr uint32_t HIGH = 4;
+
 // A 128 x 128 tile per block; a wavefront has 32 rows of it, lane (g, h) rows 8 h .. 8 h + 7 of them in columns 8 g .. 8 g + 7, so that a
 // block along a row is four neighbouring lanes' and one down a column four lanes' 16 apart.
 // SQUARE: one scale for each 32 x 32.
@@ -60,7 +64,8 @@ __global__ __launch_bounds__(256) void mx_tile_kernel(MxQuantize a, uint32_t fir
     // XCD blockIdx % 8 takes a contiguous share of the launch's tiles: neighbours' halves of a line of codes, and their scales, meet in one cache
     const uint32_t xcd = blockIdx.x % 8, q8 = tiles / 8, r8 = tiles % 8;
     const uint32_t tile = first_tile + xcd * q8 + min(xcd, r8) + blockIdx.x / 8;
-    const int bc = (int)(tile % (uint32_t)a.across), br = (int)(tile / (uint32_t)a.across);
+    const uint32_t band = tile / (HIGH * (uint32_t)a.across), in = tile % (HIGH * (uint32_t)a.across), high = min(HIGH, (uint32_t)a.down - HIGH * band);
+    const int bc = (int)(in / high), br = (int)(HIGH * band + in % high);
     const int64_t r0 = (int64_t)br * 128 + 32 * wave + 8 * h, c0 = (int64_t)bc * 128 + 8 * g;
     const int64_t wide = (a.cols + 31) & ~(int64_t)31, tall = (a.rows + 31) & ~(int64_t)31;
     Eight<TYPE> v[8];
