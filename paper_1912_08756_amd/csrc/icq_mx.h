@@ -68,6 +68,6 @@ struct MxQuantize {
 // Rows of blocks of 32 (icq_mx.hip): what icq_mx_quantize does for `codes` alone with block_rows = 1.
 int icq_launch_mx_rows(const MxQuantize &a, int x_type, hipStream_t s);
 // The product in tiles, p.splits parts of the contraction; a step along K is 256 values (icq_mx_tiles.hip).
-int icq_launch_mx_tiles(const MxProduct &q, icq_tiles tiles, int out_type, hipStream_t s);
+int icq_launch_mx_tiles(const MxProduct &q, icq_tiles tiles, int num_cu, int out_type, hipStream_t s);
 // The product of few rows of a, held (a_type ICQ_E2M1) or as values x (icq_mx_few.hip).
 int icq_launch_mx_few(const MxProduct &q, const icq_mx_plan &plan, int num_cu, const void *x, int a_type, int64_t ldx, bool fit, int out_type, hipStream_t s);

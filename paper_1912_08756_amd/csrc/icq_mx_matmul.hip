@@ -81,6 +81,6 @@ ICQ_EXPORT int icq_mx_matmul(const void *a, int a_type, int64_t lda, const uint8
         p.a = z.codes; p.lda = h.ld; q.ea = z.scales; q.ld_ea = h.ld_s;
         a_type = ICQ_E2M1;
     }
-    rc = plan.few ? icq_launch_mx_few(q, plan, cu, a, a_type, lda, scaling == ICQ_MX_FIT, out_type, s) : icq_launch_mx_tiles(q, plan.tiles, out_type, s);
+    rc = plan.few ? icq_launch_mx_few(q, plan, cu, a, a_type, lda, scaling == ICQ_MX_FIT, out_type, s) : icq_launch_mx_tiles(q, plan.tiles, cu, out_type, s);
     return rc != ICQ_OK || p.splits == 1 ? rc : icq_launch_product_join(p, out_type, s);
 }
