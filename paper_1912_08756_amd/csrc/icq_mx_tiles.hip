@@ -34,36 +34,23 @@ typedef Shape<2, 2, 2, 2, 2, 2> Small;
 typedef Shape<2, 2, 2, 2, 4, 1> Deep;
 typedef Shape<1, 1, 2, 2, 4, 2> Little;
 
-// Rows of 32 NJ words in the LDS into the result; a row's 16-byte pieces are permuted by its number.
-template <int TYPE, int NJ>
-__device__ __forceinline__ void rows_from(const float *turn, void *out, int64_t ldo, int64_t M, int64_t N, int64_t m0, int64_t n0, int lane) {
-    typedef IcqElem<TYPE> E;
-    typedef typename E::raw raw;
-    constexpr int WIDTH = 32 * NJ, PER = E::PER, LANES = WIDTH / PER, AT_ONCE = 64 / LANES;
-    const int c = lane % LANES * PER, rows = (int)min((int64_t)32, M - m0), left = (int)min((int64_t)PER, N - n0 - c);
-    raw *to = static_cast<raw *>(out) + (m0 + lane / LANES) * ldo + n0 + c;
-#pragma unroll 4
-    for (int r0 = 0; r0 < 32; r0 += AT_ONCE, to += AT_ONCE * ldo) {
-        const int r = r0 + lane / LANES;
-        if (r >= rows) break;
-        float x[PER];
-#pragma unroll
-        for (int k = 0; k < PER; k += 4) *reinterpret_cast<icq_f32x4 *>(x + k) = *reinterpret_cast<const icq_f32x4 *>(turn + r * WIDTH + (((c + k) / 4 ^ r) & (WIDTH / 4 - 1)) * 4);
-        if (left == PER) {
-            const uint4 v = E::pack(x);
-            __builtin_memcpy(to, &v, 16);                                     // (to any address)
-        } else {
-            for (int e = 0; e < left; ++e) to[e] = E::put(x[e]);
-        }
+// PER values of a row as 16 bytes of the result's type; bf16: of the two types of 16 bits.
+template <bool F32>
+__device__ __forceinline__ uint4 sixteen(const float *x, bool bf16) {
+    if constexpr (F32) return IcqElem<ICQ_F32>::pack(x);
+    else {
+        const uint4 a = IcqElem<ICQ_BF16>::pack(x), b = IcqElem<ICQ_F16>::pack(x);
+        return make_uint4(bf16 ? a.x : b.x, bf16 ? a.y : b.y, bf16 ? a.z : b.z, bf16 ? a.w : b.w);
     }
 }
 
 // 32 rows and 32 NJ columns of the result, whole rows at a time: in the accumulators a lane has four neighbours of one row and the lanes 32 rows, whose
 // stores would be 16 bytes here and there (64 bytes, with registers exchanged between lanes, took 2 us more for a tile of 256 x 256 than this).  They go into
-// the LDS as they are, where they lie: a branch for each type around them would have the compiler move and spill them.  turn: 32 rows of 32 NJ words.
-template <int NJ>
-__device__ __forceinline__ void store_rows_as(float *turn, const f32x16 *acc, void *out, int type, int64_t ldo, int64_t M, int64_t N, int64_t m0, int64_t n0, int lane) {
-    constexpr int WIDTH = 32 * NJ;
+// the LDS as they are, where they lie: branches around them would have the compiler move and spill them.  turn: 32 rows of 32 NJ words, a row's
+// 16-byte pieces permuted by its number.
+template <bool F32, int NJ>
+__device__ __forceinline__ void store_rows_as(float *turn, const f32x16 *acc, void *out, bool bf16, int64_t ldo, int64_t M, int64_t N, int64_t m0, int64_t n0, int lane) {
+    constexpr int WIDTH = 32 * NJ, PER = F32 ? 4 : 8, LANES = WIDTH / PER, AT_ONCE = 64 / LANES, TIMES = 32 / AT_ONCE, SIZE = F32 ? 4 : 2;
     const int at = lane & 31, half = lane >> 5;
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
@@ -75,7 +62,39 @@ __device__ __forceinline__ void store_rows_as(float *turn, const f32x16 *acc, vo
         }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    ICQ_FOR_TYPE(type, rows_from<TYPE, NJ>(turn, out, ldo, M, N, m0, n0, lane))
+    const int c = lane % LANES * PER, r = lane / LANES;
+    float x[TIMES][PER];
+#pragma unroll
+    for (int t = 0; t < TIMES; ++t)
+#pragma unroll
+        for (int k = 0; k < PER; k += 4) *reinterpret_cast<icq_f32x4 *>(x[t] + k) = *reinterpret_cast<const icq_f32x4 *>(turn + (t * AT_ONCE + r) * WIDTH + (((c + k) / 4 ^ (t * AT_ONCE + r)) & (WIDTH / 4 - 1)) * 4);
+    uint8_t *to = static_cast<uint8_t *>(out) + ((m0 + r) * ldo + n0 + c) * SIZE;
+    const int64_t step = AT_ONCE * ldo * SIZE;
+    if (m0 + 32 <= M && n0 + WIDTH <= N) {
+#pragma unroll
+        for (int t = 0; t < TIMES; ++t) {
+            const uint4 v = sixteen<F32>(x[t], bf16);
+            __builtin_memcpy(to + t * step, &v, 16);                          // (to any address)
+        }
+        return;
+    }
+    const int left = (int)min((int64_t)PER, N - n0 - c);
+#pragma unroll
+    for (int t = 0; t < TIMES; ++t) {
+        const uint4 v = sixteen<F32>(x[t], bf16);
+        if (m0 + t * AT_ONCE + r >= M || left <= 0) continue;
+        if (left >= PER) {
+            __builtin_memcpy(to + t * step, &v, 16);
+            continue;
+        }
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int e = 0; e < PER - 1; ++e)
+            if (e < left) {
+                if constexpr (F32) reinterpret_cast<uint32_t *>(to + t * step)[e] = w[e];
+                else reinterpret_cast<uint16_t *>(to + t * step)[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+            }
+    }
 }
 
 // Where the codes of a tile's rows lie, and this lane's places in them.
@@ -85,11 +104,11 @@ struct Target {
     uint32_t off_a[S::PARTS], off_b[S::PARTS];
 };
 
-// RAGGED: the last stage is not whole.
+// RAGGED: the last stage is not whole.  F32: the result's type (or that of the parts), else one of 16 bits.
 // A block takes tiles blockIdx.x, + gridDim.x, ...: more than one only where S::ON, the contraction is not in parts and a row has 16 bytes of
 // scales.  The requests go on into the next tile: when this one's results are stored, the next one's first stage has arrived and the second is under way.
-template <typename S, bool RAGGED>
-__global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_kernel(MxProduct q, int tiles_m, int tiles_n, int out_type, uint32_t tiles, uint32_t first_tile) {
+template <typename S, bool RAGGED, bool F32>
+__global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_kernel(MxProduct q, int tiles_m, int tiles_n, bool bf16, uint32_t tiles, uint32_t first_tile) {
     constexpr int T = S::T, NI = S::NI, NJ = S::NJ, DEPTH = S::DEPTH, WAVES = S::WAVES, PARTS = S::PARTS, WORDS = S::WORDS, LOADS = S::LOADS, FIRST = S::FIRST;
     constexpr int N = NI * NJ, F = NI + NJ;                                   // matrix instructions, fragments of a step
     constexpr bool ON = S::ON;
@@ -282,7 +301,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_
                         // requests and reads, spread over the step's matrix instructions
 #pragma unroll
                         for (int v = 0; v < LOADS; ++v) {
-                            if (s == 0 && v >= FIRST && (v - FIRST) * N / (LOADS - FIRST) == t) request(late_to, v, late, last_buf, back_late);
+                            if (s == 0 && v >= FIRST && (v - FIRST) * N / (LOADS - FIRST) == t) request(ON ? late_to : to, v, late, last_buf, back_late);
                             if (s == 3 && v < FIRST && v * N / FIRST == t) request(to, v, later, buf, back_later);
                         }
                         multiply(t / NJ, t / NJ % 2 ? NJ - 1 - t % NJ : t % NJ, s, all);         // (neighbours share an operand)
@@ -302,7 +321,6 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_
         } while (kb <= last);
         void *out = p.splits > 1 ? static_cast<void *>(p.part + (int64_t)blockIdx.y * p.M * p.N) : p.out;
         const int64_t ldo = p.splits > 1 ? p.N : p.ldo;
-        const int type = p.splits > 1 ? ICQ_F32 : out_type;
         int64_t m0, n0;
         place_of(tile, m0, n0);
         m0 += wm;
@@ -314,7 +332,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_
 #pragma unroll
             for (int i = 0; i < NI; ++i)
 #pragma unroll
-                for (int j = 0; j < NJ; j += 2) store_rows_as<2>(turn, acc[i] + j, out, type, ldo, p.M, p.N, m0 + i * 32, n0 + j * 32, lane);
+                for (int j = 0; j < NJ; j += 2) store_rows_as<F32, 2>(turn, acc[i] + j, out, bf16, ldo, p.M, p.N, m0 + i * 32, n0 + j * 32, lane);
             if (!more) break;
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup", "local");
             __builtin_amdgcn_s_barrier();
@@ -323,7 +341,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_
             __syncthreads();
             float *turn = reinterpret_cast<float *>(smem + wave * (DEPTH * S::STAGE / WAVES));
 #pragma unroll
-            for (int i = 0; i < NI; ++i) store_rows_as<NJ>(turn, acc[i], out, type, ldo, p.M, p.N, m0 + i * 32, n0, lane);
+            for (int i = 0; i < NI; ++i) store_rows_as<F32, NJ>(turn, acc[i], out, bf16, ldo, p.M, p.N, m0 + i * 32, n0, lane);
             break;
         }
         tile += gridDim.x;
@@ -341,14 +359,15 @@ int launch(const MxProduct &q, int num_cu, int out_type, hipStream_t s) {
     const auto go = [&](auto kernel) {
         if (icq_allow_lds(reinterpret_cast<const void *>(kernel), S::LDS_BYTES, true) != hipSuccess) return ICQ_ERR_HIP;
         const auto launch = [&](uint32_t blocks, uint32_t end, uint32_t first) {
-            hipLaunchKernelGGL(kernel, dim3(blocks, (uint32_t)q.p.splits), dim3(S::THREADS), S::LDS_BYTES, s, q, tm, tn, out_type, end, first);
+            hipLaunchKernelGGL(kernel, dim3(blocks, (uint32_t)q.p.splits), dim3(S::THREADS), S::LDS_BYTES, s, q, tm, tn, out_type == ICQ_BF16, end, first);
         };
         if (on && room > 0 && tiles > room) launch(room, tiles, 0);
         else
             for (uint32_t i = 0; i < tiles; i += ICQ_PRODUCT_BLOCKS) launch(std::min(tiles - i, ICQ_PRODUCT_BLOCKS), 0, i);
         return icq_check_launch();
     };
-    return q.p.K % 256 ? go(mx_tiles_kernel<S, true>) : go(mx_tiles_kernel<S, false>);
+    if (out_type == ICQ_F32 || q.p.splits > 1) return q.p.K % 256 ? go(mx_tiles_kernel<S, true, true>) : go(mx_tiles_kernel<S, false, true>);
+    return q.p.K % 256 ? go(mx_tiles_kernel<S, true, false>) : go(mx_tiles_kernel<S, false, false>);
 }
 
 }  // namespace
