@@ -9,6 +9,26 @@ constexpr int ICQ_MX_FEW_WAVES = 8;                // of a block of the kernel f
 // about 2).
 static inline bool icq_mx_few_quantises(int64_t M, int64_t per) { return per <= 32 && M * per <= 64; }
 
+// The tiles' times, by a model of them, in us, fitted to 25000 times of every form and number of parts at 3500 random sizes (17 to 8192 rows of a, 256
+// to 65536 of b, 96 to 16384 values; what it chooses takes 1 % longer than the best in the mean, 4 % in nine of ten cases): a launch, and for
+// each round of the chip's compute units (of pairs, where two blocks share one) a start with an end and a stage of 256 values, or those of a last round
+// that is not full.
+struct icq_mx_times {
+    icq_tiles tiles;
+    int T, share;              // rows and columns of a tile, blocks that share a compute unit
+    double launch, round, stage, last_round, last_stage, more;
+};
+constexpr icq_mx_times ICQ_MX_TIMES[4] = {{ICQ_TILES_WIDE, 256, 1, 4.0, 7.8, 1.5, 6.0, 1.15, 0.0}, {ICQ_TILES_SMALL, 128, 2, 2.0, 4.1, 0.98, 1.3, 0.56, 2.8},
+                                          {ICQ_TILES_DEEP, 128, 1, 2.0, 3.9, 0.48, 2.7, 0.44, 0.0}, {ICQ_TILES_LITTLE, 64, 2, 1.8, 2.6, 0.43, 1.2, 0.32, 0.7}};
+
+static inline double icq_mx_tiles_us(const icq_mx_times &t, int64_t blocks, int64_t per, int num_cu) {
+    const int64_t room = (int64_t)num_cu * t.share, left = blocks % room;
+    const double whole = t.round + t.stage * per, share = (double)left / num_cu;
+    double us = t.launch + blocks / room * whole;
+    if (t.share == 2) return us + (left > num_cu ? whole : left > 0 ? t.last_round + t.more * share + t.last_stage * per : 0.0);
+    return us + (left > 0 ? t.last_round + (t.round - t.last_round) * share + (t.last_stage + (t.stage - t.last_stage) * share) * per : 0.0);
+}
+
 // `few` rows of a: wavefronts of 32 rows of b or of 16, `along` of a block's share rows and take parts of the contraction.  Else tiles: of 256 x 256, of
 // 128 x 128 with two stages in the LDS or four, or of 64 x 64.
 struct icq_mx_plan {
@@ -40,23 +60,16 @@ static inline icq_mx_plan icq_plan_mx(int64_t M, int64_t N, int64_t K, int num_c
         return best;
     }
     double least = -1.0;
-    for (int64_t T = 256; T >= 64; T /= 2) {
-        const int64_t tiles = ((M + T - 1) / T) * ((N + T - 1) / T);
+    for (int form = 0; form < 4; ++form) {
+        const icq_mx_times &t = ICQ_MX_TIMES[form];
+        const int64_t tiles = ((M + t.T - 1) / t.T) * ((N + t.T - 1) / t.T), room = (int64_t)num_cu * t.share;
         for (int splits = 1; splits <= 16 && (splits == 1 || stages >= 2 * splits); splits *= 2) {
             const int64_t per = (stages + splits - 1) / splits, parts = (stages + per - 1) / per, blocks = tiles * parts;
-            const int64_t rounds = blocks / (2 * num_cu), left = blocks % (2 * num_cu);
-            const bool alone = blocks <= num_cu;
-            const auto last = [&](double pair, double one) { return left > num_cu ? pair : left > 0 ? one : 0.0; };
-            const double share = (double)left / num_cu;
-            double us;
-            if (T == 256) us = 1.5 * (blocks / num_cu) + (blocks % num_cu > 0 ? 1.1 + 0.4 * (blocks % num_cu) / num_cu : 0.0);
-            else if (T == 128) us = 1.0 * rounds + last(1.0, 0.5 + 0.1 * share);
-            else us = 0.45 * rounds + last(0.45, 0.3);
-            us *= per;
-            if (parts > 1) us += 2.5 + (double)parts * M * N * 8 / 4.4e6;
+            if (t.tiles == ICQ_TILES_DEEP && blocks > room) continue;
+            const double us = icq_mx_tiles_us(t, blocks, per, num_cu) + (parts > 1 ? 1.7 + 0.3 * parts + (double)parts * M * N * 8 / 4.8e6 : 0.0);
             if (least < 0.0 || us < least) {
                 least = us;
-                best.tiles = T == 256 ? ICQ_TILES_WIDE : T == 64 ? ICQ_TILES_LITTLE : alone ? ICQ_TILES_DEEP : ICQ_TILES_SMALL;
+                best.tiles = t.tiles;
                 best.splits = (int)parts;
                 best.per = (int)per;
             }
