@@ -487,26 +487,41 @@ def icq_distill_backward(logits, ids, values, scale, teacher_scale, teacher_lse,
 
 ICQ_E2M1, ICQ_MX_BLOCK = 3, 32
 ICQ_MX_FLOOR, ICQ_MX_FIT = 0, 1
+_current_device, _raw_stream_of = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 _MX_CODES = {torch.uint8: ICQ_E2M1, torch.float4_e2m1fn_x2: ICQ_E2M1}
 _MX_SCALES = {torch.uint8: 0, torch.float8_e8m0fnu: 0}
 
 
-def _here(t, name):
-    """A matrix of the current device: the work is enqueued on that device's stream."""
-    if t.get_device() != torch._C._cuda_getDevice():
-        raise ValueError("%s is on another device than the current one" % name)
+def _elsewhere(t, dtypes, name):
+    """Raises what is wrong with a tensor that is not of these types or not on the current device, on whose stream the work is enqueued."""
+    if t.dtype not in dtypes or not t.is_cuda:
+        raise TypeError("%s must be a CUDA matrix of %s" % (name, ", ".join(str(d) for d in dtypes)))
+    raise ValueError("%s is on another device than the current one" % name)
 
 
-def _mx_rows(t, dtypes, shape, step, name, written):
+def _values(t, rows, cols, name, device):
+    """(address, code of the dtype, distance between rows) of a matrix of values, as _rows; rows None: any shape."""
+    code = _TYPES.get(t.dtype)
+    if code is None or t.get_device() != device:
+        _elsewhere(t, _TYPES, name)
+    return _rows(t, _TYPES, None if rows is None else (rows, cols), name)
+
+
+def _mx_rows(t, dtypes, rows, cols, step, name, device):
     """(address, bytes between rows) of held codes or scales, whose rows take up whole `step` bytes of their own storage."""
-    ptr, _, ld = _rows(t, dtypes, shape, name)
-    _here(t, name)
-    rows, cols = t.shape
-    if rows == 1:
-        ld = -(-ld // step) * step                             # (the distance to a row that is not there)
-    if rows and cols and t.storage_offset() + (rows - 1) * ld + -(-cols // step) * step > t.untyped_storage().nbytes():
+    if t.dtype not in dtypes or t.get_device() != device:
+        _elsewhere(t, dtypes, name)
+    if t.shape != (rows, cols):
+        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), (rows, cols)))
+    ld, one = t.stride()
+    wide = -(-cols // step) * step
+    if rows <= 1:
+        ld = wide                                              # (the distance to a row that is not there)
+    if (one != 1 and cols > 1) or ld < cols:
+        raise ValueError("%s must have contiguous rows that do not overlap (strides %s)" % (name, t.stride()))
+    if rows and cols and t.storage_offset() + (rows - 1) * ld + wide > t.untyped_storage().nbytes():
         raise ValueError("%s ends before its last row's next multiple of %d bytes (see icq_mx_codes, icq_mx_scales)" % (name, step))
-    return ptr, ld
+    return t.data_ptr(), ld
 
 
 def icq_mx_codes(rows, cols, device="cuda"):
@@ -522,31 +537,31 @@ def icq_mx_scales(rows, cols, device="cuda"):
 def icq_mx_quantize(x, codes, scales, codes_t=None, scales_t=None, block_rows=1, fit=False):
     """x [rows][cols] f32 / f16 / bf16 -> codes [rows][ceil(cols/2)] and scales [rows][ceil(cols/32)] and / or those of its transpose (uint8,
     float4_e2m1fn_x2, float8_e8m0fnu, see icq_mx_codes and icq_mx_scales; either pair may be None)."""
-    xp, x_type, ldx = _rows(x, _TYPES, None, "x")
-    _here(x, "x")
+    device = _current_device()
+    xp, x_type, ldx = _values(x, None, None, "x", device)
     rows, cols = x.shape
     cp = sp = tp = stp = None
     ld = ld_s = ld_t = ld_st = 0
     if codes is not None:
-        cp, ld = _mx_rows(codes, _MX_CODES, (rows, -(-cols // 2)), 16, "codes", True)
-        sp, ld_s = _mx_rows(scales, _MX_SCALES, (rows, -(-cols // ICQ_MX_BLOCK)), 4, "scales", True)
+        cp, ld = _mx_rows(codes, _MX_CODES, rows, -(-cols // 2), 16, "codes", device)
+        sp, ld_s = _mx_rows(scales, _MX_SCALES, rows, -(-cols // ICQ_MX_BLOCK), 4, "scales", device)
     if codes_t is not None:
-        tp, ld_t = _mx_rows(codes_t, _MX_CODES, (cols, -(-rows // 2)), 16, "codes_t", True)
-        stp, ld_st = _mx_rows(scales_t, _MX_SCALES, (cols, -(-rows // ICQ_MX_BLOCK)), 4, "scales_t", True)
+        tp, ld_t = _mx_rows(codes_t, _MX_CODES, cols, -(-rows // 2), 16, "codes_t", device)
+        stp, ld_st = _mx_rows(scales_t, _MX_SCALES, cols, -(-rows // ICQ_MX_BLOCK), 4, "scales_t", device)
     rc = (_lib or load()).icq_mx_quantize(xp, x_type, rows, cols, ldx, ICQ_MX_FIT if fit else ICQ_MX_FLOOR, block_rows, cp, ld, sp, ld_s, tp, ld_t, stp, ld_st,
-                                          _raw_stream())
+                                          _raw_stream_of(device))
     if rc:
         _check(rc, "icq_mx_quantize")
 
 
 def icq_mx_dequantize(codes, scales, out):
     """out [rows][cols] f32 / f16 / bf16: the values of codes [rows][ceil(cols/2)] with scales [rows][ceil(cols/32)]."""
-    op, out_type, ldo = _rows(out, _TYPES, None, "out")
-    _here(out, "out")
+    device = _current_device()
+    op, out_type, ldo = _values(out, None, None, "out", device)
     rows, cols = out.shape
-    cp, ld = _mx_rows(codes, _MX_CODES, (rows, -(-cols // 2)), 16, "codes", False)
-    sp, ld_s = _mx_rows(scales, _MX_SCALES, (rows, -(-cols // ICQ_MX_BLOCK)), 4, "scales", False)
-    rc = (_lib or load()).icq_mx_dequantize(cp, ld, sp, ld_s, rows, cols, op, out_type, ldo, _raw_stream())
+    cp, ld = _mx_rows(codes, _MX_CODES, rows, -(-cols // 2), 16, "codes", device)
+    sp, ld_s = _mx_rows(scales, _MX_SCALES, rows, -(-cols // ICQ_MX_BLOCK), 4, "scales", device)
+    rc = (_lib or load()).icq_mx_dequantize(cp, ld, sp, ld_s, rows, cols, op, out_type, ldo, _raw_stream_of(device))
     if rc:
         _check(rc, "icq_mx_dequantize")
     return out
@@ -566,21 +581,20 @@ def icq_mx_matmul(a, a_scales, b, b_scales, out, workspace=None, K=None, fit=Fal
     if K is None:
         K = a.shape[1] if a_scales is None else 2 * b.shape[1]
     bytes_, blocks = -(-K // 2), -(-K // ICQ_MX_BLOCK)
-    op, out_type, ldo = _rows(out, _TYPES, None, "out")
-    _here(out, "out")
+    device = _current_device()
+    op, out_type, ldo = _values(out, None, None, "out", device)
     M, N = out.shape
     if a_scales is None:
-        ap, a_type, lda = _rows(a, _TYPES, (M, K), "a")
-        _here(a, "a")
+        ap, a_type, lda = _values(a, M, K, "a", device)
         sp, ld_s = None, 0
     else:
         a_type = ICQ_E2M1
-        ap, lda = _mx_rows(a, _MX_CODES, (M, bytes_), 16, "a", False)
-        sp, ld_s = _mx_rows(a_scales, _MX_SCALES, (M, blocks), 4, "a_scales", False)
-    bp, ldb = _mx_rows(b, _MX_CODES, (N, bytes_), 16, "b", False)
-    ep, ld_e = _mx_rows(b_scales, _MX_SCALES, (N, blocks), 4, "b_scales", False)
+        ap, lda = _mx_rows(a, _MX_CODES, M, bytes_, 16, "a", device)
+        sp, ld_s = _mx_rows(a_scales, _MX_SCALES, M, blocks, 4, "a_scales", device)
+    bp, ldb = _mx_rows(b, _MX_CODES, N, bytes_, 16, "b", device)
+    ep, ld_e = _mx_rows(b_scales, _MX_SCALES, N, blocks, 4, "b_scales", device)
     rc = (_lib or load()).icq_mx_matmul(ap, a_type, lda, sp, ld_s, ICQ_MX_FIT if fit else ICQ_MX_FLOOR, bp, ldb, ep, ld_e, M, N, K, op, out_type, ldo,
-                                        _ptr(workspace, torch.uint8, None, "workspace"), workspace.numel() if workspace is not None else 0, _raw_stream())
+                                        _ptr(workspace, torch.uint8, None, "workspace"), workspace.numel() if workspace is not None else 0, _raw_stream_of(device))
     if rc:
         _check(rc, "icq_mx_matmul")
     return out
@@ -618,28 +632,31 @@ def icq_grad_list_create(grads, outs=None):
     grads, outs = list(grads), None if outs is None else list(outs)
     if outs is not None and len(outs) != len(grads):
         raise ValueError("%d outs for %d gradients" % (len(outs), len(grads)))
+    device, types = _current_device(), _TYPES
     rows = []                                                  # address, type, rows, cols, ld; address, type, ld of the out
     for k, g in enumerate(grads):
         out = g if outs is None else outs[k]
-        for t, name in ((g, "grads[%d]" % k), (out, "outs[%d]" % k)):
-            if t.dtype not in _TYPES or not t.is_cuda:
-                raise TypeError("%s must be a CUDA tensor of %s" % (name, ", ".join(str(d) for d in _TYPES)))
-            _here(t, name)
+        gt, ot = types.get(g.dtype), types.get(out.dtype)
+        if gt is None or ot is None or g.get_device() != device or out.get_device() != device:
+            for t, name in ((g, "grads[%d]" % k), (out, "outs[%d]" % k)):
+                if t.dtype not in types or t.get_device() != device:
+                    _elsewhere(t, types, name)
         if out.shape != g.shape:
             raise ValueError("outs[%d] has shape %s, expected %s" % (k, tuple(out.shape), tuple(g.shape)))
         n = g.numel()
-        if n == 0 or (_without_gaps(g) and _without_gaps(out) and _same_order(g, out)):
-            rows.append((g.data_ptr(), _TYPES[g.dtype], 1, n, n, out.data_ptr(), _TYPES[out.dtype], n))
+        if n == 0 or (g.is_contiguous() and (out is g or out.is_contiguous())) or (_without_gaps(g) and _without_gaps(out) and _same_order(g, out)):
+            rows.append((g.data_ptr(), gt, 1, n, n, out.data_ptr(), ot, n))
         elif g.dim() == 2:
-            gp, gt, ld = _rows(g, _TYPES, None, "grads[%d]" % k)
-            op, ot, ldo = _rows(out, _TYPES, None, "outs[%d]" % k)
+            gp, gt, ld = _rows(g, types, None, "grads[%d]" % k)
+            op, ot, ldo = _rows(out, types, None, "outs[%d]" % k)
             rows.append((gp, gt, g.shape[0], g.shape[1], ld, op, ot, ldo))
         else:
             raise ValueError("grads[%d] must have no gaps, and outs[%d] the same order of axes" % (k, k))
-    column = lambda i, kind: (kind * len(rows))(*(r[i] for r in rows))  # noqa: E731
+    rows = list(zip(*rows)) if rows else [()] * 8
+    column = lambda i, kind: (kind * len(grads))(*rows[i])  # noqa: E731
     h = ctypes.c_void_p(0)
     rc = load().icq_grad_list_create(ctypes.byref(h), column(0, _vp), column(1, _i), column(2, _i64), column(3, _i64), column(4, _i64),
-                                     None if outs is None else column(5, _vp), column(6, _i), column(7, _i64), len(rows), _raw_stream())
+                                     None if outs is None else column(5, _vp), column(6, _i), column(7, _i64), len(grads), _raw_stream())
     _check(rc, "icq_grad_list_create")
     return GradList(h, (grads, outs))
 
