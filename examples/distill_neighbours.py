@@ -1,12 +1,15 @@
 """A scoring head learns to reproduce the neighbour lists of an index.
 
-    python examples/distill_neighbours.py
+    python examples/distill_neighbours.py [--bits 4]
 
 An index over encoded vectors answers queries (icq_search); a linear head W [items][features] learns to give each query's
 neighbours the scores the index gives them, so that afterwards one product ranks the items.  A step is five calls:
 features and weights in 8 bits with a scale per block of 128 (icq_block_quantize), logits as their product (icq_block_matmul),
 loss against the search's lists and its gradient in the logits' place (icq_distill), the gradient in 8 bits by rows and by
 columns, and the product that gives the weights' gradient.  All buffers are made once; a step allocates nothing.
+
+With --bits 4 the head is held in microscaled 4-bit floating point (icq_mx_quantize, icq_mx_matmul), has a bias for each item, and its gradients are
+clipped by their global norm before the update (icq_grad_norm_clip).
 """
 import os
 import sys
@@ -69,13 +72,53 @@ class Head:
         return self.loss
 
 
-def train(steps=60, items=8192, queries=512, d=64, features=256, topk=20, temperature=4.0, rate=8.0, seed=0):
+class MxHead:
+    """Weights [items][features] and a bias for each item in 32 bits, the weights' 4-bit form, and what a step on `rows` rows needs."""
+
+    def __init__(self, items, features, rows, max_norm=float("inf")):
+        dev = dict(device="cuda")
+        held = lambda r, c: (icq.icq_mx_codes(r, c), icq.icq_mx_scales(r, c))
+        self.max_norm = max_norm
+        self.weights, self.bias = torch.zeros((items, features), **dev), torch.zeros((items,), **dev)
+        self.w, self.x, self.xt, self.gt = held(items, features), held(rows, features), held(features, rows), held(items, rows)
+        self.logits, self.loss = torch.empty((rows, items), dtype=torch.bfloat16, **dev), torch.empty((rows,), **dev)
+        self.grad, self.bias_grad, self.norm = torch.empty((items, features), **dev), torch.empty((items,), **dev), torch.empty((1,), **dev)
+        self.grads = icq.icq_grad_list_create([self.grad, self.bias_grad])
+        need = max(icq.icq_mx_matmul_workspace_bytes(rows, items, features), icq.icq_mx_matmul_workspace_bytes(items, features, rows),
+                   icq.icq_distill_workspace_bytes(rows, items), icq.icq_grad_workspace_bytes(self.grads))
+        self.workspace = torch.empty(max(need, 256), dtype=torch.uint8, **dev)
+
+    def scores(self, features):
+        icq.icq_mx_quantize(features, *self.x, *self.xt, fit=True)
+        icq.icq_mx_quantize(self.weights, *self.w, block_rows=icq.ICQ_MX_BLOCK, fit=True)
+        icq.icq_mx_matmul(*self.x, *self.w, self.logits, self.workspace, K=features.shape[1])
+        return self.logits.add_(self.bias)
+
+    def answer(self, features):
+        """Scores of a few rows from the weights as they are held, the features quantised on the way."""
+        out = torch.empty((features.shape[0], self.bias.numel()), device="cuda")
+        return icq.icq_mx_matmul(features, None, *self.w, out, self.workspace, K=features.shape[1], fit=True).add_(self.bias)
+
+    def step(self, features, ids, dist, temperature, rate):
+        """One step of gradient descent; the losses of the rows before it."""
+        logits = self.scores(features)
+        icq.icq_distill(logits, ids, dist, 1.0, -1.0 / temperature, None, self.loss, grad=logits, workspace=self.workspace)
+        icq.icq_mx_quantize(logits, None, None, *self.gt, fit=True)
+        icq.icq_mx_matmul(*self.gt, *self.xt, self.grad, self.workspace, K=features.shape[0])
+        torch.sum(logits, 0, dtype=torch.float32, out=self.bias_grad)
+        icq.icq_grad_norm_clip(self.grads, self.norm, self.max_norm, self.workspace)
+        self.weights.add_(self.grad, alpha=-rate)
+        self.bias.add_(self.bias_grad, alpha=-rate)
+        return self.loss
+
+
+def train(steps=60, items=8192, queries=512, d=64, features=256, topk=20, temperature=4.0, rate=8.0, seed=0, bits=8):
     """Mean loss of every step, and the share of queries whose nearest item the head ranks first at the end."""
     q, ids, dist = neighbour_lists(items, queries, d, topk=topk, seed=seed)
     g = torch.Generator(device="cuda").manual_seed(seed + 1)
     x = torch.relu(q @ torch.randn((d, features), device="cuda", generator=g))
     x = (x / x.norm(dim=1, keepdim=True)).bfloat16()
-    head = Head(items, features, queries)
+    head = Head(items, features, queries) if bits == 8 else MxHead(items, features, queries, max_norm=1.0)
     losses = [head.step(x, ids, dist, temperature, rate).mean() for _ in range(steps)]
     first = head.scores(x).argmax(1) == ids[:, 0]
     return torch.stack(losses).cpu(), float(first.float().mean())
@@ -83,7 +126,7 @@ def train(steps=60, items=8192, queries=512, d=64, features=256, topk=20, temper
 
 if __name__ == "__main__":
     torch.cuda.init()
-    losses, first = train()
+    losses, first = train(bits=4 if sys.argv[1:] == ["--bits", "4"] else 8)
     for k in range(0, len(losses), 10):
         print("step %3d  loss %.4f" % (k, losses[k]))
     print("step %3d  loss %.4f; the index's nearest item ranked first for %.1f %% of the queries" % (len(losses) - 1, losses[-1], 100 * first))

@@ -510,7 +510,7 @@ int icq_distill_backward(const void *logits, int type, int64_t R, int64_t V, int
  * scale rows on 4 (pointers and ld, in bytes, multiples of these, ICQ_ERR_ARG
  * otherwise); a row's bytes up to the next multiple of 16 (4) belong to it: they
  * are zeroed where the row is written, and may be read, whatever they hold, where
- * it is read.
+ * it is read.  What a call writes shares no memory with what it reads.
  */
 #define ICQ_E2M1 3 /* a_type of icq_mx_matmul: codes */
 #define ICQ_MX_BLOCK 32
@@ -576,7 +576,8 @@ int icq_mx_matmul(const void *a, int a_type, int64_t lda, const uint8_t *a_scale
  *   factor = scale where norm <= max_norm, else scale * (max_norm / norm)  (NaN where norm is NaN)
  *   out = g * factor, in 32 bits, rounded once more to out's type
  * scale (finite, >= 0) undoes a loss scale; max_norm >= 0, may be +inf.
- * With factor 1 and outputs in place nothing is read or written.
+ * With factor 1 and outputs in place nothing is read or written a second time.
+ * 2^40 values in all at most.
  *
  * icq_grad_norm writes norm [1]; icq_grad_clip reads it (what ranks have made of
  * their norms, say); icq_grad_norm_clip does both.  Sums are in a fixed order: the

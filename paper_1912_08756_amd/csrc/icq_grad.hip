@@ -290,7 +290,7 @@ ICQ_EXPORT int icq_grad_list_create(icq_grad_list **out, const void *const *grad
             if (!in_place[i]) places.push_back({{g, rows[i], (rows[i] > 1 ? ld[i] : cols[i]) * size, cols[i] * size}, i, false});
             places.push_back({{to, rows[i], (rows[i] > 1 ? to_ld : cols[i]) * to_size, cols[i] * to_size}, i, true});
         }
-        if (total > (__int128)1 << 48 || overlap(places, in_place)) return ICQ_ERR_ARG;
+        if (total > (__int128)1 << 40 || overlap(places, in_place)) return ICQ_ERR_ARG;
         int64_t longer = 1;                                                    // (a table of 2^18 chunks and a few at most)
         while (total / (CHUNK / 4 * longer) > (1 << 18)) longer *= 2;
         for (int i = 0; i < count; ++i) {

@@ -196,8 +196,9 @@ def _check_product(got, out, x, w):
     want, size = x @ w.T, np.abs(x) @ np.abs(w).T
     half = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}[out]
     least = {"f32": 2.0 ** -149, "f16": 2.0 ** -25, "bf16": 2.0 ** -133}[out]
-    off = np.abs(got - want)
-    allowed = (x.shape[1] + 8) * 2.0 ** -24 * size + half * np.abs(want) + least
+    assert np.array_equal(np.isnan(got), np.isnan(want))       # (values beyond the type's largest make a row NaN)
+    off = np.where(np.isnan(want), 0.0, np.abs(got - want))
+    allowed = np.where(np.isnan(want), 0.0, (x.shape[1] + 8) * 2.0 ** -24 * size + half * np.abs(want) + least)
     assert (off <= allowed).all(), (np.argwhere(~(off <= allowed))[:3], off.max())
 
 
@@ -363,3 +364,99 @@ def test_the_binding_refuses_what_does_not_fit():
         b.icq_mx_matmul(x, None, codes, scales, torch.empty((4, 4), device="cuda"), K=62)
     with pytest.raises(b.IcqError):
         b.icq_mx_quantize(x, None, None)
+
+
+# ---- in graphs, on streams, on other devices
+
+@gpu
+@pytest.mark.parametrize("M", [3, 200])
+def test_captured_and_replayed_with_eager_work_between(M):
+    torch, b = _torch()
+    N, K = 500, 700
+    x, w = torch.randn((M, K), device="cuda").bfloat16(), torch.randn((N, K), device="cuda")
+    q = [b.icq_mx_codes(N, K), b.icq_mx_scales(N, K), b.icq_mx_codes(K, N), b.icq_mx_scales(K, N)]
+    y, v = torch.empty((M, N), device="cuda"), torch.empty((N, K), device="cuda")
+    space = torch.empty(max(1, b.icq_mx_matmul_workspace_bytes(M, N, K, x.dtype)), dtype=torch.uint8, device="cuda")
+
+    def run():
+        b.icq_mx_quantize(w, *q, block_rows=32, fit=True)
+        b.icq_mx_dequantize(q[0], q[1], v)
+        b.icq_mx_matmul(x, None, q[0], q[1], y, space, K=K)
+
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for seed in range(4):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        x.copy_(torch.randn((M, K), device="cuda", generator=g))
+        w.copy_(torch.randn((N, K), device="cuda", generator=g))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (*q, y, v)]
+        for t in (*q, y, v):
+            t.zero_()
+        run()
+        assert all(torch.equal(s, t) for s, t in zip(got, (*q, y, v)))
+        assert np.array_equal(_np(v), ref.values(*ref.quantize(_np(w), 32, True)))
+
+
+@gpu
+@pytest.mark.parametrize("M,N,K", [(2, 20000, 2100), (300, 4000, 1030), (1500, 1500, 9000)])
+def test_two_streams_with_a_workspace_each(M, N, K):
+    torch, b = _torch()
+    g = torch.Generator(device="cuda").manual_seed(M)
+    x, w = [torch.randn((M, K), device="cuda", generator=g).half() for _ in range(2)], torch.randn((N, K), device="cuda", generator=g)
+    wc, ws = b.icq_mx_codes(N, K), b.icq_mx_scales(N, K)
+    b.icq_mx_quantize(w, wc, ws)
+    need = max(1, b.icq_mx_matmul_workspace_bytes(M, N, K, torch.half))
+    want = []
+    for t in x:
+        want.append(b.icq_mx_matmul(t, None, wc, ws, torch.empty((M, N), device="cuda"), torch.empty(need, dtype=torch.uint8, device="cuda")))
+    torch.cuda.synchronize()
+    streams, out = [torch.cuda.Stream() for _ in x], [[torch.empty((M, N), device="cuda") for _ in range(6)] for _ in x]
+    spaces = [torch.empty(need, dtype=torch.uint8, device="cuda") for _ in x]
+    torch.cuda.synchronize()
+    for k in range(6):
+        for s, t, o, space in zip(streams, x, out, spaces):
+            with torch.cuda.stream(s):
+                b.icq_mx_matmul(t, None, wc, ws, o[k], space)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, y) for os, y in zip(out, want) for o in os)
+
+
+@gpu
+def test_values_of_wider_buffers_for_few_rows_and_many():
+    torch, b = _torch()
+    big = _values(torch, 300, 1500, "bf16", 2)
+    w = torch.randn((210, 900), device="cuda")
+    wc, ws = _held(torch, b, w)
+    wv = ref.values(*ref.quantize(_np(w)))
+    for x in (big[:5, 3:903], big[7:8, 1:901], big[::30, 600:1500], big[:200, 5:905], big.float()[:3, 1:901], big.half()[100:116, 7:907]):
+        need = b.icq_mx_matmul_workspace_bytes(x.shape[0], 210, 900, x.dtype)
+        y = torch.empty((x.shape[0], 210), device="cuda")
+        b.icq_mx_matmul(x, None, wc, ws, y, torch.empty(need, dtype=torch.uint8, device="cuda") if need else None)
+        _check_product(_np(y), "f32", ref.values(*ref.quantize(_np(x))), wv)
+
+
+@gpu
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    torch, b = _torch()
+    x = torch.randn((4, 64), device="cuda")
+    codes, scales = b.icq_mx_codes(4, 64), b.icq_mx_scales(4, 64)
+    monkeypatch.setattr(b, "_current_device", lambda: 1)
+    for call in (lambda: b.icq_mx_quantize(x, codes, scales), lambda: b.icq_mx_dequantize(codes, scales, x), lambda: b.icq_mx_matmul(x, None, codes, scales, x[:, :4]),
+                 lambda: b.icq_grad_list_create([x])):
+        with pytest.raises(ValueError):
+            call()
+
+
+@gpu
+def test_without_tensors_on_the_device_calls_say_so():
+    torch, b = _torch()
+    codes, scales = b.icq_mx_codes(4, 64), b.icq_mx_scales(4, 64)
+    with pytest.raises(TypeError):
+        b.icq_mx_quantize(torch.randn((4, 64)), codes, scales)
+    with pytest.raises(TypeError):
+        b.icq_mx_quantize(torch.randn((4, 64), device="cuda"), codes.cpu(), scales)
