@@ -329,6 +329,7 @@ ICQ_EXPORT int icq_grad_list_create(icq_grad_list **out, const void *const *grad
             if (hipMalloc(reinterpret_cast<void **>(&list->chunks), bytes) != hipSuccess ||
                 hipMemcpyAsync(list->chunks, chunks.data(), bytes, hipMemcpyHostToDevice, s) != hipSuccess || hipStreamSynchronize(s) != hipSuccess) {
                 icq_grad_list_destroy(list);
+                (void)hipGetLastError();                                       // (told here, not by the next launch's check)
                 return ICQ_ERR_HIP;
             }
         }
