@@ -11,6 +11,7 @@
 #include "icq_tiles.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace {
 
@@ -34,64 +35,59 @@ typedef Shape<2, 2, 2, 2, 2, 2> Small;
 typedef Shape<2, 2, 2, 2, 4, 1> Deep;
 typedef Shape<1, 1, 2, 2, 4, 2> Little;
 
-// PER values of a row as 16 bytes of the result's type; bf16: of the two types of 16 bits.
-template <bool F32>
-__device__ __forceinline__ uint4 sixteen(const float *x, bool bf16) {
-    if constexpr (F32) return IcqElem<ICQ_F32>::pack(x);
-    else {
-        const uint4 a = IcqElem<ICQ_BF16>::pack(x), b = IcqElem<ICQ_F16>::pack(x);
-        return make_uint4(bf16 ? a.x : b.x, bf16 ? a.y : b.y, bf16 ? a.z : b.z, bf16 ? a.w : b.w);
-    }
-}
-
 // 32 rows and 32 NJ columns of the result, whole rows at a time: in the accumulators a lane has four neighbours of one row and the lanes 32 rows, whose
-// stores would be 16 bytes here and there (64 bytes, with registers exchanged between lanes, took 2 us more for a tile of 256 x 256 than this).  They go into
-// the LDS as they are, where they lie: branches around them would have the compiler move and spill them.  turn: 32 rows of 32 NJ words, a row's
-// 16-byte pieces permuted by its number.
-template <bool F32, int NJ>
-__device__ __forceinline__ void store_rows_as(float *turn, const f32x16 *acc, void *out, bool bf16, int64_t ldo, int64_t M, int64_t N, int64_t m0, int64_t n0, int lane) {
-    constexpr int WIDTH = 32 * NJ, PER = F32 ? 4 : 8, LANES = WIDTH / PER, AT_ONCE = 64 / LANES, TIMES = 32 / AT_ONCE, SIZE = F32 ? 4 : 2;
+// stores would be 8 or 16 bytes here and there (64 bytes, with registers exchanged between lanes, took 2 us more for a tile of 256 x 256 than this).  They
+// go through the LDS in the result's type, with no branch around the accumulators (the compiler would move and spill them).  turn: 32 rows of 16-byte
+// pieces, a row's permuted by its number.
+template <int OUT, int NJ>
+__device__ __forceinline__ void store_rows_as(uint4 *turn, const f32x16 *acc, void *out, int64_t ldo, int64_t M, int64_t N, int64_t m0, int64_t n0, int lane) {
+    typedef IcqElem<OUT> Elem;
+    constexpr int WIDTH = 32 * NJ, PER = Elem::PER, PIECES = WIDTH / PER, AT_ONCE = 64 / PIECES, TIMES = 32 / AT_ONCE, SIZE = 16 / PER;
+    constexpr int SHIFT = PIECES >= 16 ? 0 : PIECES == 8 ? 1 : 2;             // 16 rows' pieces of a column fall on all banks
     const int at = lane & 31, half = lane >> 5;
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int j = 0; j < NJ; ++j)
+        if constexpr (OUT == ICQ_F32) {
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const icq_f32x4 v = {acc[j][4 * g], acc[j][4 * g + 1], acc[j][4 * g + 2], acc[j][4 * g + 3]};
-            *reinterpret_cast<icq_f32x4 *>(turn + at * WIDTH + (((j * 8 + 2 * g + half) ^ at) & (WIDTH / 4 - 1)) * 4) = v;
+            for (int g = 0; g < 4; ++g) {
+                const icq_f32x4 v = {acc[j][4 * g], acc[j][4 * g + 1], acc[j][4 * g + 2], acc[j][4 * g + 3]};
+                *reinterpret_cast<icq_f32x4 *>(turn + at * PIECES + ((j * 8 + 2 * g + half) ^ (at >> SHIFT & (PIECES - 1)))) = v;
+            }
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {                                     // a lane's halves of two pieces of eight for one whole
+                const auto first = __builtin_amdgcn_permlane32_swap(Elem::pack2(acc[j][8 * h], acc[j][8 * h + 1]), Elem::pack2(acc[j][8 * h + 4], acc[j][8 * h + 5]), false, false);
+                const auto second = __builtin_amdgcn_permlane32_swap(Elem::pack2(acc[j][8 * h + 2], acc[j][8 * h + 3]), Elem::pack2(acc[j][8 * h + 6], acc[j][8 * h + 7]), false, false);
+                turn[at * PIECES + ((j * 4 + 2 * h + half) ^ (at >> SHIFT & (PIECES - 1)))] = make_uint4(first[0], second[0], first[1], second[1]);
+            }
         }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    const int c = lane % LANES * PER, r = lane / LANES;
-    float x[TIMES][PER];
+    const int c = lane % PIECES, r = lane / PIECES;
+    uint4 x[TIMES];
 #pragma unroll
-    for (int t = 0; t < TIMES; ++t)
-#pragma unroll
-        for (int k = 0; k < PER; k += 4) *reinterpret_cast<icq_f32x4 *>(x[t] + k) = *reinterpret_cast<const icq_f32x4 *>(turn + (t * AT_ONCE + r) * WIDTH + (((c + k) / 4 ^ (t * AT_ONCE + r)) & (WIDTH / 4 - 1)) * 4);
-    uint8_t *to = static_cast<uint8_t *>(out) + ((m0 + r) * ldo + n0 + c) * SIZE;
+    for (int t = 0; t < TIMES; ++t) x[t] = turn[(t * AT_ONCE + r) * PIECES + (c ^ ((t * AT_ONCE + r) >> SHIFT & (PIECES - 1)))];
+    uint8_t *to = static_cast<uint8_t *>(out) + ((m0 + r) * ldo + n0 + c * PER) * SIZE;
     const int64_t step = AT_ONCE * ldo * SIZE;
     if (m0 + 32 <= M && n0 + WIDTH <= N) {
 #pragma unroll
-        for (int t = 0; t < TIMES; ++t) {
-            const uint4 v = sixteen<F32>(x[t], bf16);
-            __builtin_memcpy(to + t * step, &v, 16);                          // (to any address)
-        }
+        for (int t = 0; t < TIMES; ++t) __builtin_memcpy(to + t * step, &x[t], 16);              // (to any address)
         return;
     }
-    const int left = (int)min((int64_t)PER, N - n0 - c);
+    const int left = (int)max((int64_t)0, min((int64_t)PER, N - n0 - c * PER));
 #pragma unroll
     for (int t = 0; t < TIMES; ++t) {
-        const uint4 v = sixteen<F32>(x[t], bf16);
-        if (m0 + t * AT_ONCE + r >= M || left <= 0) continue;
-        if (left >= PER) {
-            __builtin_memcpy(to + t * step, &v, 16);
+        if (m0 + t * AT_ONCE + r >= M) continue;
+        if (left == PER) {
+            __builtin_memcpy(to + t * step, &x[t], 16);
             continue;
         }
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        const uint32_t w[4] = {x[t].x, x[t].y, x[t].z, x[t].w};
 #pragma unroll
         for (int e = 0; e < PER - 1; ++e)
             if (e < left) {
-                if constexpr (F32) reinterpret_cast<uint32_t *>(to + t * step)[e] = w[e];
+                if constexpr (OUT == ICQ_F32) reinterpret_cast<uint32_t *>(to + t * step)[e] = w[e];
                 else reinterpret_cast<uint16_t *>(to + t * step)[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
             }
     }
@@ -104,11 +100,11 @@ struct Target {
     uint32_t off_a[S::PARTS], off_b[S::PARTS];
 };
 
-// RAGGED: the last stage is not whole.  F32: the result's type (or that of the parts), else one of 16 bits.
+// RAGGED: the last stage is not whole.  OUT: the result's type, or that of the parts.
 // A block takes tiles blockIdx.x, + gridDim.x, ...: more than one only where S::ON, the contraction is not in parts and a row has 16 bytes of
 // scales.  The requests go on into the next tile: when this one's results are stored, the next one's first stage has arrived and the second is under way.
-template <typename S, bool RAGGED, bool F32>
-__global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_kernel(MxProduct q, int tiles_m, int tiles_n, bool bf16, uint32_t tiles, uint32_t first_tile) {
+template <typename S, bool RAGGED, int OUT>
+__global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_kernel(MxProduct q, int tiles_m, int tiles_n, uint32_t tiles, uint32_t first_tile) {
     constexpr int T = S::T, NI = S::NI, NJ = S::NJ, DEPTH = S::DEPTH, WAVES = S::WAVES, PARTS = S::PARTS, WORDS = S::WORDS, LOADS = S::LOADS, FIRST = S::FIRST;
     constexpr int N = NI * NJ, F = NI + NJ;                                   // matrix instructions, fragments of a step
     constexpr bool ON = S::ON;
@@ -180,16 +176,6 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_
     i32x4 f[2][F];                                                            // fragments of two steps: a's, then b's
     uint32_t sc[F], lo[F], hi[F];                                             // scales of the stage; of the next one as they are read
     const uint32_t pick = half ? 0x07050301u : 0x06040200u;
-    // a lane's codes and scales of the last stage that count: all others become zero in a, and their scales some number
-    uint32_t tail[4][4], keep = 0;
-    if constexpr (RAGGED) {
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const uint4 t = first_codes(make_uint4(~0u, ~0u, ~0u, ~0u), min(max(ragged - 64 * s - 32 * half, 0), 32));
-            tail[s][0] = t.x; tail[s][1] = t.y; tail[s][2] = t.z; tail[s][3] = t.w;
-            if (2 * s + half < q.blocks - 8 * whole) keep |= 0xffu << (8 * s);
-        }
-    }
     const uint8_t *row_a = smem + (wm + at) * 128, *row_b = smem + (T + wn + at) * 128;
     // fragment v of step s of the stage in place buf
     auto read = [&](int v, int s, int buf) {
@@ -210,22 +196,12 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_
             hi[v] = both.y;
         }
     };
-    // all: ~0 for a whole stage, else 0
-    auto take_scales = [&](uint32_t all) {
+    auto take_scales = [&]() {
 #pragma unroll
-        for (int v = 0; v < F; ++v) {
-            sc[v] = __builtin_amdgcn_perm(hi[v], lo[v], pick);
-            if constexpr (RAGGED) sc[v] = (sc[v] & (keep | all)) | (0x7f7f7f7fu & ~(keep | all));
-        }
+        for (int v = 0; v < F; ++v) sc[v] = __builtin_amdgcn_perm(hi[v], lo[v], pick);
     };
-    auto multiply = [&](int i, int j, int s, uint32_t all) {
-        i32x4 x = f[s & 1][NI + j], y = f[s & 1][i];
-        if constexpr (RAGGED)
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                if (j == (i % 2 ? NJ - 1 : 0)) f[s & 1][i][w] &= (int)(tail[s][w] | all);
-                y[w] = f[s & 1][i][w];
-            }
+    auto multiply = [&](int i, int j, int s) {
+        const i32x4 x = f[s & 1][NI + j], y = f[s & 1][i];
         const icq_i32x8 n = {x[0], x[1], x[2], x[3], 0, 0, 0, 0}, m = {y[0], y[1], y[2], y[3], 0, 0, 0, 0};
         const int en = (int)sc[NI + j], em = (int)sc[i];
         if (s == 0) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(n, m, acc[i][j], 4, 4, 0, en, 0, em);
@@ -233,7 +209,6 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_
         else if (s == 2) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(n, m, acc[i][j], 4, 4, 2, en, 2, em);
         else acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(n, m, acc[i][j], 4, 4, 3, en, 3, em);
     };
-    auto all_of = [&](int kb) { return RAGGED && kb == whole ? 0u : ~0u; };
 
     uint32_t tile = first_tile + blockIdx.x;
     aim(to, tile);
@@ -263,7 +238,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_
         f[0][v] = read(v, 0, 0);
         read_scales(v, k0, 0);
     }
-    take_scales(all_of(k0));
+    take_scales();
     int buf = 0, place = 0;                                                   // of the stage under way, of its four's scales
     // the stage under way is kb of `tile`; the requests in its time are of the stages kb + DEPTH - 1 and kb + DEPTH, counted on into the next tile
     for (;;) {
@@ -282,12 +257,21 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_
                 if (kb == turn + 1) late_to = to;
                 if (kb <= turn) end = min(end, kb < turn ? turn - 1 : turn);
             }
-            do {
+            const auto stage = [&](auto cut) {                                // cut: of the row's last values only, fewer than 256
+                constexpr bool CUT = decltype(cut)::value;
                 const int next_buf = (buf + 1) & (DEPTH - 1), last_buf = (buf + DEPTH - 1) & (DEPTH - 1);
                 const auto of = [&](int k) { return k <= last ? k : more ? k - last - 1 + k0 : last; };
                 const int late = of(kb + DEPTH - 1), later = of(kb + DEPTH), next = of(kb + 1);
-                const uint32_t back_late = back_of(late), back_later = back_of(later), all = all_of(kb);
+                const uint32_t back_late = back_of(late), back_later = back_of(later);
                 const int next_place = kb == group_end ? place ^ 1 : place;   // (the last of all: whatever lies there)
+                if constexpr (CUT) {                                          // scales of no block become some number, codes of no value zero in a
+                    uint32_t keep = 0;
+#pragma unroll
+                    for (int s = 0; s < 4; ++s)
+                        if (2 * s + half < q.blocks - 8 * whole) keep |= 0xffu << (8 * s);
+#pragma unroll
+                    for (int v = 0; v < F; ++v) sc[v] = (sc[v] & keep) | (0x7f7f7f7fu & ~keep);
+                }
 #pragma unroll
                 for (int s = 0; s < 4; ++s) {
                     if (s == 3) {
@@ -295,6 +279,12 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_
                         __builtin_amdgcn_s_waitcnt(loads_left((DEPTH - 2) * LOADS));
                         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup", "local");
                         __builtin_amdgcn_s_barrier();
+                    }
+                    if constexpr (CUT) {
+                        const uint4 tail = first_codes(make_uint4(~0u, ~0u, ~0u, ~0u), min(max(ragged - 64 * s - 32 * half, 0), 32));
+                        const i32x4 mask = {(int)tail.x, (int)tail.y, (int)tail.z, (int)tail.w};
+#pragma unroll
+                        for (int i = 0; i < NI; ++i) f[s & 1][i] &= mask;
                     }
 #pragma unroll
                     for (int t = 0; t < N; ++t) {
@@ -304,7 +294,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_
                             if (s == 0 && v >= FIRST && (v - FIRST) * N / (LOADS - FIRST) == t) request(ON ? late_to : to, v, late, last_buf, back_late);
                             if (s == 3 && v < FIRST && v * N / FIRST == t) request(to, v, later, buf, back_later);
                         }
-                        multiply(t / NJ, t / NJ % 2 ? NJ - 1 - t % NJ : t % NJ, s, all);         // (neighbours share an operand)
+                        multiply(t / NJ, t / NJ % 2 ? NJ - 1 - t % NJ : t % NJ, s);              // (neighbours share an operand)
 #pragma unroll
                         for (int v = 0; v < F; ++v)
                             if (v * N / F == t) {
@@ -314,9 +304,14 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 }
-                take_scales(all_of(next));
+                take_scales();
                 buf = next_buf;
-            } while (++kb <= end);
+                ++kb;
+            };
+            const int whole_end = RAGGED ? min(end, whole - 1) : end;
+            while (kb <= whole_end) stage(std::false_type());
+            if constexpr (RAGGED)
+                if (kb <= end) stage(std::true_type());
             if (kb > group_end) place ^= 1;
         } while (kb <= last);
         void *out = p.splits > 1 ? static_cast<void *>(p.part + (int64_t)blockIdx.y * p.M * p.N) : p.out;
@@ -327,21 +322,25 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_
         n0 += wn;
         if constexpr (ON) {
             // the last stage's place: of its halves of a's and of b's rows the first ones take requests, the second ones results
-            constexpr int HALF = T * 64;
-            float *turn = reinterpret_cast<float *>(smem + ((buf + DEPTH - 1) & (DEPTH - 1)) * S::STAGE + HALF + (wave & 1) * (HALF / 2) + (wave >> 1) * 2 * HALF);
+            constexpr int HALF = T * 64, AT_A_TIME = OUT == ICQ_F32 ? 2 : 4;
+            uint4 *turn = reinterpret_cast<uint4 *>(smem + ((buf + DEPTH - 1) & (DEPTH - 1)) * S::STAGE + HALF + (wave & 1) * (HALF / 2) + (wave >> 1) * 2 * HALF);
 #pragma unroll
             for (int i = 0; i < NI; ++i)
 #pragma unroll
-                for (int j = 0; j < NJ; j += 2) store_rows_as<F32, 2>(turn, acc[i] + j, out, bf16, ldo, p.M, p.N, m0 + i * 32, n0 + j * 32, lane);
+                for (int j = 0; j < NJ; j += AT_A_TIME) {
+#pragma unroll
+                    for (int e = 0; e < AT_A_TIME; ++e) asm volatile("" : "+a"(acc[i][j + e]));  // (read here, not all of them before the first branch)
+                    store_rows_as<OUT, AT_A_TIME>(turn, acc[i] + j, out, ldo, p.M, p.N, m0 + i * 32, n0 + j * 32, lane);
+                }
             if (!more) break;
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup", "local");
             __builtin_amdgcn_s_barrier();
         } else {
             __builtin_amdgcn_s_waitcnt(loads_left(0));                        // (a wavefront's part of the stages takes its results)
             __syncthreads();
-            float *turn = reinterpret_cast<float *>(smem + wave * (DEPTH * S::STAGE / WAVES));
+            uint4 *turn = reinterpret_cast<uint4 *>(smem + wave * (DEPTH * S::STAGE / WAVES));
 #pragma unroll
-            for (int i = 0; i < NI; ++i) store_rows_as<F32, NJ>(turn, acc[i], out, bf16, ldo, p.M, p.N, m0 + i * 32, n0, lane);
+            for (int i = 0; i < NI; ++i) store_rows_as<OUT, NJ>(turn, acc[i], out, ldo, p.M, p.N, m0 + i * 32, n0, lane);
             break;
         }
         tile += gridDim.x;
@@ -359,15 +358,15 @@ int launch(const MxProduct &q, int num_cu, int out_type, hipStream_t s) {
     const auto go = [&](auto kernel) {
         if (icq_allow_lds(reinterpret_cast<const void *>(kernel), S::LDS_BYTES, true) != hipSuccess) return ICQ_ERR_HIP;
         const auto launch = [&](uint32_t blocks, uint32_t end, uint32_t first) {
-            hipLaunchKernelGGL(kernel, dim3(blocks, (uint32_t)q.p.splits), dim3(S::THREADS), S::LDS_BYTES, s, q, tm, tn, out_type == ICQ_BF16, end, first);
+            hipLaunchKernelGGL(kernel, dim3(blocks, (uint32_t)q.p.splits), dim3(S::THREADS), S::LDS_BYTES, s, q, tm, tn, end, first);
         };
         if (on && room > 0 && tiles > room) launch(room, tiles, 0);
         else
             for (uint32_t i = 0; i < tiles; i += ICQ_PRODUCT_BLOCKS) launch(std::min(tiles - i, ICQ_PRODUCT_BLOCKS), 0, i);
         return icq_check_launch();
     };
-    if (out_type == ICQ_F32 || q.p.splits > 1) return q.p.K % 256 ? go(mx_tiles_kernel<S, true, true>) : go(mx_tiles_kernel<S, false, true>);
-    return q.p.K % 256 ? go(mx_tiles_kernel<S, true, false>) : go(mx_tiles_kernel<S, false, false>);
+    if (q.p.splits > 1) out_type = ICQ_F32;
+    ICQ_FOR_TYPE(out_type, return q.p.K % 256 ? go(mx_tiles_kernel<S, true, TYPE>) : go(mx_tiles_kernel<S, false, TYPE>))
 }
 
 }  // namespace
