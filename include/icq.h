@@ -566,7 +566,7 @@ int icq_mx_matmul(const void *a, int a_type, int64_t lda, const uint8_t *a_scale
  * tensor without gaps is one row), and where their clipped values go: outs NULL:
  * in their place; else addresses of their own with out_types and ld_outs (all
  * three given), of the same shape in any of the three types.  It keeps the
- * addresses, not the memory, and stays good as long as the memory does.  What is written may share
+ * addresses, not the memory, and stays good as long as the memory does; a captured graph that uses it is good as long as the list.  What is written may share
  * no memory with another matrix of the list, read or written; a matrix's own
  * place, type and ld are allowed (ICQ_ERR_ARG otherwise).  The arrays are host
  * memory.  Creation allocates and waits for a copy: not inside a captured graph.  A list

@@ -499,6 +499,14 @@ def _elsewhere(t, dtypes, name):
     raise ValueError("%s is on another device than the current one" % name)
 
 
+def _ptr_on(device, t, dtype, shape, name):
+    """_ptr of a tensor on this device."""
+    p = _ptr(t, dtype, shape, name)
+    if t is not None and t.get_device() != device:
+        _elsewhere(t, (dtype,), name)
+    return p
+
+
 def _values(t, rows, cols, name, device):
     """(address, code of the dtype, distance between rows) of a matrix of values, as _rows; rows None: any shape."""
     code = _TYPES.get(t.dtype)
@@ -594,7 +602,7 @@ def icq_mx_matmul(a, a_scales, b, b_scales, out, workspace=None, K=None, fit=Fal
     bp, ldb = _mx_rows(b, _MX_CODES, N, bytes_, 16, "b", device)
     ep, ld_e = _mx_rows(b_scales, _MX_SCALES, N, blocks, 4, "b_scales", device)
     rc = (_lib or load()).icq_mx_matmul(ap, a_type, lda, sp, ld_s, ICQ_MX_FIT if fit else ICQ_MX_FLOOR, bp, ldb, ep, ld_e, M, N, K, op, out_type, ldo,
-                                        _ptr(workspace, torch.uint8, None, "workspace"), workspace.numel() if workspace is not None else 0, _raw_stream_of(device))
+                                        _ptr_on(device, workspace, torch.uint8, None, "workspace"), workspace.numel() if workspace is not None else 0, _raw_stream_of(device))
     if rc:
         _check(rc, "icq_mx_matmul")
     return out
@@ -675,8 +683,9 @@ def icq_grad_workspace_bytes(list):
 
 def icq_grad_norm(list, norm, workspace, scale=1.0):
     """norm [1] f32 = scale times the global norm of the list's gradients."""
-    rc = (_lib or load()).icq_grad_norm(list.handle, scale, _ptr(norm, torch.float32, (1,), "norm"), _ptr(workspace, torch.uint8, None, "workspace"), workspace.numel(),
-                                        _raw_stream())
+    device = _current_device()
+    rc = (_lib or load()).icq_grad_norm(list.handle, scale, _ptr_on(device, norm, torch.float32, (1,), "norm"), _ptr_on(device, workspace, torch.uint8, None, "workspace"),
+                                        workspace.numel(), _raw_stream_of(device))
     if rc:
         _check(rc, "icq_grad_norm")
     return norm
@@ -684,15 +693,17 @@ def icq_grad_norm(list, norm, workspace, scale=1.0):
 
 def icq_grad_clip(list, norm, max_norm, scale=1.0):
     """The gradients times scale, and times max_norm / norm where norm [1] f32 is over max_norm."""
-    rc = (_lib or load()).icq_grad_clip(list.handle, scale, max_norm, _ptr(norm, torch.float32, (1,), "norm"), _raw_stream())
+    device = _current_device()
+    rc = (_lib or load()).icq_grad_clip(list.handle, scale, max_norm, _ptr_on(device, norm, torch.float32, (1,), "norm"), _raw_stream_of(device))
     if rc:
         _check(rc, "icq_grad_clip")
 
 
 def icq_grad_norm_clip(list, norm, max_norm, workspace, scale=1.0):
     """icq_grad_norm, then icq_grad_clip."""
-    rc = (_lib or load()).icq_grad_norm_clip(list.handle, scale, max_norm, _ptr(norm, torch.float32, (1,), "norm"), _ptr(workspace, torch.uint8, None, "workspace"),
-                                             workspace.numel(), _raw_stream())
+    device = _current_device()
+    rc = (_lib or load()).icq_grad_norm_clip(list.handle, scale, max_norm, _ptr_on(device, norm, torch.float32, (1,), "norm"),
+                                             _ptr_on(device, workspace, torch.uint8, None, "workspace"), workspace.numel(), _raw_stream_of(device))
     if rc:
         _check(rc, "icq_grad_norm_clip")
     return norm

@@ -277,6 +277,17 @@ def test_the_binding_refuses_what_does_not_fit():
         b.icq_grad_norm(lst, norm, space)
 
 
+@gpu
+def test_norms_and_workspaces_of_another_device_are_refused(monkeypatch):
+    torch, b = _torch()
+    lst = b.icq_grad_list_create([torch.randn(100, device="cuda")])
+    norm, space = torch.empty(1, device="cuda"), _space(torch, b, lst)
+    monkeypatch.setattr(b, "_current_device", lambda: 1)
+    for call in (lambda: b.icq_grad_norm(lst, norm, space), lambda: b.icq_grad_clip(lst, norm, 1.0), lambda: b.icq_grad_norm_clip(lst, norm, 1.0, space)):
+        with pytest.raises(ValueError):
+            call()
+
+
 # ---- on the CPU
 
 def test_bad_arguments_are_refused_before_any_device_work():
