@@ -533,8 +533,11 @@ def _mx_rows(t, dtypes, rows, cols, step, name, device):
 
 
 def icq_mx_codes(rows, cols, device="cuda"):
-    """An uninitialised matrix for [rows][cols] values in 4 bits: uint8 [rows][ceil(cols/2)], rows start on 16 bytes."""
-    return torch.empty((rows, -(-cols // 32) * 16), dtype=torch.uint8, device=device)[:, :-(-cols // 2)]
+    """An uninitialised matrix for [rows][cols] values in 4 bits: uint8 [rows][ceil(cols/2)], rows start on 16 bytes, on 128 where that takes a
+    thirty-second more at most (products of many rows read whole lines faster)."""
+    wide = -(-cols // 32) * 16
+    lines = -(-wide // 128) * 128
+    return torch.empty((rows, lines if 32 * (lines - wide) <= wide else wide), dtype=torch.uint8, device=device)[:, :-(-cols // 2)]
 
 
 def icq_mx_scales(rows, cols, device="cuda"):

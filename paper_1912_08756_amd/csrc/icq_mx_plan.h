@@ -2,11 +2,15 @@
 #pragma once
 #include "icq_matmul_plan.h"
 
-constexpr int ICQ_MX_FEW_WAVES = 8;                // of a block of the kernel for few rows
+#include <algorithm>
 
-// Whether that kernel quantises a's values itself, in every block, `per` steps of 256 values of M rows: 68 KB of the LDS at most, and while that costs
-// less than a launch of its own (values against held, 16384 x 4096, 16 steps: 1 row 8.8 - 8.6, 4 rows 10.3 - 9.2, 8 rows 12.4 - 9.8, 16 rows 16.9 - 10.8; a launch
-// about 2).
+constexpr int ICQ_MX_FEW_WAVES = 8;                // of a block of the kernel for few rows
+constexpr int ICQ_MX_FEW_LDS = 160 * 1024;         // it may use
+constexpr int ICQ_MX_FEW_STEPS = 600;              // of 256 values of one row of a that fit it (136 bytes each) beside two steps of b for each wavefront and the parts' sums
+static_assert(ICQ_MX_FEW_STEPS * 136 + 16 + ICQ_MX_FEW_WAVES * (2 * (4096 + 256) + 1024) <= ICQ_MX_FEW_LDS, "a, steps of b, sums");
+
+// Whether that kernel quantises a's values itself, in every block, `per` steps of 256 values of M rows: while that costs less than a launch of its own
+// (values against held, 16384 x 4096, 16 steps: 1 row 8.8 - 8.6, 4 rows 10.3 - 9.2, 8 rows 12.4 - 9.8, 16 rows 16.9 - 10.8; a launch about 2).
 static inline bool icq_mx_few_quantises(int64_t M, int64_t per) { return per <= 32 && M * per <= 64; }
 
 // The tiles' times, by a model of them, in us, fitted to 25000 times of every form and number of parts at 3500 random sizes (17 to 8192 rows of a, 256
@@ -40,19 +44,17 @@ struct icq_mx_plan {
 
 static inline icq_mx_plan icq_plan_mx(int64_t M, int64_t N, int64_t K, int num_cu) {
     const int64_t stages = (K + 255) / 256;
-    // (N K large: the tiles' loads into the LDS read faster, 6.3 TB/s against 5.5: 1 x 65536 x 8192 45 against 50 us, 16 x 65536 x 8192 47 against 67;
-    // 16 x 16384 x 4096 8.3 against 10.8, 1 x 16384 x 4096 8.3 against 8.6)
-    const bool long_rows = K >= 4096 && N >= 64 * (int64_t)num_cu && (M >= 8 || N * K >= (int64_t)1 << 28);
-    icq_mx_plan best = {M <= 16 && !long_rows, false, 1, ICQ_TILES_SMALL, 1, (int)stages};
+    icq_mx_plan best = {M <= 16, false, 1, ICQ_TILES_SMALL, 1, (int)stages};
     if (best.few) {
         best.wide = N >= 64 * (int64_t)num_cu;
         const int64_t groups = (N + (best.wide ? 32 : 16) - 1) / (best.wide ? 32 : 16);
-        // four wavefronts to a row as far as there are steps, eight where there are few rows
+        // four wavefronts to a row as far as there are steps, eight where there are few rows (1, 2, 4, 8 of them, in us: 8 x 1000000 x 960 116, 107, 105, 152;
+        // 8 x 500000 x 2048 111, 110, 109, 106; 1 x 100000 x 8000 106, 96, 80, 79; 1 x 16384 x 4096 13.3, 8.7, 7.0, 7.0)
         while (best.along < 4 && 2 * best.along <= stages) best.along *= 2;
         if (8 <= stages && groups * best.along < 8 * (int64_t)num_cu) best.along = 8;
-        // and as many blocks, while a wavefront keeps four steps
+        // and as many blocks, while a wavefront keeps four steps; more where a does not fit the LDS
         const int64_t blocks = (groups * best.along + ICQ_MX_FEW_WAVES - 1) / ICQ_MX_FEW_WAVES, idle = num_cu / (blocks > 0 ? blocks : 1);
-        const int64_t most = stages / (4 * best.along), n = idle < most ? idle : most;
+        const int64_t most = stages / (4 * best.along), fit = ICQ_MX_FEW_STEPS / M, n = std::max((stages + fit - 1) / fit, std::min(idle, most));
         if (n > 1) {
             best.per = (int)((stages + n - 1) / n);
             best.splits = (int)((stages + best.per - 1) / best.per);

@@ -7,6 +7,14 @@
 // A stage has four steps of 64 values. A step's fragments are read beside the matrix instructions of the step before. The one barrier of a
 // stage stands before its last step's: by then the next stage has arrived and this one's last fragments are in registers, so its place
 // in the LDS takes the stage after the next.
+//
+// Bound by the matrix instructions and the clock that they leave at 8192 x 8192 x 8192: 257 us, 4280 TFLOP/s (a large library product 308; random codes in
+// registers alone 6770; matrix pipe 48 % of the cycles, wavefronts wait for 23 %), and by the results where rows are short: 4096 x 16384 x 960 into
+// bf16 64 to 66 us, 15 of them the results' way to memory and 7 their turn through the LDS; a kernel that does nothing but fill such a result takes 21.
+// Why these tiles: a wavefront of 128 x 128 reads half the fragments from the LDS that one of 64 x 64 reads for a product, 8192^3 257 against 319 us; but
+// 4096 x 960 results of 16384 products (64 wide tiles) take 91 us so, 51 in tiles of 128 x 128, two to a compute unit, 43 with four stages.  Blocks that
+// go on to a next tile: 4096 x 16384 x 1024 59 against 66 us.  Rows of codes that start on 128 bytes are read faster: 1024 values 59 us, 960 in rows
+// of 480 bytes 66.
 #include "icq_mx.h"
 #include "icq_tiles.h"
 
@@ -43,7 +51,7 @@ template <int OUT, int NJ>
 __device__ __forceinline__ void store_rows_as(uint4 *turn, const f32x16 *acc, void *out, int64_t ldo, int64_t M, int64_t N, int64_t m0, int64_t n0, int lane) {
     typedef IcqElem<OUT> Elem;
     constexpr int WIDTH = 32 * NJ, PER = Elem::PER, PIECES = WIDTH / PER, AT_ONCE = 64 / PIECES, TIMES = 32 / AT_ONCE, SIZE = 16 / PER;
-    constexpr int SHIFT = PIECES >= 16 ? 0 : PIECES == 8 ? 1 : 2;             // 16 rows' pieces of a column fall on all banks
+    constexpr int SHIFT = PIECES >= 8 ? 0 : 1;                                // eight rows' pieces of a column fall on all banks that a write reaches at once
     const int at = lane & 31, half = lane >> 5;
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
@@ -100,14 +108,17 @@ struct Target {
     uint32_t off_a[S::PARTS], off_b[S::PARTS];
 };
 
-// RAGGED: the last stage is not whole.  OUT: the result's type, or that of the parts.
+// What is left of a row in the last stage: nothing (the stage is whole), more than half of its 256 values, or half at most.
+enum Tail { WHOLE, MORE, LESS };
+
+// OUT: the result's type, or that of the parts.
 // A block takes tiles blockIdx.x, + gridDim.x, ...: more than one only where S::ON, the contraction is not in parts and a row has 16 bytes of
 // scales.  The requests go on into the next tile: when this one's results are stored, the next one's first stage has arrived and the second is under way.
-template <typename S, bool RAGGED, int OUT>
+template <typename S, Tail TAIL, int OUT>
 __global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_kernel(MxProduct q, int tiles_m, int tiles_n, uint32_t tiles, uint32_t first_tile) {
     constexpr int T = S::T, NI = S::NI, NJ = S::NJ, DEPTH = S::DEPTH, WAVES = S::WAVES, PARTS = S::PARTS, WORDS = S::WORDS, LOADS = S::LOADS, FIRST = S::FIRST;
     constexpr int N = NI * NJ, F = NI + NJ;                                   // matrix instructions, fragments of a step
-    constexpr bool ON = S::ON;
+    constexpr bool ON = S::ON, RAGGED = TAIL != WHOLE;
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];          // stages' codes, then two places for four stages' scales
     const Product &p = q.p;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -187,10 +198,10 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES * S::SHARE / 4) void mx_tiles_
         const int row = v < NI ? wm + v * 32 + at : T + wn + (v - NI) * 32 + at;
         const int pair = (kb - k0) >> 1, at_word = 2 * kb - max(0, min(pair * 4 + 2 * k0, words - 4));
         const uint8_t *w = smem + DEPTH * S::STAGE + place * S::SCALES + (pair & 1) * 2 * T * 16 + row * 16;
-        if constexpr (RAGGED) {
+        if constexpr (TAIL == LESS) {                                         // (an odd number of words in a row)
             lo[v] = *reinterpret_cast<const uint32_t *>(w + min(at_word, 3) * 4);
             hi[v] = *reinterpret_cast<const uint32_t *>(w + min(at_word + 1, 3) * 4);
-        } else {                                                              // (an even number of words in a row)
+        } else {                                                              // (an even one: half the bank conflicts)
             const uint2 both = *reinterpret_cast<const uint2 *>(w + at_word * 4);
             lo[v] = both.x;
             hi[v] = both.y;
@@ -366,7 +377,8 @@ int launch(const MxProduct &q, int num_cu, int out_type, hipStream_t s) {
         return icq_check_launch();
     };
     if (q.p.splits > 1) out_type = ICQ_F32;
-    ICQ_FOR_TYPE(out_type, return q.p.K % 256 ? go(mx_tiles_kernel<S, true, TYPE>) : go(mx_tiles_kernel<S, false, TYPE>))
+    const int tail = (int)(q.p.K % 256);
+    ICQ_FOR_TYPE(out_type, return tail == 0 ? go(mx_tiles_kernel<S, WHOLE, TYPE>) : tail > 128 ? go(mx_tiles_kernel<S, MORE, TYPE>) : go(mx_tiles_kernel<S, LESS, TYPE>))
 }
 
 }  // namespace

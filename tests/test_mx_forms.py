@@ -12,12 +12,14 @@ PIPELINES = [(500, 65000, (2, 3, 4, 5, 6, 8, 9), "wide"), (4101, 16387, (4, 7), 
              (1300, 1900, (5, 6, 7, 8, 9, 12), "deep"), (40, 130, (1, 2, 3, 4, 5, 6, 7, 8, 9, 12), "little"), (700, 900, (1, 4, 9), "little")]
 # sizes: form and parts of the contraction
 SPLIT = [(2048, 960, 16384, "deep", 2), (256, 5003, 16001, "deep", 2), (1000, 1000, 16300, "deep", 4), (200, 131, 4100, "little", 4), (256, 256, 65000, "little", 16),
-         (130, 260, 30000, "little", 8), (12, 16384, 4096, "little", 1), (3, 65600, 4099, "little", 1)]
+         (130, 260, 30000, "little", 8), (17, 16384, 4096, "little", 1)]
 # few rows: wavefronts of 32 rows of b or of 16, how many share them, parts, whether the kernel quantises values itself
 FEW = [(1, 16384, 384, "few of 32", 2, 1, True), (3, 16500, 300, "few of 32", 2, 1, True), (16, 16390, 1030, "few of 32", 4, 1, False),
        (1, 70001, 5, "few of 32", 1, 1, True), (1, 200000, 2100, "few of 32", 4, 1, True), (8, 100003, 960, "few of 32", 4, 1, True), (8, 512, 8192, "few of 16", 8, 1, False),
        (1, 40, 20001, "few of 16", 8, 2, False), (16, 16, 65536, "few of 16", 8, 8, False), (5, 300, 700, "few of 16", 2, 1, True), (2, 4099, 4097, "few of 16", 8, 1, True),
-       (16, 300, 900, "few of 16", 4, 1, True), (1, 1, 1, "few of 16", 1, 1, True), (1, 16, 8191, "few of 16", 8, 1, True), (2, 5000, 256, "few of 16", 1, 1, True)]
+       (16, 300, 900, "few of 16", 4, 1, True), (1, 1, 1, "few of 16", 1, 1, True), (1, 16, 8191, "few of 16", 8, 1, True), (2, 5000, 256, "few of 16", 1, 1, True),
+       (12, 16384, 4096, "few of 32", 4, 1, False), (3, 65600, 4099, "few of 32", 4, 1, True), (16, 16384, 20000, "few of 32", 4, 3, False), (16, 9000, 9473, "few of 16", 4, 2, False),
+       (16, 9000, 9472, "few of 16", 4, 1, False), (1, 300, 200000, "few of 16", 8, 13, False), (11, 40000, 129, "few of 32", 1, 1, True), (6, 3000, 1500, "few of 16", 4, 1, True)]
 
 
 def _plans(tmp_path, sizes):
