@@ -6,7 +6,10 @@
 // two instructions.  a lies in the LDS whole: values are quantised by each block behind its first requests of b, which saves a launch and
 // its wait.  A block's eight wavefronts share rows of b in `along` parts of the contraction, whose sums meet in the LDS, in a fixed order.
 //
-// Bound by memory: FIGURES
+// Bound by memory: 8 x 1000000 x 960 into f32 108 us, 5.2 TB/s of b's codes and scales and of the results (a copy 5.1); 8 x 100000 x 2048, which the last-level
+// cache holds, 19.9; 1 x 16384 x 4096 7.0 held, 9.3 as values in other memory each time (its steps all arrive before the values do).  Requests into
+// registers instead, one step ahead, were bound by the lines that the first-level cache holds under way, scales' among them: 27.4 for 8 x 100000 x 2048
+// (20 without scales, 38 two steps ahead).
 #include "icq_eight.h"
 #include "icq_mx.h"
 #include "icq_tiles.h"
@@ -40,7 +43,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void mx_few_kernel(Few f, int out_ty
     const int ra = min(at, rows - 1);                                         // this lane's row of a: beyond M again M - 1's
     const int whole = (int)(p.K / 256), ragged = (int)(p.K % 256);
     uint8_t *const s_a = smem + WAVES * DEPTH * STAGE, *const s_scales = s_a + steps * rows * 128;
-    icq_f32x4 (*const s_part)[NT][64] = reinterpret_cast<icq_f32x4 (*)[NT][64]>(smem + WAVES * DEPTH * STAGE + held_bytes(p.per, rows));
+    icq_f32x4 *const s_part = reinterpret_cast<icq_f32x4 *>(smem + WAVES * DEPTH * STAGE + held_bytes(p.per, rows)) + quarter * rows + ra;   // [place][16 rows of b][quarter][row of a]
     const uint32_t mine = (uint32_t)(wave * DEPTH * STAGE);                   // (there is no other LDS: smem is at 0)
 
     // Requests, of a tile and step that run ahead: instruction i brings rows 8 i .. + 7, row r's piece c to place c ^ (r / 2 % 8), so that 16 rows' pieces fall on all
@@ -143,14 +146,14 @@ __global__ __launch_bounds__(64 * WAVES, 2) void mx_few_kernel(Few f, int out_ty
         // the parts' sums: halves onto halves
         for (int h = by / 2; h > 0; h >>= 1) {
             const int place = wave / by * (by / 2);
-            if (part >= h && part < 2 * h) {
+            if (part >= h && part < 2 * h && at < rows) {
 #pragma unroll
-                for (int j = 0; j < NT; ++j) s_part[place + part - h][j][lane] = acc[j];
+                for (int j = 0; j < NT; ++j) s_part[((place + part - h) * NT + j) * 4 * rows] = acc[j];
             }
             __syncthreads();
             if (part < h) {
 #pragma unroll
-                for (int j = 0; j < NT; ++j) acc[j] += s_part[place + part][j][lane];
+                for (int j = 0; j < NT; ++j) acc[j] += s_part[((place + part) * NT + j) * 4 * rows];
             }
             __syncthreads();
         }
@@ -171,7 +174,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void mx_few_kernel(Few f, int out_ty
 template <int TYPE>
 int launch(const Few &f, bool wide, int num_cu, int out_type, hipStream_t s) {
     const Product &p = f.q.p;
-    const auto lds = [&](int nt, int depth) { return WAVES * depth * (nt * 2048 + 256) + held_bytes(p.per, (int)p.M) + (f.along > 1 ? WAVES / 2 * nt * 1024 : 0); };
+    const auto lds = [&](int nt, int depth) { return WAVES * depth * (nt * 2048 + 256) + held_bytes(p.per, (int)p.M) + (f.along > 1 ? WAVES / 2 * nt * 64 * (int)p.M : 0); };
     const auto tiles = [&](int nt) { const int64_t rows = (int64_t)16 * nt * (WAVES / f.along); return (p.N + rows - 1) / rows; };
     const auto go = [&](auto kernel, int nt, int depth) {
         const int bytes = lds(nt, depth);
