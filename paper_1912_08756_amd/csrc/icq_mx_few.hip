@@ -178,7 +178,7 @@ int launch(const Few &f, bool wide, int num_cu, int out_type, hipStream_t s) {
     const auto tiles = [&](int nt) { const int64_t rows = (int64_t)16 * nt * (WAVES / f.along); return (p.N + rows - 1) / rows; };
     const auto go = [&](auto kernel, int nt, int depth) {
         const int bytes = lds(nt, depth);
-        if (icq_allow_lds(reinterpret_cast<const void *>(kernel), bytes) != hipSuccess) return ICQ_ERR_HIP;
+        if (icq_allow_lds(reinterpret_cast<const void *>(kernel), bytes, true) != hipSuccess) return ICQ_ERR_HIP;
         const int64_t room = (int64_t)num_cu * (2 * bytes <= ICQ_MX_FEW_LDS ? 2 : 1);
         hipLaunchKernelGGL(kernel, dim3((uint32_t)std::min(tiles(nt), room), (uint32_t)p.splits), dim3(64 * WAVES), bytes, s, f, out_type, tiles(nt));
         return icq_check_launch();

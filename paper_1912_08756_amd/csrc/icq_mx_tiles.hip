@@ -9,7 +9,7 @@
 // in the LDS takes the stage after the next.
 //
 // Bound by the matrix instructions and the clock that they leave at 8192 x 8192 x 8192: 257 us, 4280 TFLOP/s (a large library product 308; random codes in
-// registers alone 6770; matrix pipe 48 % of the cycles, wavefronts wait for 23 %), and by the results where rows are short: 4096 x 16384 x 960 into
+// registers alone 6770; matrix pipe 48 to 51 % of the cycles, wavefronts wait for 23 %), and by the results where rows are short: 4096 x 16384 x 960 into
 // bf16 64 to 66 us, 15 of them the results' way to memory and 7 their turn through the LDS; a kernel that does nothing but fill such a result takes 21.
 // Why these tiles: a wavefront of 128 x 128 reads half the fragments from the LDS that one of 64 x 64 reads for a product, 8192^3 257 against 319 us; but
 // 4096 x 960 results of 16384 products (64 wide tiles) take 91 us so, 51 in tiles of 128 x 128, two to a compute unit, 43 with four stages.  Blocks that
