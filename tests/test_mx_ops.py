@@ -441,6 +441,28 @@ def test_values_of_wider_buffers_for_few_rows_and_many():
 
 
 @gpu
+@pytest.mark.parametrize("M,N,K", [(1, 16390, 1990), (7, 700, 8000), (16, 33000, 3300), (300, 500, 1990), (700, 900, 2020)])
+def test_rows_of_codes_at_any_multiple_of_16_bytes_give_the_same_bits(M, N, K):
+    torch, b = _torch()
+    bytes_, wide = -(-K // 2), -(-K // 32) * 16
+    assert b.icq_mx_codes(N, K).stride(0) == -(-wide // 128) * 128             # (a thirty-second more at most: whole lines)
+    assert b.icq_mx_codes(N, 960).stride(0) == 480 and b.icq_mx_codes(3, 1).stride(0) == 16
+    x, w = torch.randn((M, K), device="cuda"), torch.randn((N, K), device="cuda")
+    results = []
+    for ld in (wide, wide + 16, wide + 64, -(-wide // 128) * 128):
+        held = []
+        for t in (x, w):
+            codes = torch.full((t.shape[0], ld), 0xFF, dtype=torch.uint8, device="cuda")[:, :bytes_]
+            scales = torch.full((t.shape[0], -(-K // 128) * 4 + 4), 0xFF, dtype=torch.uint8, device="cuda")[:, :-(-K // 32)]
+            b.icq_mx_quantize(t, codes, scales)
+            held += [codes, scales]
+        y = torch.empty((M, N), device="cuda")
+        need = b.icq_mx_matmul_workspace_bytes(M, N, K)
+        results.append(b.icq_mx_matmul(*held, y, torch.empty(need, dtype=torch.uint8, device="cuda") if need else None, K=K))
+    assert all(torch.equal(results[0], r) for r in results[1:])
+
+
+@gpu
 def test_tensors_of_another_device_are_refused(monkeypatch):
     torch, b = _torch()
     x = torch.randn((4, 64), device="cuda")
