@@ -509,10 +509,18 @@ def _ptr_on(device, t, dtype, shape, name):
 
 def _values(t, rows, cols, name, device):
     """(address, code of the dtype, distance between rows) of a matrix of values, as _rows; rows None: any shape."""
-    code = _TYPES.get(t.dtype)
-    if code is None or t.get_device() != device:
+    code, shape = _TYPES.get(t.dtype), t.shape
+    if code is None or t.get_device() != device or len(shape) != 2:
+        if code is not None and t.is_cuda and len(shape) != 2:
+            raise TypeError("%s must be a matrix, it has shape %s" % (name, tuple(shape)))
         _elsewhere(t, _TYPES, name)
-    return _rows(t, _TYPES, None if rows is None else (rows, cols), name)
+    m, n = shape
+    if rows is not None and (m != rows or n != cols):
+        raise ValueError("%s has shape %s, expected %s" % (name, (m, n), (rows, cols)))
+    ld, step = t.stride()
+    if (step != 1 and n > 1) or (ld < n and m > 1):
+        raise ValueError("%s must have contiguous rows that do not overlap (strides %s)" % (name, (ld, step)))
+    return t.data_ptr(), code, ld if m > 1 else max(ld, n)
 
 
 def _mx_rows(t, dtypes, rows, cols, step, name, device):
@@ -522,12 +530,13 @@ def _mx_rows(t, dtypes, rows, cols, step, name, device):
     if t.shape != (rows, cols):
         raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), (rows, cols)))
     ld, one = t.stride()
-    wide = -(-cols // step) * step
+    odd = cols % step                                          # (whole steps lie in the tensor)
+    wide = cols + step - odd if odd else cols
     if rows <= 1:
         ld = wide                                              # (the distance to a row that is not there)
     if (one != 1 and cols > 1) or ld < cols:
         raise ValueError("%s must have contiguous rows that do not overlap (strides %s)" % (name, t.stride()))
-    if rows and cols and t.storage_offset() + (rows - 1) * ld + wide > t.untyped_storage().nbytes():
+    if odd and rows and t.storage_offset() + (rows - 1) * ld + wide > t.untyped_storage().nbytes():
         raise ValueError("%s ends before its last row's next multiple of %d bytes (see icq_mx_codes, icq_mx_scales)" % (name, step))
     return t.data_ptr(), ld
 
