@@ -10,7 +10,7 @@ constexpr int ICQ_MX_FEW_STEPS = 600;              // of 256 values of one row o
 static_assert(ICQ_MX_FEW_STEPS * 136 + 16 + ICQ_MX_FEW_WAVES * (2 * (4096 + 256) + 1024) <= ICQ_MX_FEW_LDS, "a, steps of b, sums");
 
 // Whether that kernel quantises a's values itself, in every block, `per` steps of 256 values of M rows: while that costs less than a launch of its own
-// (values against held, 16384 x 4096, 16 steps: 1 row 8.8 - 8.6, 4 rows 10.3 - 9.2, 8 rows 12.4 - 9.8, 16 rows 16.9 - 10.8; a launch about 2).
+// (values against held, 16384 x 4096, 16 steps, other memory each time: 1 row 10.7 - 10.3 us, 4 rows 12.2 - 10.6; through a launch 8 rows 14.1 - 11.2).
 static inline bool icq_mx_few_quantises(int64_t M, int64_t per) { return per <= 32 && M * per <= 64; }
 
 // The tiles' times, by a model of them, in us, fitted to 25000 times of every form and number of parts at 3500 random sizes (17 to 8192 rows of a, 256
