@@ -95,9 +95,12 @@ class MxHead:
         return self.logits.add_(self.bias)
 
     def answer(self, features):
-        """Scores of a few rows from the weights as they are held, the features quantised on the way."""
-        out = torch.empty((features.shape[0], self.bias.numel()), device="cuda")
-        return icq.icq_mx_matmul(features, None, *self.w, out, self.workspace, K=features.shape[1], fit=True).add_(self.bias)
+        """Scores of any number of rows, mostly a few, from the weights as they are held, the features quantised on the way."""
+        rows, items = features.shape[0], self.bias.numel()
+        out = torch.empty((rows, items), device="cuda")
+        need = icq.icq_mx_matmul_workspace_bytes(rows, items, features.shape[1], features.dtype)
+        space = self.workspace if need <= self.workspace.numel() else torch.empty(need, dtype=torch.uint8, device="cuda")
+        return icq.icq_mx_matmul(features, None, *self.w, out, space, K=features.shape[1], fit=True).add_(self.bias)
 
     def step(self, features, ids, dist, temperature, rate):
         """One step of gradient descent; the losses of the rows before it."""
