@@ -73,7 +73,8 @@ class Head:
 
 
 class MxHead:
-    """Weights [items][features] and a bias for each item in 32 bits, the weights' 4-bit form, and what a step on `rows` rows needs."""
+    """Weights [items][features] and a bias for each item in 32 bits, the weights' 4-bit form, and what a step on `rows` rows needs.  A step changes weights
+    and bias, not the 4-bit form: hold() after the last one brings it up to date, and answer() gives scores of that head."""
 
     def __init__(self, items, features, rows, max_norm=float("inf")):
         dev = dict(device="cuda")
@@ -87,15 +88,20 @@ class MxHead:
         need = max(icq.icq_mx_matmul_workspace_bytes(rows, items, features), icq.icq_mx_matmul_workspace_bytes(items, features, rows),
                    icq.icq_distill_workspace_bytes(rows, items), icq.icq_grad_workspace_bytes(self.grads))
         self.workspace = torch.empty(max(need, 256), dtype=torch.uint8, **dev)
+        self.hold()
+
+    def hold(self):
+        """The weights' 4-bit form, from the weights as they are now."""
+        icq.icq_mx_quantize(self.weights, *self.w, block_rows=icq.ICQ_MX_BLOCK, fit=True)
 
     def scores(self, features):
         icq.icq_mx_quantize(features, *self.x, *self.xt, fit=True)
-        icq.icq_mx_quantize(self.weights, *self.w, block_rows=icq.ICQ_MX_BLOCK, fit=True)
+        self.hold()
         icq.icq_mx_matmul(*self.x, *self.w, self.logits, self.workspace, K=features.shape[1])
         return self.logits.add_(self.bias)
 
     def answer(self, features):
-        """Scores of any number of rows, mostly a few, from the weights as they are held, the features quantised on the way."""
+        """Scores of any number of rows, mostly a few, from the weights as they are held and the bias, the features quantised on the way."""
         rows, items = features.shape[0], self.bias.numel()
         out = torch.empty((rows, items), device="cuda")
         need = icq.icq_mx_matmul_workspace_bytes(rows, items, features.shape[1], features.dtype)
