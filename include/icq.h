@@ -548,7 +548,7 @@ int icq_mx_dequantize(const uint8_t *codes, int64_t ld_codes, const uint8_t *sca
  * taken as icq_mx_quantize with `scaling` and block_rows = 1 would hold them; for few
  * rows that costs no launch of its own.  With an odd K, what a row's last byte
  * holds besides its last code does not matter.
- * Rows with a NaN scale give NaN.  K = 0 gives zeros.
+ * Rows with a NaN scale give NaN, sums beyond the range of 32 bits an infinity or NaN.  K = 0 gives zeros.
  * workspace: icq_mx_matmul_workspace_bytes(M, N, K, a_type) bytes (may be 0:
  * NULL), 256-byte aligned.
  * With W held in squares of 32 x 32 as codes and codes_t, and G the gradient of
@@ -566,7 +566,10 @@ int icq_mx_matmul(const void *a, int a_type, int64_t lda, const uint8_t *a_scale
  * tensor without gaps is one row), and where their clipped values go: outs NULL:
  * in their place; else addresses of their own with out_types and ld_outs (all
  * three given), of the same shape in any of the three types.  It keeps the
- * addresses, not the memory, and stays good as long as the memory does; a captured graph that uses it is good as long as the list.  What is written may share
+ * addresses, not the memory, and stays good as long as the memory does:
+ * gradients stay where they are from step to step (zeroed, not freed), or the
+ * list is made anew.  A captured graph that uses it is good as long as the list.
+ * What is written may share
  * no memory with another matrix of the list, read or written; a matrix's own
  * place, type and ld are allowed (ICQ_ERR_ARG otherwise).  The arrays are host
  * memory.  Creation allocates and waits for a copy: not inside a captured graph.  A list

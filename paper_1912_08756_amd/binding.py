@@ -648,7 +648,8 @@ def _same_order(t, u):
 
 def icq_grad_list_create(grads, outs=None):
     """GradList of gradients (f32 / f16 / bf16 tensors without gaps, or matrices with contiguous rows); outs: where their clipped values go,
-    tensors of the same shapes and orders of axes, of any of the three types; None: in their place."""
+    tensors of the same shapes and orders of axes, of any of the three types; None: in their place.  The list keeps the tensors alive; a program whose
+    gradients are other tensors in every step makes it anew (1.5 ms for 1000 of them)."""
     grads, outs = list(grads), None if outs is None else list(outs)
     if outs is not None and len(outs) != len(grads):
         raise ValueError("%d outs for %d gradients" % (len(outs), len(grads)))

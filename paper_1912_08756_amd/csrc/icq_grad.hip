@@ -291,7 +291,7 @@ ICQ_EXPORT int icq_grad_list_create(icq_grad_list **out, const void *const *grad
             places.push_back({{to, rows[i], (rows[i] > 1 ? to_ld : cols[i]) * to_size, cols[i] * to_size}, i, true});
         }
         if (total > (__int128)1 << 40 || overlap(places, in_place)) return ICQ_ERR_ARG;
-        int64_t longer = 1;                                                    // (a table of 2^18 chunks and a few at most)
+        int64_t longer = 1;                                                    // (a table of 2^19 chunks and one for each matrix at most: rows longer than half a chunk fill it by halves)
         while (total / (CHUNK / 4 * longer) > (1 << 18)) longer *= 2;
         for (int i = 0; i < count; ++i) {
             const int type = types[i], to_type = outs ? out_types[i] : type;

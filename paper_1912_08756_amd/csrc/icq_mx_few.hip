@@ -6,10 +6,10 @@
 // two instructions.  a lies in the LDS whole: values are quantised by each block behind its first requests of b, which saves a launch and
 // its wait.  A block's eight wavefronts share rows of b in `along` parts of the contraction, whose sums meet in the LDS, in a fixed order.
 //
-// Bound by memory: 8 x 1000000 x 960 into f32 108 us, 5.2 TB/s of b's codes and scales and of the results (a copy 5.1); 8 x 100000 x 2048, which the last-level
-// cache holds, 19.9; 1 x 16384 x 4096 7.0 held, 9.3 as values in other memory each time (its steps all arrive before the values do).  Requests into
+// Bound by memory: 8 x 1000000 x 960 into f32 108 us, 5.0 TB/s of b's codes and scales and of the results (a copy 5.1); 8 x 100000 x 2048, which the last-level
+// cache holds, 20.5; 1 x 16384 x 4096 over the same memory 7.0 held or as values, over other memory each time 9.2 and 9.4.  Requests into
 // registers instead, one step ahead, were bound by the lines that the first-level cache holds under way, scales' among them: 27.4 for 8 x 100000 x 2048
-// (20 without scales, 38 two steps ahead).
+// (20 without scales, 38 two steps ahead; through the LDS 19.9 then).
 #include "icq_eight.h"
 #include "icq_mx.h"
 #include "icq_tiles.h"
@@ -183,8 +183,8 @@ int launch(const Few &f, bool wide, int num_cu, int out_type, hipStream_t s) {
         hipLaunchKernelGGL(kernel, dim3((uint32_t)std::min(tiles(nt), room), (uint32_t)p.splits), dim3(64 * WAVES), bytes, s, f, out_type, tiles(nt));
         return icq_check_launch();
     };
-    // Four steps ahead where a compute unit has one block in any case (1 x 16384 x 4096: 7.0 us, two steps 7.3), two where it can have two blocks (8 x 100000 x 2048:
-    // 19.5, four steps 19.9; 8 x 300000 x 512 14.9 and 16.6)
+    // Four steps ahead where a compute unit has one block in any case (1 x 16384 x 4096: 7.3 us, two steps 7.6), two where it can have two blocks (8 x 100000 x 2048:
+    // 20.4, four steps 21.3; 8 x 300000 x 512 16.7 and 18.0; 8 x 1000000 x 960 106.3 and 105.0)
     const int nt = wide ? 2 : 1;
     if (tiles(nt) * p.splits <= num_cu && lds(nt, 4) <= ICQ_MX_FEW_LDS) return wide ? go(mx_few_kernel<TYPE, 2, 4>, 2, 4) : go(mx_few_kernel<TYPE, 1, 4>, 1, 4);
     return wide ? go(mx_few_kernel<TYPE, 2, 2>, 2, 2) : go(mx_few_kernel<TYPE, 1, 2>, 1, 2);

@@ -14,9 +14,11 @@ static_assert(ICQ_MX_FEW_STEPS * 136 + 16 + ICQ_MX_FEW_WAVES * (2 * (4096 + 256)
 static inline bool icq_mx_few_quantises(int64_t M, int64_t per) { return per <= 32 && M * per <= 64; }
 
 // The tiles' times, by a model of them, in us, fitted to 25000 times of every form and number of parts at 3500 random sizes (17 to 8192 rows of a, 256
-// to 65536 of b, 96 to 16384 values; what it chooses takes 1 % longer than the best in the mean, 4 % in nine of ten cases): a launch, and for
-// each round of the chip's compute units (of pairs, where two blocks share one) a start with an end and a stage of 256 values, or those of a last round
-// that is not full.
+// to 65536 of b, 96 to 16384 values, over the same memory again and again, and by its own measure: what it chooses takes 1 % longer than the best in the mean, 4 % in
+// nine of ten cases): a launch, and for each round of the chip's compute units (of pairs, where two blocks share one) a start with an end and a stage of 256 values,
+// or those of a last round that is not full.  They are for the choice, not forecasts: 16384 x 960 x 4096 into f32 is modelled with 36, takes 43 so, 46 over other
+// memory each time and 49 to 53 in a training step.  There is no term for b's way from memory; 17, 32, 64 and 128 rows against 1000000 x 960 the choice was the
+// best all the same: 157, 164, 191 and 249 us, the next best form 166, 180, 226 and 259 (16 rows, by the kernel for few, 115).
 struct icq_mx_times {
     icq_tiles tiles;
     int T, share;              // rows and columns of a tile, blocks that share a compute unit

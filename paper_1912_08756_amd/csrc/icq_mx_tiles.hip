@@ -8,13 +8,14 @@
 // stage stands before its last step's: by then the next stage has arrived and this one's last fragments are in registers, so its place
 // in the LDS takes the stage after the next.
 //
-// Bound by the matrix instructions and the clock that they leave at 8192 x 8192 x 8192: 257 us, 4280 TFLOP/s (a large library product 308; random codes in
-// registers alone 6770; matrix pipe 48 to 51 % of the cycles, wavefronts wait for 23 %), and by the results where rows are short: 4096 x 16384 x 960 into
-// bf16 64 to 66 us, 15 of them the results' way to memory and 7 their turn through the LDS; a kernel that does nothing but fill such a result takes 21.
-// Why these tiles: a wavefront of 128 x 128 reads half the fragments from the LDS that one of 64 x 64 reads for a product, 8192^3 257 against 319 us; but
-// 4096 x 960 results of 16384 products (64 wide tiles) take 91 us so, 51 in tiles of 128 x 128, two to a compute unit, 43 with four stages.  Blocks that
-// go on to a next tile: 4096 x 16384 x 1024 59 against 66 us.  Rows of codes that start on 128 bytes are read faster: 1024 values 59 us, 960 in rows
-// of 480 bytes 66.
+// Bound by the matrix instructions and the clock that they leave at 8192 x 8192 x 8192: 264 us over the same memory again and again, 4170 TFLOP/s, 272 to 292
+// over other memory each time, 3770 to 4040 (a large library product 308, 3565; random codes in registers alone 6770; matrix pipe 49 % of the cycles, wavefronts
+// wait for 28 %), and by the results where rows are short: 4096 x 16384 x 960 into bf16 64 us over the same memory, 69 over other, 15 of them the
+// results' way to memory and 7 their turn through the LDS; a kernel that does nothing but fill such a result takes 21.
+// Why these tiles (same memory, other memory): a wavefront of 128 x 128 reads half the fragments from the LDS that one of 64 x 64 reads for a product, 8192^3
+// 264 and 272 against 321 and 359 us; but 4096 x 960 results of 16384 products (64 wide tiles) take 95 us so, 52 in tiles of 128 x 128, two to a compute
+// unit, 44 with four stages.  Blocks that go on to a next tile: 4096 x 16384 x 1024 59 against 66 us when that was taken, 61 now with the wait states in
+// the loads' text.  Rows of codes that start on 128 bytes are read faster: 1024 values 61 us, 960 in rows of 480 bytes 64.
 #include "icq_mx.h"
 #include "icq_tiles.h"
 
